@@ -243,6 +243,81 @@ size_t dense_attn_workspace_bytes(const mrt_problem* p, int causal_chunk);
 mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* O, const mrt_problem* p,
                              int causal_chunk, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Training step of the dense attention: the forward call that keeps its row statistics, and the
+ * gradients of  sum(O * dO)  from them.  The probabilities are formed again from Q, K and lse.
+ *   kv_heads  heads of K, V, dK and dV ([batch, kv_heads, N_kv, head_dim]); query head i reads key head
+ *             i / (heads / kv_heads), and the gradient of a shared head is the sum over its query heads.
+ *             0: as many as heads.
+ *   kv_len    device memory, int [batch], or NULL: keys at and behind kv_len[b] (taken as 0 .. N_kv) are
+ *             padding that no query of sequence b sees; dK and dV are zero there, and what K and V hold there
+ *             does not matter.  A row that sees no key has O = 0, lse = -infinity and gradients of zero.
+ *   dout, dq, dk, dv   element strides of dO and the gradients (the backward call only).
+ * lse: device memory, fp32, [batch, heads, N_q]: the natural logarithm of the sum of the exponentials of a
+ *   row's scaled, visible logits.  O, dO, dQ, dK and dV have the storage type of Q, K and V; everything is fully
+ *   overwritten, and no output overlaps an input or another output.
+ * Arithmetic.  MRT_BF16 storage with MRT_COMPUTE_DEFAULT (head_dim 64 or 128): bf16 matrix operands (the
+ *   probabilities and the gradients of the logits are rounded to bf16, by 2^-8 of the value at most), fp32
+ *   accumulation; gradients within 1e-2 of the exact ones in the 2-norm (typically 3e-3).
+ *   Otherwise fp32 throughout, within 1e-5.  The same call gives the same bits every time (no atomics).  O and lse
+ *   are those of dense_attn_fwd_ws with the same workspace (dense_attn_workspace_bytes; optional).
+ * As in the forward pass an infinite or NaN key, value, query or gradient that is hidden by causal_chunk from some
+ *   rows of a run of 256, and seen by others, may show in them all; one behind kv_len never shows.
+ * dense_attn_bwd needs dense_attn_bwd_workspace_bytes() bytes of scratch (device, 256-byte aligned, contents
+ *   undefined on entry and exit; 0: invalid arguments).  dense_attn_bwd_check applies the same rules as the call.
+ *   Thread safety as for monarch_attn_fwd; every launch is on hip_stream. */
+typedef struct {
+  int kv_heads;
+  const int* kv_len;
+  mrt_strides dout, dq, dk, dv;
+} mrt_dense_train;
+mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void* O, float* lse, const mrt_problem* p,
+                               const mrt_dense_train* t, int causal_chunk, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+mrt_status dense_attn_bwd_check(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk);
+size_t dense_attn_bwd_workspace_bytes(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk);
+mrt_status dense_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* lse,
+                          void* dQ, void* dK, void* dV, const mrt_problem* p, const mrt_dense_train* t, int causal_chunk,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Rotary positions with three axes (frame, height, width): what a layer applies to its queries and keys before
+ * either attention, and to their gradients after it.  Pair p of a token at position x of the pair's axis is turned
+ * by the angle  x theta^(-e):
+ *     y0 = x0 cos - x1 sin,   y1 = x0 sin + x1 cos        (mrt_rotary_bwd: by the opposite angle)
+ *   pairs[a]  rotary pairs of axis a (frame, height, width), in this order; features beyond 2 (pairs[0] + pairs[1] +
+ *             pairs[2]) are copied.
+ *   layout    MRT_ROTARY_ADJACENT: pair p is features 2p and 2p + 1.  MRT_ROTARY_HALVES: p and p + the number of pairs.
+ *   ladder    MRT_ROTARY_PER_AXIS: e = i / pairs[a] for the i-th pair of axis a.  MRT_ROTARY_SHARED: e = p / the number
+ *             of pairs, one ladder shared out over the axes.
+ * A tensor [batch, heads, f*h*w tokens, head_dim] has the positions of its grid, frame_offset + frame, row and column,
+ *   or, with `positions` (device memory, int32, element strides position_batch, position_axis and 1), its own: a token
+ *   of text has the same on every axis.  Angles are formed in 64 bits, exact to 1e-7 for every 32-bit position;
+ *   products and sums in fp32, rounded once to the type of Y.
+ * One call rotates one or two tensors (queries and keys, which may differ in heads, frames and types).  Y may be X
+ *   itself with the same type and strides; otherwise they do not overlap. */
+typedef enum { MRT_ROTARY_ADJACENT = 0, MRT_ROTARY_HALVES = 1 } mrt_rotary_layout;
+typedef enum { MRT_ROTARY_PER_AXIS = 0, MRT_ROTARY_SHARED = 1 } mrt_rotary_ladder;
+typedef struct {
+  int head_dim;            /* 1..256 */
+  int pairs[3];
+  mrt_rotary_layout layout;
+  mrt_rotary_ladder ladder;
+  double theta;            /* 1..1e12 */
+} mrt_rotary;
+typedef struct {
+  int batch, heads;
+  int f, h, w;
+  int frame_offset;
+  mrt_strides x, y;        /* element strides of X and Y; head_dim is contiguous */
+  mrt_dtype x_dtype, y_dtype;
+  const int* positions;    /* device memory, or NULL: the grid's */
+  long long position_batch, position_axis;
+} mrt_rotary_tensor;
+mrt_status mrt_rotary_check(const mrt_rotary* r, const mrt_rotary_tensor* x, int n);
+mrt_status mrt_rotary_fwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n, const void* const* X, void* const* Y,
+                      void* hip_stream);
+mrt_status mrt_rotary_bwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n, const void* const* dY, void* const* dX,
+                      void* hip_stream);
+
 /* Number of head groups monarch_attn_fwd and monarch_attn_bwd run concurrently: 1..4, or 0 (default) to let the library
  * choose per call (one group unless the launches are long and their grids small).  With more than one
  * group the library forks helper HIP streams from hip_stream and joins them back before it
@@ -261,10 +336,11 @@ void mrt_set_head_groups(int n);
  * library creates HIP objects, and while it is on head groups run one after the other.
  * mrt_profile_read waits for the recorded events, writes up to `capacity` (elapsed milliseconds
  * per launch, kernel kind) pairs in launch order, forgets them and returns how many it wrote.
- * Kernel kind = one of MRT_KERNEL_STAGE_R / MRT_KERNEL_STAGE_L / MRT_KERNEL_DENSE, or-ed with
+ * Kernel kind = one of MRT_KERNEL_STAGE_R / MRT_KERNEL_STAGE_L / MRT_KERNEL_DENSE, MRT_KERNEL_DENSE_BWD
+ * (all launches of a dense_attn_bwd call) or MRT_KERNEL_ROTARY, or-ed with
  * MRT_KERNEL_FIRST (first iteration: alpha_R is Q itself) and MRT_KERNEL_LAST (last iteration:
  * stage R also forms Y, stage L forms O). */
-enum { MRT_KERNEL_STAGE_R = 1, MRT_KERNEL_STAGE_L = 2, MRT_KERNEL_DENSE = 4,
+enum { MRT_KERNEL_STAGE_R = 1, MRT_KERNEL_STAGE_L = 2, MRT_KERNEL_DENSE = 4, MRT_KERNEL_DENSE_BWD = 8, MRT_KERNEL_ROTARY = 64,
        MRT_KERNEL_FIRST = 16, MRT_KERNEL_LAST = 32 };
 void mrt_profile_enable(int repeats);
 int mrt_profile_read(float* ms, int* kind, int capacity);

@@ -26,10 +26,15 @@ EXPORTED = [
     "monarch_attn_fwd_noalloc",
     "monarch_attn_bwd_saved_workspace_bytes", "monarch_attn_fwd_save", "monarch_attn_bwd_saved",
     "dense_attn_workspace_bytes", "dense_attn_fwd_ws",
+    "dense_attn_fwd_save", "dense_attn_bwd", "dense_attn_bwd_check", "dense_attn_bwd_workspace_bytes",
+    "mrt_rotary_check", "mrt_rotary_fwd", "mrt_rotary_bwd",
 ]
 NOALLOC_SCRATCH_BYTES = 128 << 20
 ASSIGNMENTS = {"fh_w": 0, "w_fh": 1, "fw_h": 2, "h_fw": 3, "f_hw": 4, "hw_f": 5}
 KERNEL_STAGE_R, KERNEL_STAGE_L, KERNEL_DENSE, KERNEL_FIRST, KERNEL_LAST = 1, 2, 4, 16, 32
+KERNEL_DENSE_BWD, KERNEL_ROTARY = 8, 64
+ROTARY_LAYOUTS = {"adjacent": 0, "halves": 1}
+ROTARY_LADDERS = {"axis": 0, "shared": 1}
 
 
 class MrtStrides(ctypes.Structure):
@@ -45,6 +50,23 @@ class MrtProblem(ctypes.Structure):
         ("dtype", ctypes.c_int), ("compute", ctypes.c_int), ("scale", ctypes.c_float),
         ("assignment", ctypes.c_int), ("tile_h", ctypes.c_int), ("head_groups", ctypes.c_int),
     ]
+
+
+class MrtDenseTrain(ctypes.Structure):
+    _fields_ = [("kv_heads", ctypes.c_int), ("kv_len", ctypes.c_void_p),
+                ("dout", MrtStrides), ("dq", MrtStrides), ("dk", MrtStrides), ("dv", MrtStrides)]
+
+
+class MrtRotary(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int), ("pairs", ctypes.c_int * 3), ("layout", ctypes.c_int),
+                ("ladder", ctypes.c_int), ("theta", ctypes.c_double)]
+
+
+class MrtRotaryTensor(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("heads", ctypes.c_int), ("f", ctypes.c_int), ("h", ctypes.c_int),
+                ("w", ctypes.c_int), ("frame_offset", ctypes.c_int), ("x", MrtStrides), ("y", MrtStrides),
+                ("x_dtype", ctypes.c_int), ("y_dtype", ctypes.c_int), ("positions", ctypes.c_void_p),
+                ("position_batch", ctypes.c_longlong), ("position_axis", ctypes.c_longlong)]
 
 
 class MrtError(RuntimeError):
@@ -98,6 +120,21 @@ def load_library() -> ctypes.CDLL:
     lib.dense_attn_workspace_bytes.restype = sz
     lib.dense_attn_fwd_ws.argtypes = [vp, vp, vp, vp, P, ci, vp, sz, vp]
     lib.dense_attn_fwd_ws.restype = ci
+    T = ctypes.POINTER(MrtDenseTrain)
+    lib.dense_attn_fwd_save.argtypes = [vp, vp, vp, vp, vp, P, T, ci, vp, sz, vp]
+    lib.dense_attn_fwd_save.restype = ci
+    lib.dense_attn_bwd_check.argtypes = [P, T, ci]
+    lib.dense_attn_bwd_check.restype = ci
+    lib.dense_attn_bwd_workspace_bytes.argtypes = [P, T, ci]
+    lib.dense_attn_bwd_workspace_bytes.restype = sz
+    lib.dense_attn_bwd.argtypes = [vp] * 9 + [P, T, ci, vp, sz, vp]
+    lib.dense_attn_bwd.restype = ci
+    R, X = ctypes.POINTER(MrtRotary), ctypes.POINTER(MrtRotaryTensor)
+    lib.mrt_rotary_check.argtypes = [R, X, ci]
+    lib.mrt_rotary_check.restype = ci
+    for f in (lib.mrt_rotary_fwd, lib.mrt_rotary_bwd):
+        f.argtypes = [R, X, ci, vp, vp, vp]
+        f.restype = ci
     lib.mrt_status_string.argtypes = [ci]
     lib.mrt_status_string.restype = ctypes.c_char_p
     lib.mrt_last_error.argtypes = []
@@ -384,3 +421,238 @@ def dense_attn_fwd(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0
     if st != MRT_OK:
         _raise(lib, st)
     return O
+
+
+# ---- a training step of the dense attention, rotary positions ------------------------------------
+def _require(ok, text, status=MRT_ERR_SHAPE):
+    if not ok:
+        raise MrtError(status, text)
+
+
+class _on:
+    """Q's device and the call's stream as torch's current ones while a call allocates and launches: memory taken
+    from torch is then ordered by the stream that uses it.  Does nothing where they are current already."""
+
+    def __init__(self, Q, stream):
+        import torch
+        self.stream, self.device, self.inner = _stream_of(Q, stream), None, None
+        if Q.device.index != torch.cuda.current_device():
+            self.device = torch.cuda.device(Q.device)
+        if self.stream != _stream_of(Q, None):
+            self.inner = torch.cuda.stream(torch.cuda.ExternalStream(self.stream, Q.device) if self.stream
+                                           else torch.cuda.default_stream(Q.device))
+
+    def __enter__(self):
+        if self.device is not None:
+            self.device.__enter__()
+        if self.inner is not None:
+            self.inner.__enter__()
+        return self.stream
+
+    def __exit__(self, *error):
+        if self.inner is not None:
+            self.inner.__exit__(*error)
+        if self.device is not None:
+            self.device.__exit__(*error)
+
+
+def _dtype_of(x, name):
+    import torch
+    _require(x.dtype in (torch.float32, torch.bfloat16), f"{name}: fp32 or bf16, got {x.dtype}")
+    return MRT_F32 if x.dtype == torch.float32 else MRT_BF16
+
+
+def _same_device(first, **others):
+    _require(first.is_cuda, "tensors must be on a GPU")
+    for name, x in others.items():
+        _require(x.device == first.device, f"{name} is on {x.device}, not on {first.device}")
+
+
+# (problem, training description without kv_len) of recent calls by their values, like _problems
+_train_problems: dict = {}
+
+
+def _train_problem(Q, K, V, O, grads, f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute):
+    key = (Q.shape, K.shape, V.shape, Q.dtype, Q.stride(), K.stride(), V.stride(), O.stride(),
+           tuple([g.stride() for g in grads]), f_q, f_kv, h, w, q_frame_offset, scale, compute)
+    found = _train_problems.get(key)
+    if found is not None:
+        return found
+    _require(Q.dim() == 4 and K.dim() == 4 and K.shape == V.shape, "Q, K and V are [batch, heads, tokens, head_dim], K like V")
+    B, H, nq, d = Q.shape
+    _require(nq == f_q * h * w, f"Q has {nq} tokens, the grid {f_q * h * w}")
+    _require(K.shape[0] == B and K.shape[2] == f_kv * h * w and K.shape[3] == d,
+             f"K and V are [{B}, heads, {f_kv * h * w}, {d}], got {tuple(K.shape)}")
+    for x in (Q, K, V, O, *grads):
+        _require(x.stride(3) == 1, "head_dim must be contiguous")
+
+    def st(x):
+        return x.stride()[:3]
+    prob = make_problem(batch=B, heads=H, head_dim=d, f_q=f_q, f_kv=f_kv, h=h, w=w, q_frame_offset=q_frame_offset,
+                        dtype=_dtype_of(Q, "Q"), compute=compute, scale=scale, q_strides=st(Q), k_strides=st(K),
+                        v_strides=st(V), o_strides=st(O))
+    train = MrtDenseTrain(K.shape[1], None, *[MrtStrides(*st(x)) for x in grads])
+    if len(_train_problems) >= _MAX_PROBLEMS:
+        _train_problems.clear()
+    _train_problems[key] = prob, train
+    return prob, train
+
+
+def _with_lengths(train, kv_len, batch):
+    if kv_len is None:
+        return train
+    import torch
+    _require(kv_len.dtype == torch.int32 and kv_len.shape == (batch,) and kv_len.stride(0) == 1,
+             f"kv_len: int32 [{batch}], contiguous")
+    return MrtDenseTrain(train.kv_heads, kv_len.data_ptr(), train.dout, train.dq, train.dk, train.dv)
+
+
+def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0, kv_len=None,
+                        compute=MRT_COMPUTE_DEFAULT, out=None, lse=None, workspace=None, stream=None):
+    """Forward call of a training step of the dense attention: (O, lse) for dense_attn_bwd.
+
+    Q [batch, heads, tokens, head_dim]; K and V [batch, kv_heads, tokens, head_dim], where kv_heads divides heads.
+    lse [batch, heads, tokens], fp32: the natural logarithm of the sum of a row's exponentials, -inf for a row that
+    sees no key (its O is 0).  kv_len (int32 [batch], on the device): keys from there on are padding.  O and lse are
+    those of dense_attn_fwd, scratch memory (`workspace`) and what it decides included."""
+    import torch
+    lib = load_library()
+    _same_device(Q, K=K, V=V, **{n: x for n, x in (("out", out), ("lse", lse), ("kv_len", kv_len), ("workspace", workspace))
+                                 if x is not None})
+    _require(Q.dtype == K.dtype == V.dtype, "Q, K and V have one type")
+    with _on(Q, stream) as s:
+        O = torch.empty_like(Q) if out is None else out
+        _require(O.shape == Q.shape and O.dtype == Q.dtype, "out has the shape and type of Q")
+        prob, train = _train_problem(Q, K, V, O, (), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute)
+        if lse is None:
+            lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+        _require(lse.shape == Q.shape[:3] and lse.dtype == torch.float32 and lse.is_contiguous(),
+                 "lse is fp32 [batch, heads, tokens], contiguous")
+        train = _with_lengths(train, kv_len, Q.shape[0])
+        if workspace is None:
+            workspace = _dense_scratch(prob, causal_chunk, Q, s)
+        ws, nbytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        st = lib.dense_attn_fwd_save(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(),
+                                     ctypes.byref(prob), ctypes.byref(train), causal_chunk, ws, nbytes, s)
+    if st != MRT_OK:
+        _raise(lib, st)
+    return O, lse
+
+
+def dense_attn_bwd_workspace_bytes(prob: MrtProblem, train: MrtDenseTrain, causal_chunk=0) -> int:
+    """Scratch a backward call needs (0: invalid arguments)."""
+    return int(load_library().dense_attn_bwd_workspace_bytes(ctypes.byref(prob), ctypes.byref(train), causal_chunk))
+
+
+def dense_attn_bwd(Q, K, V, O, dO, lse, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0, kv_len=None,
+                   compute=MRT_COMPUTE_DEFAULT, out=None, workspace=None, stream=None):
+    """Gradients (dQ, dK, dV) of sum(O * dO), in the type of Q, K and V, from the forward call's O and lse
+    (dense_attn_fwd_save with the same arguments).  The probabilities are formed again, nothing of their size is kept.
+    out: (dQ, dK, dV) to write.  workspace: scratch of dense_attn_bwd_workspace_bytes() bytes (torch's by default)."""
+    import torch
+    lib = load_library()
+    _same_device(Q, K=K, V=V, O=O, dO=dO, lse=lse,
+                 **{n: x for n, x in (("kv_len", kv_len), ("workspace", workspace)) if x is not None})
+    _require(Q.dtype == K.dtype == V.dtype == O.dtype == dO.dtype, "Q, K, V, O and dO have one type")
+    _require(O.shape == Q.shape and dO.shape == Q.shape, "O and dO have the shape of Q")
+    _require(lse.shape == Q.shape[:3] and lse.dtype == torch.float32 and lse.is_contiguous(),
+             "lse is fp32 [batch, heads, tokens], contiguous")
+    with _on(Q, stream) as s:
+        dQ, dK, dV = out if out is not None else (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V))
+        _same_device(Q, dQ=dQ, dK=dK, dV=dV)
+        _require(dQ.shape == Q.shape and dK.shape == K.shape and dV.shape == V.shape and
+                 dQ.dtype == dK.dtype == dV.dtype == Q.dtype, "gradients have the shapes and the type of Q, K and V")
+        prob, train = _train_problem(Q, K, V, O, (dO, dQ, dK, dV), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale,
+                                     compute)
+        train_now = _with_lengths(train, kv_len, Q.shape[0])
+        if workspace is None:
+            known = prob.__dict__.setdefault("dense_bwd_bytes", {})
+            nbytes = known.get(causal_chunk)
+            if nbytes is None:
+                nbytes = known[causal_chunk] = dense_attn_bwd_workspace_bytes(prob, train, causal_chunk)
+            if nbytes == 0:
+                _raise(lib, lib.dense_attn_bwd_check(ctypes.byref(prob), ctypes.byref(train), causal_chunk))
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
+        st = lib.dense_attn_bwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), dO.data_ptr(), lse.data_ptr(),
+                                dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ctypes.byref(prob), ctypes.byref(train_now),
+                                causal_chunk, workspace.data_ptr(), workspace.numel() * workspace.element_size(), s)
+    if st != MRT_OK:
+        _raise(lib, st)
+    return dQ, dK, dV
+
+
+def rotary_pairs_split(head_dim: int):
+    """Rotary pairs of (frame, height, width) by default: thirds, the rest to the frame (64 pairs -> 22, 21, 21)."""
+    pairs = head_dim // 2
+    return pairs - 2 * (pairs // 3), pairs // 3, pairs // 3
+
+
+def _rotary_tensor(x, y, f, h, w, offset, positions, name):
+    import torch
+    _require(x.dim() == 4 and x.stride(3) == 1 and y.stride(3) == 1, f"{name}: [batch, heads, tokens, head_dim], head_dim contiguous")
+    _require(y.shape == x.shape, f"{name}: the output has another shape")
+    B, H, n, _ = x.shape
+    if positions is not None:
+        _require(positions.dtype == torch.int32 and positions.shape in ((3, n), (B, 3, n)) and (n == 1 or positions.stride(-1) == 1),
+                 f"{name}: positions are int32 [3, {n}] or [{B}, 3, {n}]")
+        f, h, w, offset = 1, 1, n, 0
+        pos = positions.data_ptr(), positions.stride(0) if positions.dim() == 3 else 0, positions.stride(-2)
+    else:
+        _require(f is not None and h is not None and w is not None, f"{name}: neither a grid nor positions")
+        _require(n == f * h * w, f"{name} has {n} tokens, its grid {f * h * w}")
+        pos = None, 0, 0
+    return MrtRotaryTensor(B, H, f, h, w, offset, MrtStrides(*x.stride()[:3]), MrtStrides(*y.stride()[:3]),
+                           _dtype_of(x, name), _dtype_of(y, name), *pos)
+
+
+def _rotary(entry, Q, K, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder, q_positions,
+            k_positions, dtype, out, k_out, stream):
+    import torch
+    lib = load_library()
+    _same_device(Q, **{n: x for n, x in (("K", K), ("q_positions", q_positions), ("k_positions", k_positions), ("out", out),
+                                         ("k_out", k_out)) if x is not None})
+    _require(layout in ROTARY_LAYOUTS, f"layout is one of {sorted(ROTARY_LAYOUTS)}")
+    _require(ladder in ROTARY_LADDERS, f"ladder is one of {sorted(ROTARY_LADDERS)}")
+    split = tuple(rotary_pairs_split(Q.shape[-1]) if split is None else split)
+    _require(len(split) == 3, "split: rotary pairs of the frame, height and width axis")
+    r = MrtRotary(Q.shape[-1], (ctypes.c_int * 3)(*split), ROTARY_LAYOUTS[layout], ROTARY_LADDERS[ladder], theta)
+    with _on(Q, stream) as s:
+        Y = torch.empty_like(Q, dtype=dtype) if out is None else out
+        tensors, x, y = [_rotary_tensor(Q, Y, f_q, h, w, q_frame_offset, q_positions, "Q")], [Q], [Y]
+        if K is not None:
+            _require(K.shape[-1] == Q.shape[-1], "Q and K have one head_dim")
+            y.append(torch.empty_like(K, dtype=dtype) if k_out is None else k_out)
+            x.append(K)
+            tensors.append(_rotary_tensor(K, y[1], f_q if f_kv is None else f_kv, h, w, kv_frame_offset, k_positions, "K"))
+        n = len(x)
+        pointers = ctypes.c_void_p * n
+        st = getattr(lib, entry)(ctypes.byref(r), (MrtRotaryTensor * n)(*tensors), n, pointers(*[t.data_ptr() for t in x]),
+                                 pointers(*[t.data_ptr() for t in y]), s)
+    if st != MRT_OK:
+        _raise(lib, st)
+    return tuple(y) if n > 1 else y[0]
+
+
+def rotary_fwd(Q, K=None, *, f_q=None, f_kv=None, h=None, w=None, q_frame_offset=0, kv_frame_offset=0, theta=10000.0,
+               split=None, layout="adjacent", ladder="axis", q_positions=None, k_positions=None, dtype=None, out=None,
+               k_out=None, stream=None):
+    """Rotary positions with three axes on Q and K, [batch, heads, tokens, head_dim], in one launch: (Q', K'), or Q'
+    where K is None.  The numbers of heads may differ.
+
+    Positions: those of the grids (f_q, h, w) and (f_kv, h, w), frames counted from the offsets, or q_positions /
+    k_positions, int32 [3, tokens] or [batch, 3, tokens].  split: rotary pairs of the three axes (by default thirds
+    of head_dim); features behind them are copied.  layout "adjacent": a pair is features 2p, 2p + 1; "halves": p and
+    p + the number of pairs.  ladder "axis": every axis has the frequencies theta^(-i / its pairs); "shared": one
+    ladder theta^(-p / all pairs) is shared out.  dtype: of the results (that of Q and K by default).  out / k_out may
+    be Q / K themselves, or the place in a cache where the keys belong."""
+    return _rotary("mrt_rotary_fwd", Q, K, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder,
+                   q_positions, k_positions, dtype, out, k_out, stream)
+
+
+def rotary_bwd(dQ, dK=None, *, f_q=None, f_kv=None, h=None, w=None, q_frame_offset=0, kv_frame_offset=0, theta=10000.0,
+               split=None, layout="adjacent", ladder="axis", q_positions=None, k_positions=None, dtype=None, out=None,
+               k_out=None, stream=None):
+    """Gradients with respect to rotary_fwd's inputs from those of its results (the turn by the opposite angle), with
+    the arguments of that call.  dtype: of the results, e.g. bf16 for the fp32 gradients of monarch_attn_bwd."""
+    return _rotary("mrt_rotary_bwd", dQ, dK, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder,
+                   q_positions, k_positions, dtype, out, k_out, stream)

@@ -8,7 +8,9 @@
 #include <mutex>
 #include <vector>
 
+#include "mrt_dense_train.hpp"
 #include "mrt_internal.hpp"
+#include "mrt_rotary.hpp"
 
 namespace mrt {
 
@@ -860,11 +862,226 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
   kp.Q = Q; kp.K = K; kp.V = V; kp.O = O;
   const int BH = p->batch * p->heads;
   hipError_t e = timed_launch((hipStream_t)hip_stream, MRT_KERNEL_DENSE, [&] {
-    return f32 ? launch_f32_dense(kp, p->dtype, BH, (hipStream_t)hip_stream)
-               : launch_bf16_dense(kp, BH, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    return f32 ? launch_f32_dense(kp, p->dtype, BH, nullptr, (hipStream_t)hip_stream)
+               : launch_bf16_dense(kp, BH, workspace, workspace_bytes, nullptr, (hipStream_t)hip_stream);
   });
   if (e != hipSuccess) return hip_fail(e, "dense launch");
   return MRT_OK;
+}
+
+// ---- a training step of the dense attention ----------------------------------------------
+static mrt_status dense_train_check(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk, bool backward) {
+  mrt_status st = dense_attn_check(p, causal_chunk);
+  if (st != MRT_OK) return st;
+  const bool f32 = p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32;
+  const int kv_heads = t && t->kv_heads ? t->kv_heads : p->heads;
+  if (kv_heads < 1 || p->heads % kv_heads) {
+    set_error("kv_heads = %d must divide heads = %d", kv_heads, p->heads);
+    return MRT_ERR_SHAPE;
+  }
+  if (!(p->scale >= 1e-30f)) { set_error("scale below 1e-30"); return MRT_ERR_UNSUPPORTED; }
+  if (!backward) return MRT_OK;
+  if (!t) { set_error("the backward call needs the strides of its gradients"); return MRT_ERR_NULL; }
+  const mrt_strides* more[4] = {&t->dout, &t->dq, &t->dk, &t->dv};
+  const mrt_strides* all[8] = {&p->q, &p->k, &p->v, &p->o, &t->dout, &t->dq, &t->dk, &t->dv};
+  for (int i = 0; i < 4; ++i) {
+    if (more[i]->token < p->head_dim || more[i]->head < 1 || more[i]->batch < 1) {
+      set_error("gradient stride set %d: token stride must be >= head_dim, head/batch strides >= 1", i);
+      return MRT_ERR_SHAPE;
+    }
+    if (!f32 && (more[i]->token % 8 || more[i]->head % 8 || more[i]->batch % 8)) {
+      set_error("gradient stride set %d: bf16 path needs strides that are multiples of 8 elements", i);
+      return MRT_ERR_SHAPE;
+    }
+  }
+  // a step of 32 rows is addressed with 32-bit byte offsets
+  for (const mrt_strides* x : all)
+    if (!f32 && x->token > (1ll << 25)) {
+      set_error("token strides of the bf16 backward pass are at most 2^25 elements");
+      return MRT_ERR_UNSUPPORTED;
+    }
+  return MRT_OK;
+}
+
+mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void* O, float* lse, const mrt_problem* p,
+                               const mrt_dense_train* t, int causal_chunk, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
+  mrt_status st = dense_train_check(p, t, causal_chunk, false);
+  if (st != MRT_OK) return st;
+  if (!Q || !K || !V || !O || !lse) { set_error("Q, K, V, O and lse must be non-NULL"); return MRT_ERR_NULL; }
+  const bool f32 = p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32;
+  if (!f32) {
+    const void* ptrs[4] = {Q, K, V, O};
+    for (const void* q : ptrs)
+      if ((uintptr_t)q % 16) { set_error("bf16 path needs 16-byte aligned tensors"); return MRT_ERR_SHAPE; }
+  }
+  if ((uintptr_t)workspace % 256) { set_error("workspace must be 256-byte aligned"); return MRT_ERR_WORKSPACE; }
+  KParams kp = dense_params(p, causal_chunk);
+  kp.Q = Q; kp.K = K; kp.V = V; kp.O = O;
+  const int BH = p->batch * p->heads;
+  const int kv_heads = t && t->kv_heads ? t->kv_heads : p->heads;
+  const DenseSave save = {lse, t ? t->kv_len : nullptr, p->heads / kv_heads};
+  hipError_t e = timed_launch((hipStream_t)hip_stream, MRT_KERNEL_DENSE, [&] {
+    return f32 ? launch_f32_dense(kp, p->dtype, BH, &save, (hipStream_t)hip_stream)
+               : launch_bf16_dense(kp, BH, workspace, workspace_bytes, &save, (hipStream_t)hip_stream);
+  });
+  if (e != hipSuccess) return hip_fail(e, "dense launch");
+  return MRT_OK;
+}
+
+// Everything of a backward call but its tensors and workspace.
+static DenseBwd dense_bwd_params(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk) {
+  DenseBwd d;
+  memset(&d, 0, sizeof(d));
+  d.q = p->q; d.k = p->k; d.v = p->v; d.o = p->o;
+  d.dout = t->dout; d.dq = t->dq; d.dk = t->dk; d.dv = t->dv;
+  d.kv_len = t->kv_len;
+  d.B = p->batch; d.H = p->heads; d.KH = t->kv_heads ? t->kv_heads : p->heads; d.group = d.H / d.KH;
+  d.d = p->head_dim;
+  d.Nq = p->f_q * p->h * p->w; d.Nkv = p->f_kv * p->h * p->w; d.hw = p->h * p->w;
+  d.cc = causal_chunk; d.qoff = p->q_frame_offset; d.scale = p->scale;
+  return d;
+}
+struct DenseBwdWorkspace {
+  DenseBwdShape shape;
+  size_t stats, parts, bytes;     // offset of the parts, which the two launches use in turn
+};
+static DenseBwdWorkspace dense_bwd_workspace(const DenseBwd& d, bool f32) {
+  DenseBwdWorkspace w;
+  w.shape = f32 ? f32_dense_bwd_shape(d) : bf16_dense_bwd_shape(d);
+  w.stats = round256((size_t)d.B * d.H * ((d.Nq + 31) / 32) * 64 * sizeof(float));
+  const size_t q = w.shape.parts_q > 1 ? (size_t)w.shape.parts_q * d.B * d.H * d.Nq * d.d * sizeof(float) : 0;
+  const size_t kv = w.shape.parts_kv > 1 ? 2 * (size_t)w.shape.parts_kv * d.B * d.KH * d.Nkv * d.d * sizeof(float) : 0;
+  w.parts = w.stats;
+  w.bytes = w.stats + round256(q > kv ? q : kv);
+  return w;
+}
+
+mrt_status dense_attn_bwd_check(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk) {
+  return dense_train_check(p, t, causal_chunk, true);
+}
+
+size_t dense_attn_bwd_workspace_bytes(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk) {
+  if (dense_train_check(p, t, causal_chunk, true) != MRT_OK) return 0;
+  const bool f32 = p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32;
+  return dense_bwd_workspace(dense_bwd_params(p, t, causal_chunk), f32).bytes;
+}
+
+mrt_status dense_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* lse,
+                          void* dQ, void* dK, void* dV, const mrt_problem* p, const mrt_dense_train* t, int causal_chunk,
+                          void* workspace, size_t workspace_bytes, void* hip_stream) {
+  mrt_status st = dense_train_check(p, t, causal_chunk, true);
+  if (st != MRT_OK) return st;
+  if (!Q || !K || !V || !O || !dO || !lse || !dQ || !dK || !dV) {
+    set_error("Q, K, V, O, dO, lse, dQ, dK and dV must be non-NULL");
+    return MRT_ERR_NULL;
+  }
+  const bool f32 = p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32;
+  if (!f32) {
+    const void* ptrs[8] = {Q, K, V, O, dO, dQ, dK, dV};
+    for (const void* q : ptrs)
+      if ((uintptr_t)q % 16) { set_error("bf16 path needs 16-byte aligned tensors"); return MRT_ERR_SHAPE; }
+  }
+  DenseBwd d = dense_bwd_params(p, t, causal_chunk);
+  const DenseBwdWorkspace w = dense_bwd_workspace(d, f32);
+  if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < w.bytes) {
+    set_error("workspace: %zu bytes, 256-byte aligned, are needed", w.bytes);
+    return MRT_ERR_WORKSPACE;
+  }
+  d.Q = Q; d.K = K; d.V = V; d.O = O; d.dO = dO; d.lse = lse;
+  d.dQ = dQ; d.dK = dK; d.dV = dV;
+  d.stats = (float*)workspace;
+  d.pq = d.pk = (float*)((char*)workspace + w.parts);
+  d.pv = d.pk + (size_t)w.shape.parts_kv * d.B * d.KH * d.Nkv * d.d;
+  d.parts_q = w.shape.parts_q; d.parts_kv = w.shape.parts_kv;
+  const hipStream_t s = (hipStream_t)hip_stream;
+  hipError_t e = timed_launch(s, MRT_KERNEL_DENSE_BWD, [&] {
+    return f32 ? launch_f32_dense_bwd(d, w.shape, p->dtype, s) : launch_bf16_dense_bwd(d, w.shape, s);
+  });
+  if (e != hipSuccess) return hip_fail(e, "dense backward launch");
+  return MRT_OK;
+}
+
+// ---- rotary positions --------------------------------------------------------------------
+mrt_status mrt_rotary_check(const mrt_rotary* r, const mrt_rotary_tensor* x, int n) {
+  if (!r || !x) { set_error("rotary description is NULL"); return MRT_ERR_NULL; }
+  if (n < 1 || n > 2) { set_error("a rotary call takes one or two tensors, got %d", n); return MRT_ERR_SHAPE; }
+  int total = 0;
+  for (int pairs : r->pairs) {
+    if (pairs < 0 || pairs > 128) { set_error("pairs of an axis must be 0..128"); return MRT_ERR_SHAPE; }
+    total += pairs;
+  }
+  if (r->layout != MRT_ROTARY_ADJACENT && r->layout != MRT_ROTARY_HALVES) { set_error("unknown rotary layout"); return MRT_ERR_SHAPE; }
+  if (r->ladder != MRT_ROTARY_PER_AXIS && r->ladder != MRT_ROTARY_SHARED) { set_error("unknown rotary ladder"); return MRT_ERR_SHAPE; }
+  if (!(r->theta >= 1.0) || !(r->theta <= 1e12)) { set_error("theta must be 1..1e12"); return MRT_ERR_SHAPE; }
+  if (r->head_dim < 1 || r->head_dim > 256) { set_error("head_dim must be 1..256"); return MRT_ERR_SHAPE; }
+  if (total < 1 || 2 * total > r->head_dim) {
+    set_error("%d rotary pairs do not fit head_dim = %d", total, r->head_dim);
+    return MRT_ERR_SHAPE;
+  }
+  for (int i = 0; i < n; ++i) {
+    const mrt_rotary_tensor& t = x[i];
+    if (t.batch < 1 || t.heads < 1 || t.f < 1 || t.h < 1 || t.w < 1 || (long long)t.batch * t.heads > (1 << 24)) {
+      set_error("tensor %d: batch, heads, f, h and w must be >= 1, batch x heads at most 2^24", i);
+      return MRT_ERR_SHAPE;
+    }
+    const double tokens = (double)t.f * t.h * t.w;
+    if (tokens > (1 << 24) || tokens * t.batch > 0x1p31 - 1) { set_error("tensor %d: more than 2^24 tokens", i); return MRT_ERR_SHAPE; }
+    if (t.frame_offset < 0 || (long long)t.frame_offset + t.f > 0x7fffffffll) {
+      set_error("tensor %d: frame_offset out of range", i);
+      return MRT_ERR_SHAPE;
+    }
+    if ((t.x_dtype != MRT_F32 && t.x_dtype != MRT_BF16) || (t.y_dtype != MRT_F32 && t.y_dtype != MRT_BF16)) {
+      set_error("tensor %d: unknown dtype", i);
+      return MRT_ERR_SHAPE;
+    }
+    for (const mrt_strides* st : {&t.x, &t.y})
+      if (st->token < r->head_dim || st->head < 1 || st->batch < 1) {
+        set_error("tensor %d: token stride must be >= head_dim, head/batch strides >= 1", i);
+        return MRT_ERR_SHAPE;
+      }
+    if (t.positions && (t.position_batch < 0 || t.position_axis < 0)) {
+      set_error("tensor %d: strides of the positions must be >= 0", i);
+      return MRT_ERR_SHAPE;
+    }
+  }
+  return MRT_OK;
+}
+
+static mrt_status rotary_run(const mrt_rotary* r, const mrt_rotary_tensor* x, int n, const void* const* X, void* const* Y,
+                             bool inverse, void* hip_stream) {
+  mrt_status st = mrt_rotary_check(r, x, n);
+  if (st != MRT_OK) return st;
+  if (!X || !Y) { set_error("X and Y must be non-NULL"); return MRT_ERR_NULL; }
+  for (int i = 0; i < n; ++i) {
+    if (!X[i] || !Y[i]) { set_error("tensor %d is NULL", i); return MRT_ERR_NULL; }
+    const size_t size = x[i].x_dtype == MRT_F32 ? 4 : 2;
+    if (X[i] == Y[i] && (x[i].x_dtype != x[i].y_dtype || memcmp(&x[i].x, &x[i].y, sizeof(mrt_strides)))) {
+      set_error("tensor %d in place: both sides need one type and the same strides", i);
+      return MRT_ERR_SHAPE;
+    }
+    if ((uintptr_t)X[i] % size || (uintptr_t)Y[i] % (x[i].y_dtype == MRT_F32 ? 4 : 2)) {
+      set_error("tensor %d is not aligned to its elements", i);
+      return MRT_ERR_SHAPE;
+    }
+  }
+  // (in place a repeated launch would turn once more)
+  const bool in_place = X[0] == Y[0] || (n > 1 && X[1] == Y[1]);
+  const hipError_t e = timed_launch(
+      (hipStream_t)hip_stream, MRT_KERNEL_ROTARY,
+      [&] { return launch_rotary(*r, x, n, X, Y, inverse, (hipStream_t)hip_stream); }, !in_place);
+  if (e != hipSuccess) return hip_fail(e, "rotary launch");
+  return MRT_OK;
+}
+
+mrt_status mrt_rotary_fwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n, const void* const* X, void* const* Y,
+                      void* hip_stream) {
+  return rotary_run(r, x, n, X, Y, false, hip_stream);
+}
+
+mrt_status mrt_rotary_bwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n, const void* const* dY, void* const* dX,
+                      void* hip_stream) {
+  return rotary_run(r, x, n, dY, dX, true, hip_stream);
 }
 
 #ifdef MRT_TRACE

@@ -84,9 +84,14 @@ struct DenseParts {
   int n;
 };
 
+// A row's log-sum-exp from its reference and sum, which are base 2.
+__device__ inline float natural_lse(float m, float sum) { return sum > 0.f ? kLn2 * m + logf(sum) : -INFINITY; }
+
 // (64 features: two workgroups to a compute unit)
-template <int D, int QT, int WK, bool PART>
-__global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(KParams p, DenseParts parts) {
+// Save = DenseSave: a training step's call (heads that share keys, sequences of their own lengths, row statistics)
+template <int D, int QT, int WK, bool PART, typename Save>
+__global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(KParams p, DenseParts parts, Save save) {
+  constexpr bool SAVE = std::is_same<Save, DenseSave>::value;
   using Tile = DenseTile<D>;
   constexpr int KS1 = D / 32, NVT = D / 16, LD = kDenseLd<D>, WQ = kDenseWaves / WK, WGQ = 16 * QT * WQ;
   constexpr int NS = 2 / WK, NT = 2 * NS;                 // 32-key chunks / 16-key tiles of a wave's step
@@ -94,17 +99,41 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int wq = wave % WQ, wk = wave / WQ;
   const bool second = wave >= kDenseWaves / 2;           // the half that runs one phase behind
-  auto visible = [&](int q) { return dense_visible(p, q); };
+  int most_keys = p.Nkv;
+  auto visible = [&](int q) {
+    const int n = dense_visible(p, q);
+    return SAVE && n > most_keys ? most_keys : n;
+  };
   // Workgroups reach the eight XCDs in turn: hand each XCD a contiguous run of (head, query tile)
   // units, so that the units that stream the same keys share its L2.  (Under a mask that gives the
   // query tiles of a head different key counts the natural order spreads the long ones evenly.)
   const int nx = (p.Nq + WGQ - 1) / WGQ, total = gridDim.x, xcd = blockIdx.x & 7;
   int unit = blockIdx.x;
-  if (visible(0) == visible(p.Nq - 1)) unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
+  if (dense_visible(p, 0) == dense_visible(p, p.Nq - 1)) unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
   const int run = unit / nx, q0 = (unit - run * nx) * WGQ;         // run = (head, part)
   const int bh = PART ? run / parts.n : run, part = PART ? run - bh * parts.n : 0;
   const int b = bh / p.H, hd = bh - b * p.H;
+  int kvh = hd;
   const int qw0 = q0 + 16 * QT * wq;                      // this wave's first query
+  if constexpr (SAVE) {
+    kvh = hd / save.group;
+    if (save.kv_len) most_keys = min(max(save.kv_len[b], 0), p.Nkv);
+    if (most_keys == 0) {                                 // an empty sequence
+      const long long row0 = PART ? ((long long)part * (total / (nx * parts.n)) + bh) * p.Nq : 0;
+      for (int i = tid; i < WGQ * D; i += kDenseThreads) {
+        const int q = q0 + i / D, f = i % D;
+        if (q >= p.Nq) break;
+        if constexpr (PART) {
+          parts.o[(row0 + q) * D + f] = 0.f;
+          if (f == 0) parts.ml[row0 + q] = make_float2(kNoKey, 0.f);
+        } else {
+          ((u16*)p.O)[b * p.os.batch + hd * p.os.head + (long long)q * p.os.token + f] = 0;
+          if (f == 0) save.lse[(long long)bh * p.Nq + q] = -INFINITY;
+        }
+      }
+      return;
+    }
+  }
   const int nkeys = visible(q0 + WGQ - 1 < p.Nq ? q0 + WGQ - 1 : p.Nq - 1), nfree = visible(q0);
 
   const u16* Qp = (const u16*)p.Q + b * p.qs.batch + hd * p.qs.head;
@@ -123,8 +152,8 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
   const int nmid = (mid + 63) >> 6, npairs = nmid + ((nkeys - mid + 63) >> 6);
   auto first_key = [&](int pr) { return pr < nmid ? 64 * pr : mid + 64 * (pr - nmid); };
   const int p0 = PART ? part * npairs / parts.n : 0, p1 = PART ? (part + 1) * npairs / parts.n : npairs;   // this part's pairs
-  const u16* Kp = (const u16*)p.K + b * p.ks.batch + hd * p.ks.head;
-  const u16* Vp = (const u16*)p.V + b * p.vs.batch + hd * p.vs.head;
+  const u16* Kp = (const u16*)p.K + b * p.ks.batch + kvh * p.ks.head;
+  const u16* Vp = (const u16*)p.V + b * p.vs.batch + kvh * p.vs.head;
   const unsigned kvoff = (unsigned)(tid / Tile::CPR) * krow + 16u * (tid % Tile::CPR);
   const unsigned vvoff = (unsigned)(tid / Tile::CPR) * vrow + 16u * (tid % Tile::CPR);
   Tile kt, vt;
@@ -338,14 +367,16 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
         typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
         *(bf16x4*)(row + 16 * vt) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
       }
+      if constexpr (SAVE)
+        if (g == 0) save.lse[(long long)bh * p.Nq + qi] = natural_lse(mref[q], lsum);
     }
   }
 }
 
 // O from the parts: every part's sum and accumulators against the largest reference.  A thread owns
 // four features of a query and has eight parts in flight at once: what it waits for is memory.
-template <int D>
-__global__ __launch_bounds__(256) void k_dense_merge(KParams p, DenseParts parts, int rows) {
+template <int D, typename Save>
+__global__ __launch_bounds__(256) void k_dense_merge(KParams p, DenseParts parts, int rows, Save save) {
   constexpr int TPR = D / 4, AHEAD = 8;
   const int row = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, f = 4 * (threadIdx.x % TPR);
   if (row >= rows) return;
@@ -381,18 +412,20 @@ __global__ __launch_bounds__(256) void k_dense_merge(KParams p, DenseParts parts
   typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
   *(bf16x4*)((u16*)p.O + b * p.os.batch + hd * p.os.head + (long long)q * p.os.token + f) =
       bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+  if constexpr (std::is_same<Save, DenseSave>::value)
+    if (f == 0) save.lse[row] = natural_lse(m, lsum);
 }
 
-template <int D, int QT, int WK, bool PART>
-hipError_t run_dense(const KParams& kp, int nbh, const DenseParts& parts, hipStream_t s) {
-  const hipError_t e = hipFuncSetAttribute((const void*)k_bf16_dense<D, QT, WK, PART>,
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)kDenseLds<D>);
+template <int D, int QT, int WK, bool PART, typename Save>
+hipError_t run_dense(const KParams& kp, int nbh, const DenseParts& parts, const Save& save, hipStream_t s) {
+  const auto kernel = k_bf16_dense<D, QT, WK, PART, Save>;
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kDenseLds<D>);
   if (e != hipSuccess) return e;
   constexpr int wgq = 16 * QT * kDenseWaves / WK;
-  k_bf16_dense<D, QT, WK, PART><<<(kp.Nq + wgq - 1) / wgq * nbh * parts.n, kDenseThreads, kDenseLds<D>, s>>>(kp, parts);
+  kernel<<<(kp.Nq + wgq - 1) / wgq * nbh * parts.n, kDenseThreads, kDenseLds<D>, s>>>(kp, parts, save);
   if constexpr (PART) {
     const int rows = nbh * kp.Nq, rpw = 256 / (D / 4);
-    k_dense_merge<D><<<(rows + rpw - 1) / rpw, 256, 0, s>>>(kp, parts, rows);
+    k_dense_merge<D><<<(rows + rpw - 1) / rpw, 256, 0, s>>>(kp, parts, rows, save);
   }
   return hipGetLastError();
 }
@@ -495,12 +528,20 @@ DenseShape dense_shape(const KParams& kp, int nbh, bool may_split) {
   return best;
 }
 
-template <int D, bool PART>
-hipError_t run_dense_d(const KParams& kp, int nbh, int queries, const DenseParts& parts, hipStream_t s) {
-  if (queries == 64) return run_dense<D, 1, 2, PART>(kp, nbh, parts, s);
+template <int D, bool PART, typename Save>
+hipError_t run_dense_d(const KParams& kp, int nbh, int queries, const DenseParts& parts, const Save& save, hipStream_t s) {
+  if (queries == 64) return run_dense<D, 1, 2, PART>(kp, nbh, parts, save, s);
   if constexpr (D == 128)
-    if (queries == 256) return run_dense<D, 2, 1, PART>(kp, nbh, parts, s);
-  return run_dense<D, 2, 2, PART>(kp, nbh, parts, s);
+    if (queries == 256) return run_dense<D, 2, 1, PART>(kp, nbh, parts, save, s);
+  return run_dense<D, 2, 2, PART>(kp, nbh, parts, save, s);
+}
+template <typename Save>
+hipError_t run_dense_shape(const KParams& kp, int nbh, const DenseShape& shape, const DenseParts& parts, const Save& save, hipStream_t s) {
+  if (kp.d == 128)
+    return shape.parts > 1 ? run_dense_d<128, true>(kp, nbh, shape.queries, parts, save, s)
+                           : run_dense_d<128, false>(kp, nbh, shape.queries, parts, save, s);
+  return shape.parts > 1 ? run_dense_d<64, true>(kp, nbh, shape.queries, parts, save, s)
+                         : run_dense_d<64, false>(kp, nbh, shape.queries, parts, save, s);
 }
 
 }  // namespace
@@ -510,14 +551,12 @@ size_t bf16_dense_workspace_bytes(const KParams& kp, int nbh) {
   return shape.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d) : 0;
 }
 
-hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, hipStream_t s) {
+hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseSave* save, hipStream_t s) {
   DenseShape shape = dense_shape(kp, nbh, workspace != nullptr);
   if (shape.parts > 1 && workspace_bytes < dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d)) shape = dense_shape(kp, nbh, false);
   const size_t rows = (size_t)kp.Nq * nbh * shape.parts;
   const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), shape.parts};
-  if (kp.d == 128)
-    return shape.parts > 1 ? run_dense_d<128, true>(kp, nbh, shape.queries, parts, s) : run_dense_d<128, false>(kp, nbh, shape.queries, parts, s);
-  return shape.parts > 1 ? run_dense_d<64, true>(kp, nbh, shape.queries, parts, s) : run_dense_d<64, false>(kp, nbh, shape.queries, parts, s);
+  return save ? run_dense_shape(kp, nbh, shape, parts, *save, s) : run_dense_shape(kp, nbh, shape, parts, NoSave{}, s);
 }
 
 }  // namespace mrt

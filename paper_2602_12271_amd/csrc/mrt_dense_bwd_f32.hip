@@ -1,0 +1,279 @@
+// Backward pass of the dense softmax attention in fp32 arithmetic, and the sums of its parts.
+//
+// Products of fp32 operands (v_mfma_f32_16x16x4_f32).  A wave owns 16 rows of one (batch, head), keys (KV) or
+// queries, on the N side: their operands and gradients stay in its registers, and the rows of the other side
+// stream through LDS, 16 a step.  With feature 16 ks + 4 g + e as slot g of step (ks, e) a lane's operands of
+// four steps are 16 contiguous bytes; register r of a logit tile (streamed rows 4 g + r) is as it stands the
+// second products' operand of step r.  Those take 16 bytes of a row for four result tiles: lane c reads the
+// features 64 blk + 4 c + e of tile e, so register r of the four tiles is feature 64 blk + 16 g + 4 r + e.
+#include "mrt_dense_train.hpp"
+#include "mrt_f32_rows.hpp"
+
+#include <algorithm>
+
+namespace mrt {
+
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16 * kWaves, kStep = 16;
+template <int D> constexpr int kLd = D + 4;                          // LDS row stride in floats
+template <int D> constexpr int kSlot = 2 * kStep * kLd<D> + 2 * kStep;
+
+__device__ inline f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+template <int D, typename T, bool VEC, bool KV, bool PART>
+__global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p) {
+  constexpr int KS = D / 16, BLK = D / 64, LD = kLd<D>, QUADS = kStep * D / 4 / kThreads;
+  __shared__ __attribute__((aligned(16))) float lds[2 * kSlot<D>];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int n_own = KV ? p.Nkv : p.Nq, n_heads = p.B * (KV ? p.KH : p.H), d = p.d;
+  const int tiles = (n_own + kRows - 1) / kRows, parts = PART ? (KV ? p.parts_kv : p.parts_q) : 1;
+  int unit = blockIdx.x;
+  const int bh = unit % n_heads;
+  unit /= n_heads;
+  const int part = unit % parts, tile = KV ? unit / parts : tiles - 1 - unit / parts;    // under a mask the longest first
+  const int b = bh / (KV ? p.KH : p.H), hd = bh - b * (KV ? p.KH : p.H), kvh = KV ? hd : hd / p.group;
+  const int own0 = tile * kRows, keys = dense_keys(p, b), own_last = own0 + kRows < n_own ? own0 + kRows - 1 : n_own - 1;
+
+  // the streamed rows: queries qfirst .. Nq of every head that shares these keys, or keys 0 .. last
+  const int qfirst = KV ? dense_first_query(p, own0) & ~(kStep - 1) : 0;
+  const int s_end = KV ? p.Nq : dense_last_key(p, own_last, keys);
+  const int per_head = !KV || own0 < keys ? (s_end - qfirst + kStep - 1) / kStep : 0;
+  const int all = KV ? per_head * p.group : per_head;
+  const int i0 = PART ? (int)((long long)all * part / parts) : 0, i1 = PART ? (int)((long long)all * (part + 1) / parts) : all;
+  const int nqb = (p.Nq + 31) >> 5;
+
+  const T* own_a = KV ? (const T*)p.K + b * p.k.batch + hd * p.k.head : (const T*)p.Q + b * p.q.batch + hd * p.q.head;
+  const T* own_b = KV ? (const T*)p.V + b * p.v.batch + hd * p.v.head : (const T*)p.dO + b * p.dout.batch + hd * p.dout.head;
+  const long long own_at = KV ? p.k.token : p.q.token, own_bt = KV ? p.v.token : p.dout.token;
+  const T* st_a = KV ? (const T*)p.Q + b * p.q.batch + (long long)hd * p.group * p.q.head
+                     : (const T*)p.K + b * p.k.batch + kvh * p.k.head;
+  const T* st_b = KV ? (const T*)p.dO + b * p.dout.batch + (long long)hd * p.group * p.dout.head
+                     : (const T*)p.V + b * p.v.batch + kvh * p.v.head;
+  const long long st_at = KV ? p.q.token : p.k.token, st_bt = KV ? p.dout.token : p.v.token;
+
+  f32x4 ra[QUADS], rb[QUADS];
+  float rst = 0.f;
+  auto fetch = [&](int i) {
+    const int gh = KV ? i / per_head : 0, row = KV ? qfirst + kStep * (i - gh * per_head) : kStep * i;
+    const T* a = st_a + (KV ? gh * p.q.head : 0);
+    const T* bb = st_b + (KV ? gh * p.dout.head : 0);
+#pragma unroll
+    for (int j = 0; j < QUADS; ++j) {
+      const int at = tid + j * kThreads, r = row + at / (D / 4), v = 4 * (at % (D / 4));
+      const bool in = r < s_end;
+      const long long rr = in ? r : s_end - 1;
+      ra[j] = blank4<VEC>(ld4<VEC>(a + rr * st_at, v, d), v, d);
+      rb[j] = blank4<VEC>(ld4<VEC>(bb + rr * st_bt, v, d), v, d);
+      if (!in) ra[j] = rb[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if constexpr (KV)
+      if (tid < 2 * kStep) {
+        const int r = row + (tid & (kStep - 1));
+        rst = p.stats[((long long)(b * p.H + hd * p.group + gh) * nqb + (r >> 5)) * 64 + 32 * (tid / kStep) + (r & 31)];
+      }
+  };
+  auto commit = [&](int slot) {
+    float* at = lds + slot * kSlot<D>;
+#pragma unroll
+    for (int j = 0; j < QUADS; ++j) {
+      const int q = tid + j * kThreads, r = q / (D / 4), v = 4 * (q % (D / 4));
+      *(f32x4*)(at + r * LD + v) = ra[j];
+      *(f32x4*)(at + (kStep + r) * LD + v) = rb[j];
+    }
+    if (KV && tid < 2 * kStep) at[2 * kStep * LD + tid] = rst;
+  };
+  if (i0 < i1) {
+    fetch(i0);
+    commit(0);
+  }
+
+  const int r_own = own0 + 16 * wave + c, rc = r_own < n_own ? r_own : n_own - 1;
+  f32x4 oa[KS], ob[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const int v = 16 * ks + 4 * g;
+    oa[ks] = blank4<VEC>(ld4<VEC>(own_a + rc * own_at, v, d), v, d);
+    ob[ks] = blank4<VEC>(ld4<VEC>(own_b + rc * own_bt, v, d), v, d);
+  }
+  const int lim = KV ? dense_first_query(p, rc) : dense_last_key(p, rc, keys);
+  float nlse = 0.f, ndelta = 0.f;
+  if constexpr (!KV) {
+    const T* orow = (const T*)p.O + b * p.o.batch + hd * p.o.head + rc * p.o.token;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int v = 16 * ks + 4 * g;
+      const f32x4 o = blank4<VEC>(ld4<VEC>(orow, v, d), v, d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(o[e], ob[ks][e], sum[e]);
+    }
+    ndelta = -xsum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    const float l = p.lse[(long long)bh * p.Nq + rc];
+    nlse = l == -INFINITY ? -INFINITY : -kLog2e * l;
+    if (part == 0 && g == 0 && r_own < nqb * 32) {
+      float* st = p.stats + ((long long)bh * nqb + (r_own >> 5)) * 64 + (r_own & 31);
+      st[0] = r_own >= p.Nq ? -INFINITY : nlse;
+      st[32] = r_own >= p.Nq ? 0.f : ndelta;
+    }
+  }
+  f32x4 g1[BLK][4], g2[BLK][4];
+#pragma unroll
+  for (int blk = 0; blk < BLK; ++blk)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g1[blk][e] = g2[blk][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float scale2 = p.scale * kLog2e;
+
+  for (int i = i0; i < i1; ++i) {
+    __syncthreads();
+    const float* at = lds + ((i - i0) & 1) * kSlot<D>;
+    const float* bt = at + kStep * LD;
+    if (i + 1 < i1) fetch(i + 1);
+    const int row = KV ? qfirst + kStep * (i % per_head) : kStep * i;
+    f32x4 s[4], dp[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] = dp[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const f32x4 a = *(const f32x4*)(at + c * LD + 16 * ks + 4 * g), x = *(const f32x4*)(bt + c * LD + 16 * ks + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] = mfma4(a[e], oa[ks][e], s[e]);
+        dp[e] = mfma4(x[e], ob[ks][e], dp[e]);
+      }
+    }
+    f32x4 w = (s[0] + s[1]) + (s[2] + s[3]), ds = (dp[0] + dp[1]) + (dp[2] + dp[3]);
+    f32x4 nl = {nlse, nlse, nlse, nlse}, nd = {ndelta, ndelta, ndelta, ndelta};
+    if constexpr (KV) {
+      nl = *(const f32x4*)(bt + kStep * LD + 4 * g);
+      nd = *(const f32x4*)(bt + kStep * LD + kStep + 4 * g);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int at_row = row + 4 * g + r;
+      const bool seen = KV ? at_row >= lim : at_row < lim;
+      const float pr = exp2_fast(fmaf(w[r], scale2, nl[r]));
+      w[r] = seen ? pr : 0.f;
+      ds[r] = seen ? pr * (ds[r] + nd[r]) : 0.f;
+    }
+    const float* a2 = at + 4 * g * LD + 4 * c;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int blk = 0; blk < BLK; ++blk) {
+        const f32x4 y = *(const f32x4*)(a2 + r * LD + 64 * blk);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g2[blk][e] = mfma4(y[e], ds[r], g2[blk][e]);
+        if constexpr (KV) {
+          const f32x4 x = *(const f32x4*)(a2 + (kStep + r) * LD + 64 * blk);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) g1[blk][e] = mfma4(x[e], w[r], g1[blk][e]);
+        }
+      }
+    if (i + 1 < i1) commit((i + 1 - i0) & 1);
+  }
+  if (r_own >= n_own) return;
+  const bool live = KV ? r_own < keys : true;
+#pragma unroll
+  for (int blk = 0; blk < BLK; ++blk)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int v = 64 * blk + 16 * g + 4 * r;
+      f32x4 x, y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = live ? p.scale * g2[blk][e][r] : 0.f;
+        y[e] = live ? g1[blk][e][r] : 0.f;
+      }
+      if constexpr (PART) {
+        const long long to = (((long long)part * n_heads + bh) * n_own + r_own) * d;
+        st4<false>((KV ? p.pk : p.pq) + to, x, v, d);
+        if (KV) st4<false>(p.pv + to, y, v, d);
+      } else if constexpr (KV) {
+        st4<VEC>((T*)p.dK + b * p.dk.batch + hd * p.dk.head + r_own * p.dk.token, x, v, d);
+        st4<VEC>((T*)p.dV + b * p.dv.batch + hd * p.dv.head + r_own * p.dv.token, y, v, d);
+      } else {
+        st4<VEC>((T*)p.dQ + b * p.dq.batch + hd * p.dq.head + r_own * p.dq.token, x, v, d);
+      }
+    }
+}
+
+// A gradient from its parts, added in their order.  A thread owns four features of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_dense_bwd_join(const float* parts, int n, void* to, mrt_strides st, int rows,
+                                                        int tokens, int heads, int d) {
+  const int quads = (d + 3) >> 2;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int row = (int)(at / quads), v = 4 * (int)(at - (long long)row * quads);
+  if (row >= rows) return;
+  const int left = d - v < 4 ? d - v : 4;
+  const float* from = parts + (long long)row * d + v;
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < n; ++i, from += (long long)rows * d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) x[e] += from[e];
+  const int bh = row / tokens, tok = row - bh * tokens, b = bh / heads, hd = bh - b * heads;
+  T* out = (T*)to + b * st.batch + hd * st.head + tok * st.token + v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < left) {
+      if constexpr (sizeof(T) == 2) out[e] = f2bf(x[e]);
+      else out[e] = x[e];
+    }
+}
+
+template <int D, typename T, bool VEC, bool KV>
+hipError_t run(const DenseBwd& p, hipStream_t s) {
+  const int n = KV ? p.Nkv : p.Nq, heads = p.B * (KV ? p.KH : p.H), parts = KV ? p.parts_kv : p.parts_q;
+  const dim3 grid((n + kRows - 1) / kRows * heads * parts);
+  if (parts > 1) k_f32_dense_bwd<D, T, VEC, KV, true><<<grid, kThreads, 0, s>>>(p);
+  else k_f32_dense_bwd<D, T, VEC, KV, false><<<grid, kThreads, 0, s>>>(p);
+  return hipGetLastError();
+}
+template <int D, typename T, bool VEC>
+hipError_t run_both(const DenseBwd& p, int dtype, hipStream_t s) {
+  hipError_t e = run<D, T, VEC, false>(p, s);
+  if (e == hipSuccess && p.parts_q > 1) e = launch_dense_bwd_join(p, false, dtype, s);
+  if (e == hipSuccess) e = run<D, T, VEC, true>(p, s);
+  if (e == hipSuccess && p.parts_kv > 1) e = launch_dense_bwd_join(p, true, dtype, s);
+  return e;
+}
+template <typename T>
+bool rows_of_four(const DenseBwd& p) {
+  const void* ptrs[8] = {p.Q, p.K, p.V, p.O, p.dO, p.dQ, p.dK, p.dV};
+  const mrt_strides* st[8] = {&p.q, &p.k, &p.v, &p.o, &p.dout, &p.dq, &p.dk, &p.dv};
+  if (p.d % 4) return false;
+  for (int i = 0; i < 8; ++i)
+    if ((uintptr_t)ptrs[i] % (4 * sizeof(T)) || st[i]->token % 4 || st[i]->head % 4 || st[i]->batch % 4) return false;
+  return true;
+}
+template <typename T>
+hipError_t run_t(const DenseBwd& p, int dtype, hipStream_t s) {
+  if (rows_of_four<T>(p)) return p.d <= 64 ? run_both<64, T, true>(p, dtype, s) : run_both<128, T, true>(p, dtype, s);
+  return p.d <= 64 ? run_both<64, T, false>(p, dtype, s) : run_both<128, T, false>(p, dtype, s);
+}
+
+}  // namespace
+
+hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStream_t s) {
+  const int tokens = kv ? p.Nkv : p.Nq, heads = kv ? p.KH : p.H, rows = p.B * heads * tokens;
+  const long long threads = (long long)rows * ((p.d + 3) / 4);
+  for (int i = 0; i < (kv ? 2 : 1); ++i) {
+    const float* from = kv ? (i ? p.pv : p.pk) : p.pq;
+    void* to = kv ? (i ? p.dV : p.dK) : p.dQ;
+    const mrt_strides& st = kv ? (i ? p.dv : p.dk) : p.dq;
+    const dim3 grid((unsigned)((threads + 255) / 256));
+    if (dtype == MRT_BF16) k_dense_bwd_join<u16><<<grid, 256, 0, s>>>(from, kv ? p.parts_kv : p.parts_q, to, st, rows, tokens, heads, p.d);
+    else k_dense_bwd_join<float><<<grid, 256, 0, s>>>(from, kv ? p.parts_kv : p.parts_q, to, st, rows, tokens, heads, p.d);
+  }
+  return hipGetLastError();
+}
+
+DenseBwdShape f32_dense_bwd_shape(const DenseBwd&) { return {kRows, 1, kRows, 1}; }
+
+hipError_t launch_f32_dense_bwd(const DenseBwd& p, const DenseBwdShape&, int dtype, hipStream_t s) {
+  return dtype == MRT_F32 ? run_t<float>(p, dtype, s) : run_t<u16>(p, dtype, s);
+}
+
+}  // namespace mrt

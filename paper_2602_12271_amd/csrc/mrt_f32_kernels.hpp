@@ -40,6 +40,7 @@
 // d % 4 == 0; the other variant moves single elements.
 #pragma once
 #include "mrt_internal.hpp"
+#include "mrt_f32_rows.hpp"
 #include "mrt_f32_split.hpp"
 
 namespace mrt {
@@ -61,60 +62,6 @@ struct Sums4 {
   }
   __device__ inline f32x4 total() const { return (s[0] + s[1]) + (s[2] + s[3]); }
 };
-
-// ---- rows of four features -------------------------------------------------------------------
-template <typename T> struct Quad;
-template <> struct Quad<float> {
-  typedef f32x4 raw;
-  static __device__ inline f32x4 widen(raw x) { return x; }
-  static __device__ inline float one(float x) { return x; }
-};
-template <> struct Quad<u16> {
-  typedef __attribute__((ext_vector_type(4))) u16 raw;
-  static __device__ inline float one(u16 x) { return __uint_as_float((uint32_t)x << 16); }
-  static __device__ inline f32x4 widen(raw x) { return f32x4{one(x[0]), one(x[1]), one(x[2]), one(x[3])}; }
-};
-// features v .. v + 3 of the row at p (the load itself is unconditional); from d on they are zeros, where
-// rows are moved by four only once blank4 has seen them
-template <bool VEC, typename T>
-__device__ inline f32x4 ld4(const T* p, int v, int d) {
-  f32x4 x;
-  if constexpr (VEC) {
-    x = Quad<T>::widen(*(const typename Quad<T>::raw*)(p + (v < d ? v : 0)));
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float one = Quad<T>::one(p[v + e < d ? v + e : 0]);
-      x[e] = v + e < d ? one : 0.f;
-    }
-  }
-  return x;
-}
-template <bool VEC>
-__device__ inline f32x4 blank4(f32x4 x, int v, int d) {
-  return VEC && v >= d ? f32x4{0.f, 0.f, 0.f, 0.f} : x;
-}
-template <bool VEC>
-__device__ inline void st4(float* p, f32x4 x, int v, int d) {
-  if constexpr (VEC) {
-    if (v < d) *(f32x4*)(p + v) = x;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (v + e < d) p[v + e] = x[e];
-  }
-}
-template <bool VEC>
-__device__ inline void st4(u16* p, f32x4 x, int v, int d) {
-  if constexpr (VEC) {
-    typedef typename Quad<u16>::raw raw;
-    if (v < d) *(raw*)(p + v) = raw{f2bf(x[0]), f2bf(x[1]), f2bf(x[2]), f2bf(x[3])};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (v + e < d) p[v + e] = f2bf(x[e]);
-  }
-}
 
 template <int D> constexpr int kLd = D + 4;   // LDS row stride in floats
 
@@ -1063,25 +1010,41 @@ constexpr int kDenseWaves32 = 8, kDenseQ32 = 16 * kDenseWaves32;
 
 // MASKED: chunk-causal (a kernel of its own: the shorter chunks' bookkeeping costs 4 % of a
 // call at 64 features)
-template <int D, typename TIn, bool VEC, bool MASKED, bool SPLIT, typename Again>
-__device__ inline bool dense_32(const Place& at, const KParams& p, float* lds, Again again) {
+// Save = DenseSave: a training step's call (heads that share keys, sequences of their own lengths, row statistics)
+template <int D, typename TIn, bool VEC, bool MASKED, bool SPLIT, typename Save, typename Again>
+__device__ inline bool dense_32(const Place& at, const KParams& p, const Save& save, float* lds, Again again) {
+  constexpr bool SAVE = std::is_same<Save, DenseSave>::value;
   const int tid = at.tid, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int q0 = at.x * kDenseQ32, bh = at.y, d = p.d;
   const int b = bh / p.H, hd = bh - b * p.H;
+  int kvh = hd, most_keys = p.Nkv;
+  if constexpr (SAVE) {
+    kvh = hd / save.group;
+    if (save.kv_len) most_keys = min(max(save.kv_len[b], 0), p.Nkv);
+  }
   const TIn* Qp = (const TIn*)p.Q + b * p.qs.batch + hd * p.qs.head;
-  const TIn* Kp = (const TIn*)p.K + b * p.ks.batch + hd * p.ks.head;
-  const TIn* Vp = (const TIn*)p.V + b * p.vs.batch + hd * p.vs.head;
+  const TIn* Kp = (const TIn*)p.K + b * p.ks.batch + kvh * p.ks.head;
+  const TIn* Vp = (const TIn*)p.V + b * p.vs.batch + kvh * p.vs.head;
   const int qi = q0 + 16 * wave + c, qc = qi < p.Nq ? qi : p.Nq - 1;
   Query32<D, SPLIT> q;
   Out32<D, SPLIT> o;
+  if constexpr (SAVE)
+    if (most_keys == 0) {       // an empty sequence
+      o.clear();
+      if (qi < p.Nq) {
+        o.template store<VEC>((TIn*)p.O + b * p.os.batch + hd * p.os.head + (long long)qi * p.os.token, 0.f, g, d);
+        if (g == 0) save.lse[(long long)bh * p.Nq + qi] = -INFINITY;
+      }
+      return false;
+    }
   Watch watch(p.scale);
   q.template load<VEC, kSeeSmall | kSeeHuge>(Qp + (long long)qc * p.qs.token, d, g, watch);
   o.clear();
   // the keys query row r sees: a prefix, up to the end of its own chunk
   auto visible = [&](int r) {
-    if (p.cc == 0) return p.Nkv;
+    if (p.cc == 0) return most_keys;
     const long long most = (long long)((p.qoff + r / p.hw) / p.cc + 1) * p.cc * p.hw;
-    return most < p.Nkv ? (int)most : p.Nkv;
+    return most < most_keys ? (int)most : most_keys;
   };
   auto last_of = [&](int r) { return r < p.Nq ? r : p.Nq - 1; };
   const int nkeys = visible(last_of(q0 + kDenseQ32 - 1)), lim = visible(qc);
@@ -1091,13 +1054,17 @@ __device__ inline bool dense_32(const Place& at, const KParams& p, float* lds, A
   // chunks end where a query of this workgroup stops seeing keys: a wave whose queries stop there leaves the
   // next chunk out, and no value hidden from all of them gets to meet their weights of zero (0 x inf)
   flash32<D, kDenseWaves32, true, VEC, SPLIT>(Kp, p.ks.token, Vp, p.vs.token, nkeys, d, p.scale, q, wkeys, MASKED ? visible(q0) : 0,
-                                       MASKED ? p.cc * p.hw : 0, lds, [](int) { return 0.f; },
+                                       MASKED ? (SAVE && p.cc == 0 ? p.Nkv : p.cc * p.hw) : 0, lds, [](int) { return 0.f; },
                                        [&](int key) { return MASKED && key >= lim; }, st, o, watch, tid);
   o.show(watch);
   const float lsum = xsum(st.l);
   if (again(watch)) return true;
   TIn* Op = (TIn*)p.O + b * p.os.batch + hd * p.os.head;
   if (qi < p.Nq) o.template store<VEC>(Op + (long long)qi * p.os.token, lsum > 0.f ? 1.0f / lsum : 0.f, g, d);
+  if constexpr (SAVE) {
+    // (split weights, and so their sum, carry a factor 2^24)
+    if (qi < p.Nq && g == 0) save.lse[(long long)bh * p.Nq + qi] = st.m + logf(SPLIT ? lsum * (1.f / kWeight) : lsum);
+  }
   return false;
 }
 // A few keys do not pay for splitting the queries: up to these the operands stay fp32 (us with split and with
@@ -1106,11 +1073,11 @@ __device__ inline bool dense_32(const Place& at, const KParams& p, float* lds, A
 // of 40 keys 21.3, 17.3, of 80 keys 30.7, about 27, of 96 keys 30.0, 30.6).
 template <int D, bool MASKED>
 constexpr int kFewKeys32 = D == 64 ? 16 : (MASKED ? 160 : 64);
-template <int D, typename TIn, bool VEC, bool MASKED>
-__global__ __launch_bounds__(64 * kDenseWaves32, 4) void k_f32_dense(KParams p) {
+template <int D, typename TIn, bool VEC, bool MASKED, typename Save>
+__global__ __launch_bounds__(64 * kDenseWaves32, 4) void k_f32_dense(KParams p, Save save) {
   __shared__ __attribute__((aligned(16))) float lds[kRing32<D, true, VEC>];
   run_split<VEC>([&](auto split, const Place& at, auto again) {
-    return dense_32<D, TIn, VEC, MASKED, decltype(split)::value>(at, p, lds, again);
+    return dense_32<D, TIn, VEC, MASKED, decltype(split)::value>(at, p, save, lds, again);
   }, p.Nkv > kFewKeys32<D, MASKED>);
 }
 
@@ -1273,15 +1240,21 @@ hipError_t run_l_t(const KParams& kp, dim3 grid, bool last, hipStream_t s) {
 }
 
 template <int D, typename TIn, bool VEC>
-hipError_t run_dense(const KParams& kp, dim3 grid, hipStream_t s) {
-  if (kp.cc > 0) k_f32_dense<D, TIn, VEC, true><<<grid, 64 * kDenseWaves32, 0, s>>>(kp);
-  else k_f32_dense<D, TIn, VEC, false><<<grid, 64 * kDenseWaves32, 0, s>>>(kp);
+hipError_t run_dense(const KParams& kp, dim3 grid, const DenseSave* save, hipStream_t s) {
+  constexpr int threads = 64 * kDenseWaves32;
+  if (save) {
+    if (kp.cc > 0 || save->kv_len) k_f32_dense<D, TIn, VEC, true><<<grid, threads, 0, s>>>(kp, *save);
+    else k_f32_dense<D, TIn, VEC, false><<<grid, threads, 0, s>>>(kp, *save);
+  } else {
+    if (kp.cc > 0) k_f32_dense<D, TIn, VEC, true><<<grid, threads, 0, s>>>(kp, NoSave{});
+    else k_f32_dense<D, TIn, VEC, false><<<grid, threads, 0, s>>>(kp, NoSave{});
+  }
   return hipGetLastError();
 }
 template <typename TIn>
-hipError_t run_dense_t(const KParams& kp, dim3 grid, hipStream_t s) {
-  if (vec_ok<TIn>(kp)) return kp.d <= 64 ? run_dense<64, TIn, true>(kp, grid, s) : run_dense<128, TIn, true>(kp, grid, s);
-  return kp.d <= 64 ? run_dense<64, TIn, false>(kp, grid, s) : run_dense<128, TIn, false>(kp, grid, s);
+hipError_t run_dense_t(const KParams& kp, dim3 grid, const DenseSave* save, hipStream_t s) {
+  if (vec_ok<TIn>(kp)) return kp.d <= 64 ? run_dense<64, TIn, true>(kp, grid, save, s) : run_dense<128, TIn, true>(kp, grid, save, s);
+  return kp.d <= 64 ? run_dense<64, TIn, false>(kp, grid, save, s) : run_dense<128, TIn, false>(kp, grid, save, s);
 }
 
 }  // namespace

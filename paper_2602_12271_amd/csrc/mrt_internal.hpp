@@ -120,6 +120,14 @@ struct BwdParams {
                         // bf16 workspace), like that of the later iterations: the dQ kernel widens it
 };
 
+// What a dense forward call of a training step takes and leaves beyond O.
+struct DenseSave {
+  float* lse;           // [batch][heads][Nq]: natural logarithm of the sum of a row's exponentials
+  const int* kv_len;    // [batch]: keys of every sequence, or null
+  int group;            // heads that share one head of K and V
+};
+struct NoSave {};
+
 struct Plan {
   KParams kp;          // everything but the pointers
   int B, T;
@@ -143,11 +151,11 @@ mrt_status fwd_run(const void* Q, const void* K, const void* V, void* O, const m
 // bf16 storage, fp32 arithmetic (called by the launchers below)
 hipError_t run_f32_stage_r_bf16(const KParams& kp, dim3 grid, bool first, bool last, hipStream_t s);
 hipError_t run_f32_stage_l_bf16(const KParams& kp, dim3 grid, bool last, hipStream_t s);
-hipError_t run_f32_dense_bf16(const KParams& kp, dim3 grid, hipStream_t s);
+hipError_t run_f32_dense_bf16(const KParams& kp, dim3 grid, const DenseSave* save, hipStream_t s);
 hipError_t launch_f32_stage_r(const KParams& kp, int dtype, int nbh, bool first, bool last,
                               hipStream_t s);
 hipError_t launch_f32_stage_l(const KParams& kp, int dtype, int nbh, bool last, hipStream_t s);
-hipError_t launch_f32_dense(const KParams& kp, int dtype, int nbh, hipStream_t s);
+hipError_t launch_f32_dense(const KParams& kp, int dtype, int nbh, const DenseSave* save, hipStream_t s);
 
 // backward pass, fp32 (mrt_bwd_f32.hip)
 bool bwd_fits(int b1, int b2, int d);
@@ -178,6 +186,7 @@ bool bf16_stage_l_out_streams(const KParams& kp);   // its last-iteration kernel
 // workspace: null, or scratch for the parts of a call whose keys are split (used if it holds
 // bf16_dense_workspace_bytes(), 0 for a call that is not split)
 size_t bf16_dense_workspace_bytes(const KParams& kp, int nbh);
-hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, hipStream_t s);
+// save: null, or what a training step keeps
+hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseSave* save, hipStream_t s);
 
 }  // namespace mrt
