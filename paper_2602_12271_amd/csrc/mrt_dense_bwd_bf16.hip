@@ -1,4 +1,23 @@
-// Backward pass of the dense softmax attention on the bf16 matrix unit.
+// Backward pass of the dense softmax attention on the bf16 matrix unit (formulas: mrt_dense_train.hpp).
+//
+// Two launches, no atomics: the gradients of the queries, whose workgroups own queries and stream the keys, and those
+// of the keys, whose workgroups own keys and stream the queries of every head that reads them.  Seven products where
+// one launch would form five; but one launch has to add to dQ from every key tile, in an order that changes, or to
+// write and read as many partial arrays as there are key tiles (half a gigabyte each way for 12 heads of 4680
+// tokens).  The first launch also leaves what the second one needs of a row: -log2(e) lse and -delta.
+//
+// A wave owns 32 rows: their operands and gradients stay in registers, the streamed rows pass through an LDS ring 32 a
+// step, loaded by instructions that write LDS directly, several steps ahead.  Logits have the streamed rows on the M
+// side and the wave's rows on the N side of a product, so that weights, packed to bf16, are as they stand the operand
+// of the second products, whose other operand is the streamed tile read transposed.
+//
+// What bounds the launches is power: a wave's 32 rows take a kilobyte of LDS reads for every 32768 operations, and at
+// that ratio the card's clock falls until bare products reach about 1400 TFLOP/s (32 x 32 tiles) or 1550 (16 x 16),
+// where products from registers reach 1670 and 1950 and a large library product 1355.  Vector instructions do not run
+// beside another wave's 16 x 16 products and half hide behind a wave's own; behind 32 x 32 products of another wave
+// they hide whole.  So the launch of the queries, which has the registers for the logits of two steps, forms the
+// weights of one step between its own products of the next, 16 x 16 tiles; the launch of the keys, which has not, parts
+// the two waves of a SIMD by half a step, 32 x 32 tiles.
 #include "mrt_dense_train.hpp"
 #include "mrt_bf16_tiles.hpp"
 
@@ -9,327 +28,491 @@ namespace mrt {
 namespace {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((address_space(3))) void lds_void;
 
 __device__ inline f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
-// global memory (zeros beyond the resource's end) -> LDS: lane i's bytes to at + SIZE i
-__device__ inline void load_lds_16B(__amdgpu_buffer_rsrc_t r, char* at, unsigned voff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)at, 16, voff, 0, 0, 0);
+// Global memory -> LDS, zeros from `bytes` on: lane i's SIZE bytes from base + voff to LDS address at + SIZE i.  Written
+// as instructions without a result: to the compiler, which would wait for every load in flight before the next
+// transposed read, they touch no register and no counter; wait_and_meet does the waiting.
+__device__ inline u32x4 rows_at(const void* base, unsigned bytes) {
+  const unsigned long long at = (unsigned long long)base;
+  return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32)) & 0xffffu,
+               (unsigned)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
-__device__ inline void load_lds_4B(__amdgpu_buffer_rsrc_t r, char* at, unsigned voff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)at, 4, voff, 0, 0, 0);
+// (M0 holds the LDS address; it is put back, because the compiler may keep something there)
+__device__ inline void load_lds_16B(u32x4 rows, unsigned at, unsigned voff) {
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(at), "v"(voff), "s"(rows) : "memory");
+}
+__device__ inline void load_lds_4B(u32x4 rows, unsigned at, unsigned voff) {
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(at), "v"(voff), "s"(rows) : "memory");
 }
 // waits for this wave's loads but the last N, and for its LDS reads, then for the other waves
 template <int N> __device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
-constexpr int kStep = 32;      // streamed rows a step
-constexpr int kSlots = 4;      // LDS ring of steps: one is consumed, three are on their way
-
-// LDS tile of 32 rows of D bf16, not padded (loads write LDS directly, 64 consecutive 16-byte pieces an
-// instruction): piece p of row r lies at p ^ swz(r).
-template <int D> __device__ inline int swz(int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
+constexpr int kStep = 32;          // streamed rows a step
 template <int D> constexpr int kTileBytes = kStep * D * 2;
-template <int D, bool KV> constexpr int kSlotBytes = 2 * kTileBytes<D> + (KV ? 256 : 0);
-template <int D, bool KV> constexpr int kBwdLds = kSlots * kSlotBytes<D, KV>;
 
-__device__ inline float half_sum(float x) {      // over the two lanes that share lane % 32
-  float a = x, b = x;
-  row_swap32(a, b);
-  return a + b;
-}
+extern __shared__ __attribute__((aligned(1024))) char bwd_lds[];
 
-// One workgroup owns 32 NT W rows of one (batch, head): keys (KV) or queries; every wave 32 NT of them, whose
-// operands and gradients stay in its registers.  The rows of the other side stream through LDS, 32 a step.
-template <int D, int NT, int W, bool KV, bool PART>
-__global__ __launch_bounds__(64 * W) void k_bf16_dense_bwd(DenseBwd p) {
-  constexpr int KS = D / 16, FT = D / 32, ROWS = 32 * NT * W, RB = 2 * D, PIECES = D / 8;
-  constexpr int TILE_LOADS = kTileBytes<D> / 1024, LOADS = 2 * TILE_LOADS / W;   // of one array's tile; of a wave's share of both
-  constexpr int PERSTEP = LOADS + (KV ? 1 : 0);
+// The streamed rows of two arrays (and, KV, the row statistics of the queries) on their way through the LDS ring.
+//
+// A tile of 32 rows of D bf16 is not padded, because an instruction writes 64 consecutive 16-byte pieces: piece p of row
+// r lies at p ^ swz(r), whichever suits the reads (the lane that writes a piece fetches the one that belongs there).
+template <int D, int W, bool KV, int SLOTS>
+struct Stream {
+  static constexpr int RB = 2 * D, PIECES = D / 8, SLOT = 2 * kTileBytes<D> + (KV ? 256 : 0), RING = SLOTS * SLOT;
+  static constexpr int TILE_LOADS = kTileBytes<D> / 1024, LOADS = 2 * TILE_LOADS / W;   // of one array's tile; a wave's share of both
+  static constexpr int PERSTEP = LOADS + (KV ? 1 : 0);                                  // loads a wave has in flight for a step
   static_assert(LOADS * W == 2 * TILE_LOADS && (TILE_LOADS % W == 0 || W % TILE_LOADS == 0), "whole loads, of one array each");
-  extern __shared__ __attribute__((aligned(1024))) char bwd_lds[];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
+  const u16 *a, *b;
+  const float* stats;
+  long long at, bt, anext, bnext;       // elements from row to row, and from the end of a head's rows to the next head's
+  int steps, per_head, left, left0, snext;
+  unsigned to, lds0, arow, brow;
+  int wave, lane;
 
-  const int n_own = KV ? p.Nkv : p.Nq, n_heads = p.B * (KV ? p.KH : p.H);
-  const int tiles = (n_own + ROWS - 1) / ROWS, parts = PART ? (KV ? p.parts_kv : p.parts_q) : 1;
+  // n steps of rows from `row` on, `left` of them; the rows of a head end after per_head steps
+  __device__ inline void start(const u16* a_, long long at_, const u16* b_, long long bt_, const float* stats_, int n, int left_, int wave_, int lane_) {
+    a = a_; b = b_; at = at_; bt = bt_; stats = stats_;
+    steps = n; left = left_; wave = wave_; lane = lane_;
+    arow = (unsigned)at * 2u; brow = (unsigned)bt * 2u;
+    to = 0;
+    lds0 = (unsigned)(unsigned long long)(const lds_void*)bwd_lds;
+  }
+  template <typename Swz>
+  __device__ inline void issue(Swz swz) {
+    const unsigned rows = steps > 0 ? (left < kStep ? left : kStep) : 0;
+    const u32x4 ra = rows_at(a, rows ? (rows - 1) * arow + RB : 0), rb = rows_at(b, rows ? (rows - 1) * brow + RB : 0);
+    const unsigned slot = __builtin_amdgcn_readfirstlane(lds0 + to);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const bool of_b = TILE_LOADS % W == 0 ? j * W >= TILE_LOADS : wave >= TILE_LOADS;
+      const int s = (j * W + wave) % TILE_LOADS * 64 + lane, row = s / PIECES, piece = (s % PIECES) ^ swz(row);
+      load_lds_16B(of_b ? rb : ra, slot + (j * W + wave) * 1024, row * (of_b ? brow : arow) + piece * 16);
+    }
+    if constexpr (KV) {       // (every wave writes the same 256 bytes: all wait for the same number of loads)
+      load_lds_4B(rows_at(stats, rows ? 256 : 0), slot + 2 * kTileBytes<D>, lane * 4);
+      stats += 64;
+    }
+    --steps;
+    a += kStep * at;
+    b += kStep * bt;
+    left -= kStep;
+    if (KV && left <= 0 && steps > 0) {
+      a += anext;
+      b += bnext;
+      stats += snext;
+      left = left0;
+    }
+    to = to + SLOT == RING ? 0 : to + SLOT;
+  }
+  static __device__ inline int after(int slot) { return slot + SLOT == RING ? 0 : slot + SLOT; }
+};
+
+// Unit of work of a workgroup: a tile of a (batch, head)'s own rows and one of `parts` runs of the streamed ones.
+// Without a mask every XCD gets a contiguous run of units, so that those that stream the same rows share its L2;
+// under a mask, where tiles differ in length, the longest go first.
+struct Unit {
+  int bh, tile, part;
+};
+__device__ inline Unit unit_of(const DenseBwd& p, int n_heads, int tiles, int parts, bool last_first) {
   int unit = blockIdx.x;
   const int total = gridDim.x;
-  int bh, tile, part = 0;
+  Unit u;
   if (p.cc == 0) {
     const int xcd = unit & 7;
     unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (unit >> 3);
-    tile = unit % tiles;
+    u.tile = unit % tiles;
     unit /= tiles;
-    part = unit % parts;
-    bh = unit / parts;
+    u.part = unit % parts;
+    u.bh = unit / parts;
   } else {
-    bh = unit % n_heads;
+    u.bh = unit % n_heads;
     unit /= n_heads;
-    part = unit % parts;
-    tile = unit / parts;
-    if (!KV) tile = tiles - 1 - tile;
+    u.part = unit % parts;
+    u.tile = unit / parts;
+    if (last_first) u.tile = tiles - 1 - u.tile;
   }
-  const int b = bh / (KV ? p.KH : p.H), hd = bh - b * (KV ? p.KH : p.H), kvh = KV ? hd : hd / p.group;
-  const int own0 = tile * ROWS, keys = dense_keys(p, b);
-  const int own_last = own0 + ROWS < n_own ? own0 + ROWS - 1 : n_own - 1;
+  return u;
+}
 
-  // the streamed rows: queries qfirst .. Nq of every head that shares these keys, or keys 0 .. klast
-  const int qfirst = KV ? dense_first_query(p, own0) & ~31 : 0;
-  const int s_end = KV ? p.Nq : dense_last_key(p, own_last, keys);
-  const int per_head = KV ? (own0 < keys ? (s_end - qfirst + 31) >> 5 : 0) : (s_end + 31) >> 5;
-  const int all = KV ? per_head * p.group : per_head;
-  const int i0 = PART ? (int)((long long)all * part / parts) : 0, i1 = PART ? (int)((long long)all * (part + 1) / parts) : all;
+// A row's four consecutive features as bf16, or in fp32 among the parts.
+template <bool PART>
+__device__ inline void put4(u16* row, float* part, int f, f32x4 x) {
+  if constexpr (PART) *(f32x4*)(part + f) = x;
+  else *(bf16x4*)(row + f) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+}
 
-  const u16* own_a = KV ? (const u16*)p.K + b * p.k.batch + hd * p.k.head : (const u16*)p.Q + b * p.q.batch + hd * p.q.head;
-  const u16* own_b = KV ? (const u16*)p.V + b * p.v.batch + hd * p.v.head : (const u16*)p.dO + b * p.dout.batch + hd * p.dout.head;
-  const long long own_at = KV ? p.k.token : p.q.token, own_bt = KV ? p.v.token : p.dout.token;
-  const u16* st_a = KV ? (const u16*)p.Q + b * p.q.batch + (long long)hd * p.group * p.q.head
-                       : (const u16*)p.K + b * p.k.batch + kvh * p.k.head;
-  const u16* st_b = KV ? (const u16*)p.dO + b * p.dout.batch + (long long)hd * p.group * p.dout.head
-                       : (const u16*)p.V + b * p.v.batch + kvh * p.v.head;
-  const long long st_at = KV ? p.q.token : p.k.token, st_bt = KV ? p.dout.token : p.v.token;
-  const int nqb = (p.Nq + 31) >> 5;
+// ---- queries -----------------------------------------------------------------------------------
+// Two tiles of 16 queries a wave.  A step's products run in this order: A, the logits and dO V^T of the next step's keys;
+// B, dQ^T += K^T dS of this step.  Between the products of A stand the exponentials and gradients of this step's logits.
+template <int D, int W, bool PART>
+__global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
+  constexpr int NT = 2, KS = D / 32, FT = D / 16, ROWS = 16 * NT * W, RB = 2 * D, SLOTS = W == 8 ? 6 : 4;
+  using S = Stream<D, W, false, SLOTS>;
+  // rows are swizzled by pairs of pieces: the sixteen rows x two pairs a 16-byte read takes at once (rows 0-3 and 12-15
+  // of one piece, 4-11 of the next, and so on) and the eight rows x one pair of a transposed read lie on all 64 banks
+  auto swz = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int parts = PART ? p.parts_q : 1;
+  const Unit u = unit_of(p, p.B * p.H, (p.Nq + ROWS - 1) / ROWS, parts, true);
+  const int b = u.bh / p.H, hd = u.bh - b * p.H, kvh = hd / p.group;
+  const int q0 = u.tile * ROWS, q_last = q0 + ROWS < p.Nq ? q0 + ROWS - 1 : p.Nq - 1;
+  const int keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), k_end = dense_last_key(p, q_last, keys), nqb = (p.Nq + 31) >> 5;
+  const int all = (k_end + kStep - 1) / kStep;
+  const int i0 = PART ? (int)((long long)all * u.part / parts) : 0, i1 = PART ? (int)((long long)all * (u.part + 1) / parts) : all;
 
-  // streamed tile -> LDS
-  const unsigned arow = (unsigned)st_at * 2u, brow = (unsigned)st_bt * 2u;
-  unsigned voff[LOADS];
-  auto of_b = [&](int j) { return TILE_LOADS % W == 0 ? j * W >= TILE_LOADS : wave >= TILE_LOADS; };   // load j is of the second array
+  S st;
+  st.start((const u16*)p.K + b * p.k.batch + kvh * p.k.head + (long long)kStep * i0 * p.k.token, p.k.token,
+           (const u16*)p.V + b * p.v.batch + kvh * p.v.head + (long long)kStep * i0 * p.v.token, p.v.token, nullptr,
+           i1 - i0, k_end - kStep * i0, wave, lane);
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j) {
-    const int s = (j * W + wave) % TILE_LOADS * 64 + lane, row = s / PIECES, piece = (s % PIECES) ^ swz<D>(row);
-    voff[j] = row * (of_b(j) ? brow : arow) + piece * 16;
-  }
-  auto issue = [&](int i) {
-    const int slot = (i & (kSlots - 1)) * kSlotBytes<D, KV>;
-    int gh = 0, row = i << 5;
-    if (KV) {
-      gh = p.group == 1 ? 0 : i / (per_head > 0 ? per_head : 1);
-      row = qfirst + ((i - gh * per_head) << 5);
-    }
-    const int left = i < i1 ? s_end - row : 0;
-    const unsigned rows = left < 32 ? left : 32;
-    const u16* a = st_a + (KV ? gh * p.q.head : 0) + row * st_at;
-    const u16* bb = st_b + (KV ? gh * p.dout.head : 0) + row * st_bt;
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)a, 0, rows ? (rows - 1) * arow + RB : 0, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)bb, 0, rows ? (rows - 1) * brow + RB : 0, 0x00020000);
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j) load_lds_16B(of_b(j) ? rb : ra, bwd_lds + slot + (j * W + wave) * 1024, voff[j]);
-    if constexpr (KV) {       // (every wave writes the same 256 bytes: all wait for the same number of loads)
-      const float* st = p.stats + ((long long)(b * p.H + hd * p.group + gh) * nqb + (row >> 5)) * 64;
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)st, 0, rows ? 256 : 0, 0x00020000);
-      load_lds_4B(rs, bwd_lds + slot + 2 * kTileBytes<D>, lane * 4);
-    }
-  };
-  issue(i0);
-  issue(i0 + 1);
-  issue(i0 + 2);
+  for (int j = 0; j < SLOTS - 1; ++j) st.issue(swz);
 
-  // operands of this wave's rows
-  const int ow0 = own0 + 32 * NT * wave;
-  bf16x8 oa[NT][KS], ob[NT][KS];
-  int lim[NT];                         // KV: first query that sees the lane's key; else: its query's number of keys
-  float nlse[NT], ndelta[NT];          // (queries) -log2(e) lse, -delta
+  // the wave's queries
+  const u16* Qp = (const u16*)p.Q + b * p.q.batch + hd * p.q.head;
+  const u16* dOp = (const u16*)p.dO + b * p.dout.batch + hd * p.dout.head;
+  const u16* Op = (const u16*)p.O + b * p.o.batch + hd * p.o.head;
+  const int qw = q0 + 16 * NT * wave;
+  bf16x8 qf[NT][KS], of[NT][KS];
+  float nlse[NT], ndelta[NT];          // -log2(e) lse, -delta
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int r = ow0 + 32 * t + c, rc = r < n_own ? r : n_own - 1;
+    const int q = qw + 16 * t + c;
+    const long long r = q < p.Nq ? q : p.Nq - 1;
+    float sum = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      oa[t][ks] = ld_global_16B(own_a + rc * own_at + 16 * ks + 8 * hi);
-      ob[t][ks] = ld_global_16B(own_b + rc * own_bt + 16 * ks + 8 * hi);
+      qf[t][ks] = ld_global_16B(Qp + r * p.q.token + 32 * ks + 8 * g);
+      of[t][ks] = ld_global_16B(dOp + r * p.dout.token + 32 * ks + 8 * g);
+      const bf16x8 o = ld_global_16B(Op + r * p.o.token + 32 * ks + 8 * g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf((float)o[e], (float)of[t][ks][e], sum);
     }
-    lim[t] = KV ? dense_first_query(p, rc) : dense_last_key(p, rc, keys);
-    if constexpr (!KV) {
-      const u16* orow = (const u16*)p.O + b * p.o.batch + hd * p.o.head + rc * p.o.token;
-      float sum = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 o = ld_global_16B(orow + 16 * ks + 8 * hi);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf((float)o[e], (float)ob[t][ks][e], sum);
-      }
-      ndelta[t] = -half_sum(sum);
-      const float l = p.lse[(long long)bh * p.Nq + rc];
-      const bool none = l == -INFINITY;
-      nlse[t] = none ? -INFINITY : -kLog2e * l;
-      if (part == 0 && hi == 0 && r < nqb * 32) {
-        float* st = p.stats + ((long long)bh * nqb + (r >> 5)) * 64 + (r & 31);
-        st[0] = none || r >= p.Nq ? -INFINITY : -l / p.scale;
-        st[32] = r >= p.Nq ? 0.f : ndelta[t];
-      }
+    ndelta[t] = -xsum(sum);
+    const float l = p.lse[(long long)u.bh * p.Nq + r];
+    nlse[t] = l == -INFINITY ? -INFINITY : -kLog2e * l;       // (a row that sees no key: weights of zero)
+    if (u.part == 0 && g == 0 && q < nqb * 32) {
+      float* s = p.stats + ((long long)u.bh * nqb + (q >> 5)) * 64 + (q & 31);
+      s[0] = q >= p.Nq ? -INFINITY : nlse[t];
+      s[32] = q >= p.Nq ? 0.f : ndelta[t];
     }
   }
   const float scale2 = p.scale * kLog2e;
-  f32x16 g1[KV ? NT : 1][FT], g2[NT][FT];    // dV^T; dK^T or dQ^T
+  f32x4 dq[NT][FT];    // dQ^T
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int f = 0; f < FT; ++f)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if constexpr (KV) g1[t][f][r] = 0.f;
-        g2[t][f][r] = 0.f;
-      }
+    for (int f = 0; f < FT; ++f) dq[t][f] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // where a lane reads its operands of a tile
-  int arow_at[KS], tr_at[FT];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) arow_at[ks] = c * RB + ((2 * ks) ^ swz<D>(c)) * 16 + hi * 16;
-  const int G = lane >> 4, s = lane & 15, trow = 4 * hi + (s >> 2);
-#pragma unroll
-  for (int f = 0; f < FT; ++f)       // (rows 8 apart are swizzled alike)
-    tr_at[f] = trow * RB + (((4 * f + 2 * (G & 1)) ^ swz<D>(trow)) * 16) + 8 * (s & 3);
-
-  auto row_op = [&](const char* at, int ks) { return *(const bf16x8*)(at + arow_at[ks]); };
-  auto tr_op = [&](const char* at, int f, int kk) {
-    const u16* q = (const u16*)(at + tr_at[f] + 16 * kk * RB);
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(ld_lds_tr(q), ld_lds_tr(q + 8 * D), 0, 1, 2, 3, 4, 5, 6, 7));
+  // where a lane reads the first of its operands of a tile; the others differ in bits (^) and rows (+)
+  const int s4 = c >> 2, trow = 4 * g + s4;
+  const int row_at = c * RB + (swz(c) ^ g) * 16, tr_at = trow * RB + swz(trow) * 16 + 8 * (c & 3);
+  auto row_op = [&](int at, int ks, int m) { return *(const bf16x8*)(bwd_lds + (at ^ (64 * ks)) + 16 * m * RB); };
+  auto tr_op = [&](int at, int f) {
+    const u16* q = (const u16*)(bwd_lds + (at ^ (32 * f)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(ld_lds_tr(q), ld_lds_tr(q + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
   };
 
-  for (int i = i0; i < i1; ++i) {
-    wait_and_meet<2 * PERSTEP>();
-    issue(i + 3);
-    const char* at = bwd_lds + (i & (kSlots - 1)) * kSlotBytes<D, KV>;
-    const char* bt = at + kTileBytes<D>;
-    int row = i << 5;
-    if (KV) row = qfirst + ((p.group == 1 ? i : i % per_head) << 5);
-
-    f32x16 sv[NT], dp[NT];
-    if constexpr (KV) {
-      const float* st = (const float*)(bt + kTileBytes<D>) + 4 * hi;
+  f32x4 sv[2][NT][2], dp[2][NT][2];     // logits and dO V^T of two steps in turn
+  bf16x8 db[NT];
+  // operands are read from LDS three ahead of their products, over the end of a step too
+  constexpr int NA = 4 * KS, OPS = NA + FT;
+  static_assert(OPS % 4 == 0, "operands keep their registers from step to step");
+  bf16x8 op[4];
+  auto read_op = [&](int i, int next, int slot) {
+    if (i < NA) op[i & 3] = row_op(i & 1 ? next + kTileBytes<D> : next, i >> 2, (i >> 1) & 1);
+    else op[i & 3] = tr_op(slot, i - NA);
+  };
+  auto product_a = [&](auto buf, int i, int t) {
+    constexpr int B = decltype(buf)::value;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const int ks = i >> 2, m = (i >> 1) & 1;
+    if ((i & 1) == 0) sv[B][t][m] = mfma(op[i & 3], qf[t][ks], ks == 0 ? zero : sv[B][t][m]);
+    else dp[B][t][m] = mfma(op[i & 3], of[t][ks], ks == 0 ? zero : dp[B][t][m]);
+  };
+  auto soften = [&](auto buf, int e) {
+    constexpr int B = decltype(buf)::value;
+    const int t = e >> 3, m = (e >> 2) & 1, r = e & 3;
+    dp[B][t][m][r] = exp2_fast(fmaf(sv[B][t][m][r], scale2, nlse[t])) * (dp[B][t][m][r] + ndelta[t]);
+    if ((e & 7) == 7) db[t] = pack8(dp[B][t][0], dp[B][t][1]);
+  };
+  const int free_keys = dense_last_key(p, q0, keys);       // every query of the workgroup sees these
+  int row = kStep * i0, slot = 0, next = S::SLOT;
+  auto step = [&](auto buf, bool live) {
+    constexpr int B = decltype(buf)::value;
+    const std::integral_constant<int, 1 - B> other;
+    // some query does not see the step whole, or there is no such step (an odd number of them)
+    if (!live || row + kStep > free_keys) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x4 l = *(const f32x4*)(st + 8 * j), dl = *(const f32x4*)(st + 32 + 8 * j);
+      for (int t = 0; t < NT; ++t) {
+        const int q = qw + 16 * t + c, lim = live ? dense_last_key(p, q < p.Nq ? q : p.Nq - 1, keys) : 0;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) { sv[t][4 * j + r] = l[r]; dp[t][4 * j + r] = dl[r]; }
-      }
-    } else {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) { sv[t][r] = 0.f; dp[t][r] = ndelta[t]; }
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 a = row_op(at, ks);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) sv[t] = mfma32(a, oa[t][ks], sv[t]);
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 a = row_op(bt, ks);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) dp[t] = mfma32(a, ob[t][ks], dp[t]);
-    }
-    // a step that some row of the workgroup does not see whole
-    const bool edge = KV ? p.cc != 0 && row < dense_first_query(p, own_last) : row + 32 > dense_last_key(p, own0, keys);
-    if (edge) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int at_row = row + 8 * (r >> 2) + 4 * hi + (r & 3);
-          if (KV ? at_row < lim[t] : at_row >= lim[t]) { sv[t][r] = -INFINITY; dp[t][r] = 0.f; }
-        }
-    }
-    bf16x8 pb[NT][2], db[NT][2];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float w = exp2_fast(KV ? sv[t][r] * scale2 : fmaf(sv[t][r], scale2, nlse[t]));
-        const float d = w * dp[t][r];
-        pb[t][r >> 3][r & 7] = (__bf16)w;
-        db[t][r >> 3][r & 7] = (__bf16)d;
+          for (int r = 0; r < 4; ++r)
+            if (row + 16 * m + 4 * g + r >= lim) { sv[B][t][m][r] = -INFINITY; dp[B][t][m][r] = 0.f; }
       }
     }
+    const int at = slot + tr_at, nt = next + row_at;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
+    for (int i = 0; i < NA; ++i) {
+      read_op(i + 3, nt, at);
 #pragma unroll
-      for (int f = 0; f < FT; ++f) {
-        if constexpr (KV) {
-          const bf16x8 a = tr_op(bt, f, kk);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) g1[t][f] = mfma32(a, pb[t][kk], g1[t][f]);
-        }
+      for (int t = 0; t < NT; ++t) {
+        product_a(other, i, t);
+        constexpr int EVERY = NA * NT / (8 * NT);
+        if ((i * NT + t) % EVERY == 0) soften(buf, (i * NT + t) / EVERY);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    // (the ring holds this step, the next one and the one after, which the first reads below are for)
+    wait_and_meet<(SLOTS - 4) * S::PERSTEP>();
+    st.issue(swz);
+    const int then = S::after(next), nnt = then + row_at;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
+    for (int i = NA; i < OPS; ++i) {
+      if (i + 3 < OPS) read_op(i + 3, nt, at);
+      else read_op(i + 3 - OPS, nnt, at);
 #pragma unroll
-      for (int f = 0; f < FT; ++f) {
-        const bf16x8 a = tr_op(at, f, kk);
+      for (int t = 0; t < NT; ++t) dq[t][i - NA] = mfma(op[i & 3], db[t], dq[t][i - NA]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    slot = next;
+    next = then;
+    row += kStep;
+  };
+  wait_and_meet<(SLOTS - 3) * S::PERSTEP>();
+  if (i0 < i1) {
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) g2[t][f] = mfma32(a, db[t][kk], g2[t][f]);
-      }
+    for (int i = 0; i < NA; ++i) {
+      read_op(i, row_at, 0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) product_a(even, i, t);
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) read_op(i, next + row_at, 0);
+    for (int i = i0; i < i1; i += 2) {
+      step(even, true);
+      step(odd, i + 1 < i1);
+    }
   }
-
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing is on its way to LDS when the workgroup leaves it
 
-  typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int r = ow0 + 32 * t + c;
-    if (r >= n_own) continue;
-    const bool live = KV ? r < keys : true;
-    if constexpr (PART) {
-      float* to = (KV ? p.pk : p.pq) + (((long long)part * n_heads + bh) * n_own + r) * D + 4 * hi;
-      float* tv = KV ? p.pv + (((long long)part * n_heads + bh) * n_own + r) * D + 4 * hi : nullptr;
+    const long long q = qw + 16 * t + c;
+    if (q >= p.Nq) continue;
+    u16* to = (u16*)p.dQ + b * p.dq.batch + hd * p.dq.head + q * p.dq.token + 4 * g;
+    float* part = p.pq + (((long long)u.part * p.B * p.H + u.bh) * p.Nq + q) * D + 4 * g;
 #pragma unroll
-      for (int f = 0; f < FT; ++f)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          f32x4 x, y;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[e] = live ? g2[t][f][4 * j + e] * p.scale : 0.f;
-            if constexpr (KV) y[e] = live ? g1[t][f][4 * j + e] : 0.f;
-          }
-          *(f32x4*)(to + 32 * f + 8 * j) = x;
-          if constexpr (KV) *(f32x4*)(tv + 32 * f + 8 * j) = y;
-        }
-    } else {
-      u16* to = (KV ? (u16*)p.dK + b * p.dk.batch + hd * p.dk.head + r * p.dk.token
-                    : (u16*)p.dQ + b * p.dq.batch + hd * p.dq.head + r * p.dq.token) + 4 * hi;
-      u16* tv = KV ? (u16*)p.dV + b * p.dv.batch + hd * p.dv.head + r * p.dv.token + 4 * hi : nullptr;
-#pragma unroll
-      for (int f = 0; f < FT; ++f)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          bf16x4 x, y;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[e] = (__bf16)(live ? g2[t][f][4 * j + e] * p.scale : 0.f);
-            if constexpr (KV) y[e] = (__bf16)(live ? g1[t][f][4 * j + e] : 0.f);
-          }
-          *(bf16x4*)(to + 32 * f + 8 * j) = x;
-          if constexpr (KV) *(bf16x4*)(tv + 32 * f + 8 * j) = y;
-        }
-    }
+    for (int f = 0; f < FT; ++f) put4<PART>(to, part, 16 * f, dq[t][f] * p.scale);
   }
 }
 
-template <int D, int NT, int W, bool KV, bool PART>
-hipError_t run_bwd(const DenseBwd& p, hipStream_t s) {
-  constexpr int lds = kBwdLds<D, KV>, rows = 32 * NT * W;
-  const hipError_t e = hipFuncSetAttribute((const void*)k_bf16_dense_bwd<D, NT, W, KV, PART>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return e;
-  const int n = KV ? p.Nkv : p.Nq, heads = p.B * (KV ? p.KH : p.H), parts = PART ? (KV ? p.parts_kv : p.parts_q) : 1;
-  k_bf16_dense_bwd<D, NT, W, KV, PART><<<(n + rows - 1) / rows * heads * parts, 64 * W, lds, s>>>(p);
-  return hipGetLastError();
+// ---- keys --------------------------------------------------------------------------------------
+// One tile of 32 keys a wave.  A step is a vector phase (weights and gradients of the logits) and a matrix phase (what
+// these give to dV^T and dK^T, then the logits and dO V^T of the next step's queries), and the two waves of a SIMD are
+// half a step apart: between two meetings the first half of the workgroup takes its matrix phase, then its vector phase,
+// the second half its vector phase, then its matrix phase.
+
+template <int D, int W, bool PART>
+__global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
+  constexpr int KS = D / 16, FT = D / 32, ROWS = 32 * W, RB = 2 * D, SLOTS = W == 8 ? 5 : 4, AHEAD = 3;
+  using S = Stream<D, W, true, SLOTS>;
+  // sixteen rows that agree in a piece lie on all 64 banks (those a 16-byte read takes at once: 0-3, 12-15 and 20-27 of a
+  // tile, and the other sixteen), and so do four consecutive rows of four pieces (a transposed read).  Rows 8 apart
+  // differ in bit 1, rows 16 apart in nothing.
+  auto swz = [](int row) { return D == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : (row & 2) << 1 | ((row >> 2) & 3); };
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
+  const int parts = PART ? p.parts_kv : 1;
+  const Unit u = unit_of(p, p.B * p.KH, (p.Nkv + ROWS - 1) / ROWS, parts, false);
+  const int b = u.bh / p.KH, hd = u.bh - b * p.KH;
+  const int k0 = u.tile * ROWS, k_last = k0 + ROWS < p.Nkv ? k0 + ROWS - 1 : p.Nkv - 1;
+  const int keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), nqb = (p.Nq + 31) >> 5;
+  const int q_first = dense_first_query(p, k0) & ~(kStep - 1);      // of every head that reads these keys
+  const int per_head = k0 < keys && q_first < p.Nq ? (p.Nq - q_first + kStep - 1) / kStep : 0, all = per_head * p.group;
+  const int i0 = PART ? (int)((long long)all * u.part / parts) : 0, i1 = PART ? (int)((long long)all * (u.part + 1) / parts) : all;
+
+  S st;
+  int row;           // of the step in hand
+  {
+    const int gh = per_head > 0 ? i0 / per_head : 0, hq = hd * p.group + gh;
+    row = q_first + kStep * (i0 - gh * per_head);
+    st.start((const u16*)p.Q + b * p.q.batch + hq * p.q.head + row * p.q.token, p.q.token,
+             (const u16*)p.dO + b * p.dout.batch + hq * p.dout.head + row * p.dout.token, p.dout.token,
+             p.stats + ((long long)(b * p.H + hq) * nqb + (row >> 5)) * 64, i1 - i0, p.Nq - row, wave, lane);
+    st.anext = p.q.head - (long long)per_head * kStep * p.q.token;
+    st.bnext = p.dout.head - (long long)per_head * kStep * p.dout.token;
+    st.snext = 64 * (nqb - per_head);
+    st.left0 = p.Nq - q_first;
+  }
+#pragma unroll
+  for (int j = 0; j < SLOTS - 1; ++j) st.issue(swz);
+
+  // the wave's keys
+  const int kw = k0 + 32 * wave, key = kw + c;
+  const long long kr = key < p.Nkv ? key : p.Nkv - 1;
+  const u16* Kp = (const u16*)p.K + b * p.k.batch + hd * p.k.head + kr * p.k.token;
+  const u16* Vp = (const u16*)p.V + b * p.v.batch + hd * p.v.head + kr * p.v.token;
+  bf16x8 kf[KS], vf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kf[ks] = ld_global_16B(Kp + 16 * ks + 8 * hi);
+    vf[ks] = ld_global_16B(Vp + 16 * ks + 8 * hi);
+  }
+  const float scale2 = p.scale * kLog2e;
+  f32x16 dv[FT], dk[FT];    // dV^T, dK^T
+#pragma unroll
+  for (int f = 0; f < FT; ++f) dv[f] = dk[f] = f32x16{};
+
+  // where a lane reads the first of its operands of a tile; the others differ in bits (^) and rows (+)
+  const int G = lane >> 4, s = lane & 15, trow = 4 * hi + (s >> 2);
+  const int row_at = c * RB + (swz(c) ^ hi) * 16, tr_at = trow * RB + ((2 * (G & 1) + ((s >> 1) & 1)) ^ swz(trow)) * 16 + 8 * (s & 1);
+  auto row_op = [&](int at, int ks) { return *(const bf16x8*)(bwd_lds + (at ^ (32 * ks))); };
+  auto tr_op = [&](int at, int f, int kk) {
+    const char* lo = bwd_lds + (at ^ (64 * f)) + 16 * kk * RB;
+    const char* up = bwd_lds + (at ^ (64 * f + 32)) + (16 * kk + 8) * RB;
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(ld_lds_tr((const u16*)lo), ld_lds_tr((const u16*)up), 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto stats_at = [&](int slot, int which, int j) { return *(const f32x4*)(bwd_lds + slot + 2 * kTileBytes<D> + 128 * which + 32 * j + 16 * hi); };
+
+  f32x16 sv, dp;
+  bf16x8 pb[2], db[2];
+  // The matrix phase.  Operands are read from LDS AHEAD ahead of their products, in this fixed order.
+  constexpr int N1 = 2 * FT, NG = 2 * N1, OPS = NG + 2 * KS;
+  bf16x8 op[OPS];
+  auto read_op = [&](int i, int at, int nt) {
+    if (i < N1) op[i] = tr_op(at + kTileBytes<D>, i % FT, i / FT);
+    else if (i < NG) op[i] = tr_op(at, (i - N1) % FT, (i - N1) / FT);
+    else op[i] = row_op((i - NG) & 1 ? nt + kTileBytes<D> : nt, (i - NG) / 2);
+  };
+  auto matrix = [&](int slot, int next, int from) {
+    const int at = slot + tr_at, nt = next + row_at;
+#pragma unroll
+    for (int i = 0; i < OPS; ++i)
+      if (i >= from && i < from + AHEAD) read_op(i, at, nt);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < OPS; ++i) {
+      if (i < from) continue;
+      if (i + AHEAD < OPS) read_op(i + AHEAD, at, nt);
+      if (i == from ? i == NG : i == NG - 1) {          // the sums of dO V^T begin with -delta
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 x = stats_at(next, 1, j);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dp[4 * j + r] = x[r];
+        }
+      }
+      if (i < N1) dv[i % FT] = mfma32(op[i], pb[i / FT], dv[i % FT]);
+      else if (i < NG) dk[(i - N1) % FT] = mfma32(op[i], db[(i - N1) / FT], dk[(i - N1) % FT]);
+      else if (((i - NG) & 1) == 0) sv = mfma32(op[i], kf[(i - NG) / 2], i == NG ? f32x16{} : sv);
+      else dp = mfma32(op[i], vf[(i - NG) / 2], dp);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // The vector phase, of the step in `slot` whose queries begin at `row`.
+  const int free_from = p.cc ? dense_first_query(p, k_last) : 0;       // every key of the workgroup is seen from here on
+  auto soften = [&](int row, int slot) {
+    f32x4 nl[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) nl[j] = stats_at(slot, 0, j);
+    if (row < free_from) {
+      const int lim = dense_first_query(p, (int)kr);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (row + 8 * (r >> 2) + 4 * hi + (r & 3) < lim) { sv[r] = -INFINITY; dp[r] = 0.f; }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float w = exp2_fast(fmaf(sv[r], scale2, nl[r >> 2][r & 3]));
+      pb[r >> 3][r & 7] = (__bf16)w;
+      db[r >> 3][r & 7] = (__bf16)(w * dp[r]);
+    }
+  };
+
+  const bool second = wave >= W / 2;
+  int left_steps = per_head - (per_head > 0 ? i0 % per_head : 0);
+  wait_and_meet<(SLOTS - 2) * S::PERSTEP>();
+  if (i0 < i1) matrix(0, 0, NG);
+  for (int i = i0, slot = 0; i < i1; ++i) {
+    const int next = S::after(slot);
+    if (second) {
+      wait_and_meet<(SLOTS - 3) * S::PERSTEP>();
+      st.issue(swz);
+    }
+    soften(row, slot);
+    __builtin_amdgcn_sched_barrier(0);
+    if (!second) {
+      wait_and_meet<(SLOTS - 3) * S::PERSTEP>();
+      st.issue(swz);
+    }
+    matrix(slot, next, 0);
+    slot = next;
+    row += kStep;
+    if (--left_steps == 0) {
+      left_steps = per_head;
+      row = q_first;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing is on its way to LDS when the workgroup leaves it
+
+  if (key >= p.Nkv) return;
+  const bool live = key < keys;                 // (padding's columns may hold anything)
+  u16* tk = (u16*)p.dK + b * p.dk.batch + hd * p.dk.head + kr * p.dk.token + 4 * hi;
+  u16* tv = (u16*)p.dV + b * p.dv.batch + hd * p.dv.head + kr * p.dv.token + 4 * hi;
+  const long long part = (((long long)u.part * p.B * p.KH + u.bh) * p.Nkv + kr) * D + 4 * hi;
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x4 x, y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = live ? dk[f][4 * j + e] * p.scale : 0.f;
+        y[e] = live ? dv[f][4 * j + e] : 0.f;
+      }
+      put4<PART>(tk, p.pk + part, 32 * f + 8 * j, x);
+      put4<PART>(tv, p.pv + part, 32 * f + 8 * j, y);
+    }
 }
 
-template <int D, int NT, int W, bool KV>
-hipError_t run_parts(const DenseBwd& p, hipStream_t s) {
-  if ((KV ? p.parts_kv : p.parts_q) == 1) return run_bwd<D, NT, W, KV, false>(p, s);
-  const hipError_t e = run_bwd<D, NT, W, KV, true>(p, s);
-  return e != hipSuccess ? e : launch_dense_bwd_join(p, KV, MRT_BF16, s);
+template <typename Kernel>
+hipError_t launch(Kernel kernel, int rows, int heads, int tile, int parts, int threads, int lds, const DenseBwd& p, hipStream_t s) {
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)((rows + tile - 1) / tile * (long long)heads * parts), threads, lds, s>>>(p);
+  return hipGetLastError();
+}
+template <int D, int W>
+hipError_t run_q(const DenseBwd& p, hipStream_t s) {
+  constexpr int lds = Stream<D, W, false, W == 8 ? 6 : 4>::RING;
+  if (p.parts_q == 1) return launch(k_bf16_dense_bwd_q<D, W, false>, p.Nq, p.B * p.H, 32 * W, 1, 64 * W, lds, p, s);
+  const hipError_t e = launch(k_bf16_dense_bwd_q<D, W, true>, p.Nq, p.B * p.H, 32 * W, p.parts_q, 64 * W, lds, p, s);
+  return e != hipSuccess ? e : launch_dense_bwd_join(p, false, MRT_BF16, s);
+}
+template <int D, int W>
+hipError_t run_kv(const DenseBwd& p, hipStream_t s) {
+  constexpr int lds = Stream<D, W, true, W == 8 ? 5 : 4>::RING;
+  if (p.parts_kv == 1) return launch(k_bf16_dense_bwd_kv<D, W, false>, p.Nkv, p.B * p.KH, 32 * W, 1, 64 * W, lds, p, s);
+  const hipError_t e = launch(k_bf16_dense_bwd_kv<D, W, true>, p.Nkv, p.B * p.KH, 32 * W, p.parts_kv, 64 * W, lds, p, s);
+  return e != hipSuccess ? e : launch_dense_bwd_join(p, true, MRT_BF16, s);
 }
 
 }  // namespace
 
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
-  DenseBwdShape shape = {256, 1, p.d == 64 ? 256 : 128, 1};
+  DenseBwdShape shape = {256, 1, 256, 1};
   const long long cus = compute_units(), most = 1 << 27;      // elements of the parts
   auto parts = [&](long long rows, long long heads, long long tile, long long streamed) {
     const long long wgs = (rows + tile - 1) / tile * heads, steps = (streamed + 31) / 32;
@@ -344,17 +527,16 @@ DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
 }
 
 hipError_t launch_bf16_dense_bwd(const DenseBwd& p, const DenseBwdShape& shape, hipStream_t s) {
-  (void)shape;
+  const bool q8 = shape.rows_q == 256, kv8 = shape.rows_kv == 256;
   hipError_t e;
   if (p.d == 64) {
-    e = run_parts<64, 2, 4, false>(p, s);
-    return e != hipSuccess ? e : run_parts<64, 1, 8, true>(p, s);
+    e = q8 ? run_q<64, 8>(p, s) : run_q<64, 4>(p, s);
+    if (e == hipSuccess) e = kv8 ? run_kv<64, 8>(p, s) : run_kv<64, 4>(p, s);
+  } else {
+    e = q8 ? run_q<128, 8>(p, s) : run_q<128, 4>(p, s);
+    if (e == hipSuccess) e = kv8 ? run_kv<128, 8>(p, s) : run_kv<128, 4>(p, s);
   }
-  e = run_parts<128, 2, 4, false>(p, s);
-  return e != hipSuccess ? e : run_parts<128, 1, 4, true>(p, s);
+  return e;
 }
 
-#ifdef PROBE
-hipError_t (*probes[])(const DenseBwd&, hipStream_t) = {PROBE};
-#endif
 }  // namespace mrt

@@ -198,29 +198,34 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p) {
     }
 }
 
-// A gradient from its parts, added in their order.  A thread owns four features of a row.
-template <typename T>
-__global__ __launch_bounds__(256) void k_dense_bwd_join(const float* parts, int n, void* to, mrt_strides st, int rows,
-                                                        int tokens, int heads, int d) {
+// Gradients from their parts, added in their order: dQ, or dK and dV (blockIdx.y).  A thread owns four features of a
+// row and has four parts in flight: what it waits for is memory.
+struct JoinArgs {
+  const float* parts[2];
+  void* to[2];
+  mrt_strides st[2];
+};
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_dense_bwd_join(JoinArgs a, int n, long long rows, int tokens, int heads, int d) {
+  constexpr int AHEAD = 4;
+  const bool second = blockIdx.y != 0;
   const int quads = (d + 3) >> 2;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int row = (int)(at / quads), v = 4 * (int)(at - (long long)row * quads);
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / quads;
+  const int v = 4 * (int)(at - row * quads);
   if (row >= rows) return;
-  const int left = d - v < 4 ? d - v : 4;
-  const float* from = parts + (long long)row * d + v;
-  float x[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < n; ++i, from += (long long)rows * d)
+  const float* from = (second ? a.parts[1] : a.parts[0]) + row * d;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < n; i += AHEAD) {
+    f32x4 y[AHEAD];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < left) x[e] += from[e];
-  const int bh = row / tokens, tok = row - bh * tokens, b = bh / heads, hd = bh - b * heads;
-  T* out = (T*)to + b * st.batch + hd * st.head + tok * st.token + v;
+    for (int k = 0; k < AHEAD; ++k) y[k] = ld4<VEC>(from + (long long)(i + k < n ? i + k : n - 1) * rows * d, v, d);
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < left) {
-      if constexpr (sizeof(T) == 2) out[e] = f2bf(x[e]);
-      else out[e] = x[e];
-    }
+    for (int k = 0; k < AHEAD; ++k)
+      if (i + k < n) x = x + y[k];
+  }
+  const int bh = (int)(row / tokens), tok = (int)(row - (long long)bh * tokens), b = bh / heads, hd = bh - b * heads;
+  const mrt_strides& st = second ? a.st[1] : a.st[0];
+  st4<VEC>((T*)(second ? a.to[1] : a.to[0]) + b * st.batch + hd * st.head + tok * st.token, x, v, d);
 }
 
 template <int D, typename T, bool VEC, bool KV>
@@ -257,16 +262,15 @@ hipError_t run_t(const DenseBwd& p, int dtype, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStream_t s) {
-  const int tokens = kv ? p.Nkv : p.Nq, heads = kv ? p.KH : p.H, rows = p.B * heads * tokens;
-  const long long threads = (long long)rows * ((p.d + 3) / 4);
-  for (int i = 0; i < (kv ? 2 : 1); ++i) {
-    const float* from = kv ? (i ? p.pv : p.pk) : p.pq;
-    void* to = kv ? (i ? p.dV : p.dK) : p.dQ;
-    const mrt_strides& st = kv ? (i ? p.dv : p.dk) : p.dq;
-    const dim3 grid((unsigned)((threads + 255) / 256));
-    if (dtype == MRT_BF16) k_dense_bwd_join<u16><<<grid, 256, 0, s>>>(from, kv ? p.parts_kv : p.parts_q, to, st, rows, tokens, heads, p.d);
-    else k_dense_bwd_join<float><<<grid, 256, 0, s>>>(from, kv ? p.parts_kv : p.parts_q, to, st, rows, tokens, heads, p.d);
-  }
+  const int tokens = kv ? p.Nkv : p.Nq, heads = kv ? p.KH : p.H, n = kv ? p.parts_kv : p.parts_q;
+  const long long rows = (long long)p.B * heads * tokens, threads = rows * ((p.d + 3) / 4);
+  const JoinArgs a = {{kv ? p.pk : p.pq, p.pv}, {kv ? p.dK : p.dQ, p.dV}, {kv ? p.dk : p.dq, p.dv}};
+  const dim3 grid((unsigned)((threads + 255) / 256), kv ? 2 : 1);
+  const bool bf16 = dtype == MRT_BF16, vec = bf16 ? rows_of_four<u16>(p) : rows_of_four<float>(p);
+  if (bf16 && vec) k_dense_bwd_join<u16, true><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
+  else if (bf16) k_dense_bwd_join<u16, false><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
+  else if (vec) k_dense_bwd_join<float, true><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
+  else k_dense_bwd_join<float, false><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
   return hipGetLastError();
 }
 
