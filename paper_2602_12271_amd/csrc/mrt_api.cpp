@@ -996,7 +996,7 @@ mrt_status dense_attn_bwd(const void* Q, const void* K, const void* V, const voi
   d.parts_q = w.shape.parts_q; d.parts_kv = w.shape.parts_kv;
   const hipStream_t s = (hipStream_t)hip_stream;
   hipError_t e = timed_launch(s, MRT_KERNEL_DENSE_BWD, [&] {
-    return f32 ? launch_f32_dense_bwd(d, w.shape, p->dtype, s) : launch_bf16_dense_bwd(d, w.shape, s);
+    return f32 ? launch_f32_dense_bwd(d, p->dtype, s) : launch_bf16_dense_bwd(d, s);
   });
   if (e != hipSuccess) return hip_fail(e, "dense backward launch");
   return MRT_OK;

@@ -13,15 +13,18 @@
 //
 // What bounds the launches is power: a wave's 32 rows take a kilobyte of LDS reads for every 32768 operations, and at
 // that ratio the card's clock falls until bare products reach about 1400 TFLOP/s (32 x 32 tiles) or 1550 (16 x 16),
-// where products from registers reach 1670 and 1950 and a large library product 1355.  Vector instructions do not run
-// beside another wave's 16 x 16 products and half hide behind a wave's own; behind 32 x 32 products of another wave
-// they hide whole.  So the launch of the queries, which has the registers for the logits of two steps, forms the
-// weights of one step between its own products of the next, 16 x 16 tiles; the launch of the keys, which has not, parts
-// the two waves of a SIMD by half a step, 32 x 32 tiles.
+// where products from registers reach 1670 and 1950 and a large library product 1355.  Vector instructions hardly run
+// beside another wave's 16 x 16 products and half hide behind a wave's own; beside 32 x 32 products of another wave they
+// run whole.  So the launch of the queries, which has the registers for the logits of two steps, forms the weights of
+// one step between its own products of the next, 16 x 16 tiles; the launch of the keys, which has not, takes 32 x 32
+// tiles and leaves it to the two workgroups of a compute unit to be in different phases.  (Waves of 64 rows, one to a
+// SIMD, halve the LDS reads, but what does not fit 256 registers moves between the two halves of the register file:
+// 1.2 to 1.8 times as long.)
 #include "mrt_dense_train.hpp"
 #include "mrt_bf16_tiles.hpp"
 
 #include <algorithm>
+#include <cmath>
 
 namespace mrt {
 
@@ -56,7 +59,9 @@ __device__ inline void load_lds_4B(u32x4 rows, unsigned at, unsigned voff) {
 // waits for this wave's loads but the last N, and for its LDS reads, then for the other waves
 template <int N> __device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves;     // two workgroups to a compute unit
 constexpr int kStep = 32;          // streamed rows a step
+constexpr int kSlots = 4;          // steps in the LDS ring: two or three in use, the others on their way
 template <int D> constexpr int kTileBytes = kStep * D * 2;
 
 extern __shared__ __attribute__((aligned(1024))) char bwd_lds[];
@@ -65,12 +70,12 @@ extern __shared__ __attribute__((aligned(1024))) char bwd_lds[];
 //
 // A tile of 32 rows of D bf16 is not padded, because an instruction writes 64 consecutive 16-byte pieces: piece p of row
 // r lies at p ^ swz(r), whichever suits the reads (the lane that writes a piece fetches the one that belongs there).
-template <int D, int W, bool KV, int SLOTS>
+template <int D, bool KV>
 struct Stream {
-  static constexpr int RB = 2 * D, PIECES = D / 8, SLOT = 2 * kTileBytes<D> + (KV ? 256 : 0), RING = SLOTS * SLOT;
-  static constexpr int TILE_LOADS = kTileBytes<D> / 1024, LOADS = 2 * TILE_LOADS / W;   // of one array's tile; a wave's share of both
+  static constexpr int RB = 2 * D, PIECES = D / 8, SLOT = 2 * kTileBytes<D> + (KV ? 256 : 0), RING = kSlots * SLOT;
+  static constexpr int TILE_LOADS = kTileBytes<D> / 1024, LOADS = 2 * TILE_LOADS / kWaves;   // of one array's tile; a wave's share of both
   static constexpr int PERSTEP = LOADS + (KV ? 1 : 0);                                  // loads a wave has in flight for a step
-  static_assert(LOADS * W == 2 * TILE_LOADS && (TILE_LOADS % W == 0 || W % TILE_LOADS == 0), "whole loads, of one array each");
+  static_assert(TILE_LOADS % kWaves == 0, "whole loads, of one array each");
   const u16 *a, *b;
   const float* stats;
   long long at, bt, anext, bnext;       // elements from row to row, and from the end of a head's rows to the next head's
@@ -93,9 +98,9 @@ struct Stream {
     const unsigned slot = __builtin_amdgcn_readfirstlane(lds0 + to);
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const bool of_b = TILE_LOADS % W == 0 ? j * W >= TILE_LOADS : wave >= TILE_LOADS;
-      const int s = (j * W + wave) % TILE_LOADS * 64 + lane, row = s / PIECES, piece = (s % PIECES) ^ swz(row);
-      load_lds_16B(of_b ? rb : ra, slot + (j * W + wave) * 1024, row * (of_b ? brow : arow) + piece * 16);
+      const bool of_b = j * kWaves >= TILE_LOADS;
+      const int s = (j * kWaves + wave) % TILE_LOADS * 64 + lane, row = s / PIECES, piece = (s % PIECES) ^ swz(row);
+      load_lds_16B(of_b ? rb : ra, slot + (j * kWaves + wave) * 1024, row * (of_b ? brow : arow) + piece * 16);
     }
     if constexpr (KV) {       // (every wave writes the same 256 bytes: all wait for the same number of loads)
       load_lds_4B(rows_at(stats, rows ? 256 : 0), slot + 2 * kTileBytes<D>, lane * 4);
@@ -153,18 +158,18 @@ __device__ inline void put4(u16* row, float* part, int f, f32x4 x) {
 // ---- queries -----------------------------------------------------------------------------------
 // Two tiles of 16 queries a wave.  A step's products run in this order: A, the logits and dO V^T of the next step's keys;
 // B, dQ^T += K^T dS of this step.  Between the products of A stand the exponentials and gradients of this step's logits.
-template <int D, int W, bool PART>
-__global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
-  constexpr int NT = 2, KS = D / 32, FT = D / 16, ROWS = 16 * NT * W, RB = 2 * D, SLOTS = W == 8 ? 6 : 4;
-  using S = Stream<D, W, false, SLOTS>;
+template <int D, bool PART>
+__global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
+  constexpr int NT = 2, KS = D / 32, FT = D / 16, RB = 2 * D;
+  using S = Stream<D, false>;
   // rows are swizzled by pairs of pieces: the sixteen rows x two pairs a 16-byte read takes at once (rows 0-3 and 12-15
   // of one piece, 4-11 of the next, and so on) and the eight rows x one pair of a transposed read lie on all 64 banks
   auto swz = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int parts = PART ? p.parts_q : 1;
-  const Unit u = unit_of(p, p.B * p.H, (p.Nq + ROWS - 1) / ROWS, parts, true);
+  const Unit u = unit_of(p, p.B * p.H, (p.Nq + kRows - 1) / kRows, parts, true);
   const int b = u.bh / p.H, hd = u.bh - b * p.H, kvh = hd / p.group;
-  const int q0 = u.tile * ROWS, q_last = q0 + ROWS < p.Nq ? q0 + ROWS - 1 : p.Nq - 1;
+  const int q0 = u.tile * kRows, q_last = q0 + kRows < p.Nq ? q0 + kRows - 1 : p.Nq - 1;
   const int keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), k_end = dense_last_key(p, q_last, keys), nqb = (p.Nq + 31) >> 5;
   const int all = (k_end + kStep - 1) / kStep;
   const int i0 = PART ? (int)((long long)all * u.part / parts) : 0, i1 = PART ? (int)((long long)all * (u.part + 1) / parts) : all;
@@ -174,7 +179,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
            (const u16*)p.V + b * p.v.batch + kvh * p.v.head + (long long)kStep * i0 * p.v.token, p.v.token, nullptr,
            i1 - i0, k_end - kStep * i0, wave, lane);
 #pragma unroll
-  for (int j = 0; j < SLOTS - 1; ++j) st.issue(swz);
+  for (int j = 0; j < kSlots - 1; ++j) st.issue(swz);
 
   // the wave's queries
   const u16* Qp = (const u16*)p.Q + b * p.q.batch + hd * p.q.head;
@@ -274,7 +279,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
       }
     }
     // (the ring holds this step, the next one and the one after, which the first reads below are for)
-    wait_and_meet<(SLOTS - 4) * S::PERSTEP>();
+    wait_and_meet<(kSlots - 4) * S::PERSTEP>();
     st.issue(swz);
     const int then = S::after(next), nnt = then + row_at;
 #pragma unroll
@@ -289,7 +294,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
     next = then;
     row += kStep;
   };
-  wait_and_meet<(SLOTS - 3) * S::PERSTEP>();
+  wait_and_meet<(kSlots - 3) * S::PERSTEP>();
   if (i0 < i1) {
     const std::integral_constant<int, 0> even;
     const std::integral_constant<int, 1> odd;
@@ -320,24 +325,22 @@ __global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
 }
 
 // ---- keys --------------------------------------------------------------------------------------
-// One tile of 32 keys a wave.  A step is a vector phase (weights and gradients of the logits) and a matrix phase (what
-// these give to dV^T and dK^T, then the logits and dO V^T of the next step's queries), and the two waves of a SIMD are
-// half a step apart: between two meetings the first half of the workgroup takes its matrix phase, then its vector phase,
-// the second half its vector phase, then its matrix phase.
-
-template <int D, int W, bool PART>
-__global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
-  constexpr int KS = D / 16, FT = D / 32, ROWS = 32 * W, RB = 2 * D, SLOTS = W == 8 ? 5 : 4, AHEAD = 3;
-  using S = Stream<D, W, true, SLOTS>;
+// One tile of 32 keys a wave.  A step is a vector phase (weights and gradients of the logits), which runs beside the
+// matrix phase of the other workgroup's wave on the SIMD, and a matrix phase (what these give to dV^T and dK^T, then the
+// logits and dO V^T of the next step's queries).
+template <int D, bool PART>
+__global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
+  constexpr int KS = D / 16, FT = D / 32, RB = 2 * D, AHEAD = 3;
+  using S = Stream<D, true>;
   // sixteen rows that agree in a piece lie on all 64 banks (those a 16-byte read takes at once: 0-3, 12-15 and 20-27 of a
   // tile, and the other sixteen), and so do four consecutive rows of four pieces (a transposed read).  Rows 8 apart
   // differ in bit 1, rows 16 apart in nothing.
   auto swz = [](int row) { return D == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : (row & 2) << 1 | ((row >> 2) & 3); };
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
   const int parts = PART ? p.parts_kv : 1;
-  const Unit u = unit_of(p, p.B * p.KH, (p.Nkv + ROWS - 1) / ROWS, parts, false);
+  const Unit u = unit_of(p, p.B * p.KH, (p.Nkv + kRows - 1) / kRows, parts, false);
   const int b = u.bh / p.KH, hd = u.bh - b * p.KH;
-  const int k0 = u.tile * ROWS, k_last = k0 + ROWS < p.Nkv ? k0 + ROWS - 1 : p.Nkv - 1;
+  const int k0 = u.tile * kRows, k_last = k0 + kRows < p.Nkv ? k0 + kRows - 1 : p.Nkv - 1;
   const int keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), nqb = (p.Nq + 31) >> 5;
   const int q_first = dense_first_query(p, k0) & ~(kStep - 1);      // of every head that reads these keys
   const int per_head = k0 < keys && q_first < p.Nq ? (p.Nq - q_first + kStep - 1) / kStep : 0, all = per_head * p.group;
@@ -357,7 +360,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
     st.left0 = p.Nq - q_first;
   }
 #pragma unroll
-  for (int j = 0; j < SLOTS - 1; ++j) st.issue(swz);
+  for (int j = 0; j < kSlots - 1; ++j) st.issue(swz);
 
   // the wave's keys
   const int kw = k0 + 32 * wave, key = kw + c;
@@ -441,22 +444,15 @@ __global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
     }
   };
 
-  const bool second = wave >= W / 2;
   int left_steps = per_head - (per_head > 0 ? i0 % per_head : 0);
-  wait_and_meet<(SLOTS - 2) * S::PERSTEP>();
+  wait_and_meet<(kSlots - 2) * S::PERSTEP>();
   if (i0 < i1) matrix(0, 0, NG);
   for (int i = i0, slot = 0; i < i1; ++i) {
     const int next = S::after(slot);
-    if (second) {
-      wait_and_meet<(SLOTS - 3) * S::PERSTEP>();
-      st.issue(swz);
-    }
     soften(row, slot);
     __builtin_amdgcn_sched_barrier(0);
-    if (!second) {
-      wait_and_meet<(SLOTS - 3) * S::PERSTEP>();
-      st.issue(swz);
-    }
+    wait_and_meet<(kSlots - 3) * S::PERSTEP>();
+    st.issue(swz);
     matrix(slot, next, 0);
     slot = next;
     row += kStep;
@@ -488,55 +484,61 @@ __global__ __launch_bounds__(64 * W, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
 }
 
 template <typename Kernel>
-hipError_t launch(Kernel kernel, int rows, int heads, int tile, int parts, int threads, int lds, const DenseBwd& p, hipStream_t s) {
+hipError_t launch(Kernel kernel, int rows, int heads, int parts, int lds, const DenseBwd& p, hipStream_t s) {
   const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  kernel<<<(unsigned)((rows + tile - 1) / tile * (long long)heads * parts), threads, lds, s>>>(p);
+  kernel<<<(unsigned)((rows + kRows - 1) / kRows * (long long)heads * parts), kThreads, lds, s>>>(p);
   return hipGetLastError();
 }
-template <int D, int W>
-hipError_t run_q(const DenseBwd& p, hipStream_t s) {
-  constexpr int lds = Stream<D, W, false, W == 8 ? 6 : 4>::RING;
-  if (p.parts_q == 1) return launch(k_bf16_dense_bwd_q<D, W, false>, p.Nq, p.B * p.H, 32 * W, 1, 64 * W, lds, p, s);
-  const hipError_t e = launch(k_bf16_dense_bwd_q<D, W, true>, p.Nq, p.B * p.H, 32 * W, p.parts_q, 64 * W, lds, p, s);
-  return e != hipSuccess ? e : launch_dense_bwd_join(p, false, MRT_BF16, s);
-}
-template <int D, int W>
-hipError_t run_kv(const DenseBwd& p, hipStream_t s) {
-  constexpr int lds = Stream<D, W, true, W == 8 ? 5 : 4>::RING;
-  if (p.parts_kv == 1) return launch(k_bf16_dense_bwd_kv<D, W, false>, p.Nkv, p.B * p.KH, 32 * W, 1, 64 * W, lds, p, s);
-  const hipError_t e = launch(k_bf16_dense_bwd_kv<D, W, true>, p.Nkv, p.B * p.KH, 32 * W, p.parts_kv, 64 * W, lds, p, s);
+template <int D>
+hipError_t run(const DenseBwd& p, hipStream_t s) {
+  constexpr int lq = Stream<D, false>::RING, lkv = Stream<D, true>::RING;
+  hipError_t e;
+  if (p.parts_q == 1) e = launch(k_bf16_dense_bwd_q<D, false>, p.Nq, p.B * p.H, 1, lq, p, s);
+  else e = launch(k_bf16_dense_bwd_q<D, true>, p.Nq, p.B * p.H, p.parts_q, lq, p, s);
+  if (e == hipSuccess && p.parts_q > 1) e = launch_dense_bwd_join(p, false, MRT_BF16, s);
+  if (e != hipSuccess) return e;
+  if (p.parts_kv == 1) return launch(k_bf16_dense_bwd_kv<D, false>, p.Nkv, p.B * p.KH, 1, lkv, p, s);
+  e = launch(k_bf16_dense_bwd_kv<D, true>, p.Nkv, p.B * p.KH, p.parts_kv, lkv, p, s);
   return e != hipSuccess ? e : launch_dense_bwd_join(p, true, MRT_BF16, s);
 }
 
 }  // namespace
 
-DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
-  DenseBwdShape shape = {256, 1, 256, 1};
-  const long long cus = compute_units(), most = 1 << 27;      // elements of the parts
-  auto parts = [&](long long rows, long long heads, long long tile, long long streamed) {
-    const long long wgs = (rows + tile - 1) / tile * heads, steps = (streamed + 31) / 32;
-    long long n = wgs < cus ? cus / wgs : 1;
-    if (n > steps / 4) n = steps / 4;
-    if (n > most / (rows * heads * p.d)) n = most / (rows * heads * p.d);
-    return (int)(n < 1 ? 1 : n);
+// How many workgroups share the streamed rows of a tile: as many as promise the least time by this model, fitted to 14
+// shapes of 1 to 40 heads, 200 to 10800 tokens.  A step takes t microseconds where a compute unit has one workgroup, 1.5 t
+// where it has two; a join costs a launch and the parts' bytes.  (One head of 4680 tokens: queries 98 -> 14 us and keys
+// 112 -> 12 with 7 parts, of 37 tiles; 5 heads 97 -> 66 and 110 -> 75 with 4; 12 heads, 444 tiles, one part: 3 % less
+// than with two.)
+constexpr long long kMostPartElements = 1 << 27;      // of all parts together
+static int share(long long rows, long long heads, int d, double t, double first, double last, int arrays) {
+  const double cus = compute_units(), longest = std::max(first, last), mean = 0.5 * (first + last);
+  const long long tiles = (rows + kRows - 1) / kRows * heads, elements = rows * heads * d * arrays;
+  auto time = [&](int parts) {
+    const double each = tiles * parts / cus, pairs = floor(each / 2), rest = each - 2 * pairs;
+    const double rounds = 1.5 * pairs + (rest > 1 ? 1.5 : rest > 0 ? 1.0 : 0.0);
+    const double steps = std::max(ceil(longest / parts) * std::min(rounds, 1.5), (mean / parts + 1) * rounds);
+    return steps * t + (parts > 1 ? 5.0 + 8e-6 * elements * parts / 8 : 0.0);
   };
-  shape.parts_q = parts(p.Nq, (long long)p.B * p.H, shape.rows_q, p.Nkv);
-  shape.parts_kv = parts(p.Nkv, (long long)p.B * p.KH, shape.rows_kv, (long long)p.Nq * p.group);
+  int best = 1;
+  double least = time(1) * 0.95;
+  for (int parts = 2; parts <= 32 && 2 * parts <= longest && elements * parts <= kMostPartElements; ++parts) {
+    const double us = time(parts);
+    if (us < least) { least = us; best = parts; }
+  }
+  return best;
+}
+
+DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
+  auto steps = [](long long rows) { return (double)((rows + kStep - 1) / kStep); };
+  auto keys = [&](long long q) { return steps(dense_last_key(p, (int)std::min<long long>(q, p.Nq - 1), p.Nkv)); };
+  auto queries = [&](long long k) { return steps((long long)(p.Nq - dense_first_query(p, (int)std::min<long long>(k, p.Nkv - 1))) * p.group); };
+  DenseBwdShape shape;
+  shape.parts_q = share(p.Nq, (long long)p.B * p.H, p.d, p.d == 64 ? 0.43 : 0.66, keys(kRows - 1), keys(p.Nq - 1), 1);
+  shape.parts_kv = share(p.Nkv, (long long)p.B * p.KH, p.d, p.d == 64 ? 0.51 : 0.78, queries(0), queries((p.Nkv - 1) / kRows * (long long)kRows), 2);
   return shape;
 }
 
-hipError_t launch_bf16_dense_bwd(const DenseBwd& p, const DenseBwdShape& shape, hipStream_t s) {
-  const bool q8 = shape.rows_q == 256, kv8 = shape.rows_kv == 256;
-  hipError_t e;
-  if (p.d == 64) {
-    e = q8 ? run_q<64, 8>(p, s) : run_q<64, 4>(p, s);
-    if (e == hipSuccess) e = kv8 ? run_kv<64, 8>(p, s) : run_kv<64, 4>(p, s);
-  } else {
-    e = q8 ? run_q<128, 8>(p, s) : run_q<128, 4>(p, s);
-    if (e == hipSuccess) e = kv8 ? run_kv<128, 8>(p, s) : run_kv<128, 4>(p, s);
-  }
-  return e;
-}
+hipError_t launch_bf16_dense_bwd(const DenseBwd& p, hipStream_t s) { return p.d == 64 ? run<64>(p, s) : run<128>(p, s); }
 
 }  // namespace mrt

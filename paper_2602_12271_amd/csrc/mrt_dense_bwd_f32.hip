@@ -274,9 +274,12 @@ hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStrea
   return hipGetLastError();
 }
 
-DenseBwdShape f32_dense_bwd_shape(const DenseBwd&) { return {kRows, 1, kRows, 1}; }
+DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p) {
+  DenseBwdShape shape = {1, 1};
+  return shape;
+}
 
-hipError_t launch_f32_dense_bwd(const DenseBwd& p, const DenseBwdShape&, int dtype, hipStream_t s) {
+hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s) {
   return dtype == MRT_F32 ? run_t<float>(p, dtype, s) : run_t<u16>(p, dtype, s);
 }
 

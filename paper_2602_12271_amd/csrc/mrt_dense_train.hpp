@@ -46,14 +46,14 @@ __host__ __device__ inline int dense_first_query(const DenseBwd& p, int k) {
   return q <= 0 ? 0 : q < p.Nq ? (int)q : p.Nq;
 }
 
-// Rows, workgroups per row tile and parts of one launch.
+// Workgroups that share the keys of a query tile, and the queries of a key tile.
 struct DenseBwdShape {
-  int rows_q, parts_q, rows_kv, parts_kv;
+  int parts_q, parts_kv;
 };
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p);
-hipError_t launch_bf16_dense_bwd(const DenseBwd& p, const DenseBwdShape& shape, hipStream_t s);
+hipError_t launch_bf16_dense_bwd(const DenseBwd& p, hipStream_t s);
 DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p);
-hipError_t launch_f32_dense_bwd(const DenseBwd& p, const DenseBwdShape& shape, int dtype, hipStream_t s);
+hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s);
 // sums the parts of dQ, or of dK and dV, into the gradients (`dtype`)
 hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStream_t s);
 
