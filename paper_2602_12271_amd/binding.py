@@ -429,31 +429,20 @@ def _require(ok, text, status=MRT_ERR_SHAPE):
         raise MrtError(status, text)
 
 
-class _on:
-    """Q's device and the call's stream as torch's current ones while a call allocates and launches: memory taken
-    from torch is then ordered by the stream that uses it.  Does nothing where they are current already."""
-
-    def __init__(self, Q, stream):
-        import torch
-        self.stream, self.device, self.inner = _stream_of(Q, stream), None, None
-        if Q.device.index != torch.cuda.current_device():
-            self.device = torch.cuda.device(Q.device)
-        if self.stream != _stream_of(Q, None):
-            self.inner = torch.cuda.stream(torch.cuda.ExternalStream(self.stream, Q.device) if self.stream
-                                           else torch.cuda.default_stream(Q.device))
-
-    def __enter__(self):
-        if self.device is not None:
-            self.device.__enter__()
-        if self.inner is not None:
-            self.inner.__enter__()
-        return self.stream
-
-    def __exit__(self, *error):
-        if self.inner is not None:
-            self.inner.__exit__(*error)
-        if self.device is not None:
-            self.device.__exit__(*error)
+def _run_on(Q, stream, call):
+    """call(stream) with Q's device and the call's stream as torch's current ones: memory that it takes from torch is
+    then ordered by the stream that uses it."""
+    import torch
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    same_device = Q.get_device() == (get() if get is not None else torch.cuda.current_device())
+    s = _stream_of(Q, None)
+    if same_device and (stream is None or stream == s):
+        return call(s)
+    with torch.cuda.device(Q.device):
+        if stream is None:
+            return call(_stream_of(Q, None))
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, Q.device) if stream else torch.cuda.default_stream(Q.device)):
+            return call(stream)
 
 
 def _dtype_of(x, name):
@@ -462,19 +451,20 @@ def _dtype_of(x, name):
     return MRT_F32 if x.dtype == torch.float32 else MRT_BF16
 
 
-def _same_device(first, **others):
+def _same_device(first, *others):
     _require(first.is_cuda, "tensors must be on a GPU")
-    for name, x in others.items():
-        _require(x.device == first.device, f"{name} is on {x.device}, not on {first.device}")
+    at = first.get_device()
+    for x in others:
+        _require(x is None or (x.is_cuda and x.get_device() == at), "tensors are on different devices")
 
 
-# (problem, training description without kv_len) of recent calls by their values, like _problems
+# (problem, training description without kv_len, backward scratch) of recent calls by their values, like _problems
 _train_problems: dict = {}
 
 
 def _train_problem(Q, K, V, O, grads, f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute):
-    key = (Q.shape, K.shape, V.shape, Q.dtype, Q.stride(), K.stride(), V.stride(), O.stride(),
-           tuple([g.stride() for g in grads]), f_q, f_kv, h, w, q_frame_offset, scale, compute)
+    key = (Q.shape, K.shape, V.shape, O.shape, Q.dtype, K.dtype, V.dtype, O.dtype, Q.stride(), K.stride(), V.stride(), O.stride(),
+           tuple([(g.shape, g.dtype, g.stride()) for g in grads]), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute)
     found = _train_problems.get(key)
     if found is not None:
         return found
@@ -483,7 +473,10 @@ def _train_problem(Q, K, V, O, grads, f_q, f_kv, h, w, causal_chunk, q_frame_off
     _require(nq == f_q * h * w, f"Q has {nq} tokens, the grid {f_q * h * w}")
     _require(K.shape[0] == B and K.shape[2] == f_kv * h * w and K.shape[3] == d,
              f"K and V are [{B}, heads, {f_kv * h * w}, {d}], got {tuple(K.shape)}")
+    for x, like in zip((O, *grads), (Q, Q, Q, K, V)):
+        _require(x.shape == like.shape, "O, dO and the gradients have the shapes of Q, K and V")
     for x in (Q, K, V, O, *grads):
+        _require(x.dtype == Q.dtype, "all tensors have one type")
         _require(x.stride(3) == 1, "head_dim must be contiguous")
 
     def st(x):
@@ -492,19 +485,30 @@ def _train_problem(Q, K, V, O, grads, f_q, f_kv, h, w, causal_chunk, q_frame_off
                         dtype=_dtype_of(Q, "Q"), compute=compute, scale=scale, q_strides=st(Q), k_strides=st(K),
                         v_strides=st(V), o_strides=st(O))
     train = MrtDenseTrain(K.shape[1], None, *[MrtStrides(*st(x)) for x in grads])
+    scratch = 0
+    if grads:
+        scratch = dense_attn_bwd_workspace_bytes(prob, train, causal_chunk)
+        if scratch == 0:
+            lib = load_library()
+            _raise(lib, lib.dense_attn_bwd_check(ctypes.byref(prob), ctypes.byref(train), causal_chunk))
     if len(_train_problems) >= _MAX_PROBLEMS:
         _train_problems.clear()
-    _train_problems[key] = prob, train
-    return prob, train
+    _train_problems[key] = found = prob, train, scratch
+    return found
 
 
 def _with_lengths(train, kv_len, batch):
     if kv_len is None:
         return train
     import torch
-    _require(kv_len.dtype == torch.int32 and kv_len.shape == (batch,) and kv_len.stride(0) == 1,
-             f"kv_len: int32 [{batch}], contiguous")
+    _require(kv_len.dtype == torch.int32 and kv_len.shape == (batch,) and kv_len.is_contiguous(), f"kv_len: int32 [{batch}], contiguous")
     return MrtDenseTrain(train.kv_heads, kv_len.data_ptr(), train.dout, train.dq, train.dk, train.dv)
+
+
+def _require_lse(lse, Q):
+    import torch
+    _require(lse.shape == Q.shape[:3] and lse.dtype == torch.float32 and lse.is_contiguous(),
+             "lse is fp32 [batch, heads, tokens], contiguous")
 
 
 def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0, kv_len=None,
@@ -517,26 +521,22 @@ def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_off
     those of dense_attn_fwd, scratch memory (`workspace`) and what it decides included."""
     import torch
     lib = load_library()
-    _same_device(Q, K=K, V=V, **{n: x for n, x in (("out", out), ("lse", lse), ("kv_len", kv_len), ("workspace", workspace))
-                                 if x is not None})
-    _require(Q.dtype == K.dtype == V.dtype, "Q, K and V have one type")
-    with _on(Q, stream) as s:
+    _same_device(Q, K, V, out, lse, kv_len, workspace)
+
+    def call(s):
         O = torch.empty_like(Q) if out is None else out
-        _require(O.shape == Q.shape and O.dtype == Q.dtype, "out has the shape and type of Q")
-        prob, train = _train_problem(Q, K, V, O, (), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute)
-        if lse is None:
-            lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
-        _require(lse.shape == Q.shape[:3] and lse.dtype == torch.float32 and lse.is_contiguous(),
-                 "lse is fp32 [batch, heads, tokens], contiguous")
+        prob, train, _ = _train_problem(Q, K, V, O, (), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute)
+        stats = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if lse is None else lse
+        _require_lse(stats, Q)
         train = _with_lengths(train, kv_len, Q.shape[0])
-        if workspace is None:
-            workspace = _dense_scratch(prob, causal_chunk, Q, s)
-        ws, nbytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-        st = lib.dense_attn_fwd_save(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(),
+        scratch = _dense_scratch(prob, causal_chunk, Q, s) if workspace is None else workspace
+        ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
+        st = lib.dense_attn_fwd_save(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), stats.data_ptr(),
                                      ctypes.byref(prob), ctypes.byref(train), causal_chunk, ws, nbytes, s)
-    if st != MRT_OK:
-        _raise(lib, st)
-    return O, lse
+        if st != MRT_OK:
+            _raise(lib, st)
+        return O, stats
+    return _run_on(Q, stream, call)
 
 
 def dense_attn_bwd_workspace_bytes(prob: MrtProblem, train: MrtDenseTrain, causal_chunk=0) -> int:
@@ -551,34 +551,22 @@ def dense_attn_bwd(Q, K, V, O, dO, lse, *, f_q, f_kv, h, w, causal_chunk=0, q_fr
     out: (dQ, dK, dV) to write.  workspace: scratch of dense_attn_bwd_workspace_bytes() bytes (torch's by default)."""
     import torch
     lib = load_library()
-    _same_device(Q, K=K, V=V, O=O, dO=dO, lse=lse,
-                 **{n: x for n, x in (("kv_len", kv_len), ("workspace", workspace)) if x is not None})
-    _require(Q.dtype == K.dtype == V.dtype == O.dtype == dO.dtype, "Q, K, V, O and dO have one type")
-    _require(O.shape == Q.shape and dO.shape == Q.shape, "O and dO have the shape of Q")
-    _require(lse.shape == Q.shape[:3] and lse.dtype == torch.float32 and lse.is_contiguous(),
-             "lse is fp32 [batch, heads, tokens], contiguous")
-    with _on(Q, stream) as s:
+    _same_device(Q, K, V, O, dO, lse, kv_len, workspace, *(out or ()))
+    _require_lse(lse, Q)
+
+    def call(s):
         dQ, dK, dV = out if out is not None else (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V))
-        _same_device(Q, dQ=dQ, dK=dK, dV=dV)
-        _require(dQ.shape == Q.shape and dK.shape == K.shape and dV.shape == V.shape and
-                 dQ.dtype == dK.dtype == dV.dtype == Q.dtype, "gradients have the shapes and the type of Q, K and V")
-        prob, train = _train_problem(Q, K, V, O, (dO, dQ, dK, dV), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale,
-                                     compute)
-        train_now = _with_lengths(train, kv_len, Q.shape[0])
-        if workspace is None:
-            known = prob.__dict__.setdefault("dense_bwd_bytes", {})
-            nbytes = known.get(causal_chunk)
-            if nbytes is None:
-                nbytes = known[causal_chunk] = dense_attn_bwd_workspace_bytes(prob, train, causal_chunk)
-            if nbytes == 0:
-                _raise(lib, lib.dense_attn_bwd_check(ctypes.byref(prob), ctypes.byref(train), causal_chunk))
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
+        prob, train, nbytes = _train_problem(Q, K, V, O, (dO, dQ, dK, dV), f_q, f_kv, h, w, causal_chunk, q_frame_offset,
+                                             scale, compute)
+        train = _with_lengths(train, kv_len, Q.shape[0])
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if workspace is None else workspace
         st = lib.dense_attn_bwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), dO.data_ptr(), lse.data_ptr(),
-                                dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ctypes.byref(prob), ctypes.byref(train_now),
-                                causal_chunk, workspace.data_ptr(), workspace.numel() * workspace.element_size(), s)
-    if st != MRT_OK:
-        _raise(lib, st)
-    return dQ, dK, dV
+                                dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ctypes.byref(prob), ctypes.byref(train),
+                                causal_chunk, scratch.data_ptr(), scratch.numel() * scratch.element_size(), s)
+        if st != MRT_OK:
+            _raise(lib, st)
+        return dQ, dK, dV
+    return _run_on(Q, stream, call)
 
 
 def rotary_pairs_split(head_dim: int):
@@ -596,7 +584,7 @@ def _rotary_tensor(x, y, f, h, w, offset, positions, name):
         _require(positions.dtype == torch.int32 and positions.shape in ((3, n), (B, 3, n)) and (n == 1 or positions.stride(-1) == 1),
                  f"{name}: positions are int32 [3, {n}] or [{B}, 3, {n}]")
         f, h, w, offset = 1, 1, n, 0
-        pos = positions.data_ptr(), positions.stride(0) if positions.dim() == 3 else 0, positions.stride(-2)
+        pos = None, positions.stride(0) if positions.dim() == 3 else 0, positions.stride(-2)
     else:
         _require(f is not None and h is not None and w is not None, f"{name}: neither a grid nor positions")
         _require(n == f * h * w, f"{name} has {n} tokens, its grid {f * h * w}")
@@ -605,32 +593,55 @@ def _rotary_tensor(x, y, f, h, w, offset, positions, name):
                            _dtype_of(x, name), _dtype_of(y, name), *pos)
 
 
+def _layout_of(x):
+    return None if x is None else (x.shape, x.stride(), x.dtype)
+
+
+# (description, tensors without their positions) of recent calls by their values, like _problems
+_rotary_problems: dict = {}
+
+
 def _rotary(entry, Q, K, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder, q_positions,
             k_positions, dtype, out, k_out, stream):
     import torch
     lib = load_library()
-    _same_device(Q, **{n: x for n, x in (("K", K), ("q_positions", q_positions), ("k_positions", k_positions), ("out", out),
-                                         ("k_out", k_out)) if x is not None})
-    _require(layout in ROTARY_LAYOUTS, f"layout is one of {sorted(ROTARY_LAYOUTS)}")
-    _require(ladder in ROTARY_LADDERS, f"ladder is one of {sorted(ROTARY_LADDERS)}")
-    split = tuple(rotary_pairs_split(Q.shape[-1]) if split is None else split)
-    _require(len(split) == 3, "split: rotary pairs of the frame, height and width axis")
-    r = MrtRotary(Q.shape[-1], (ctypes.c_int * 3)(*split), ROTARY_LAYOUTS[layout], ROTARY_LADDERS[ladder], theta)
-    with _on(Q, stream) as s:
-        Y = torch.empty_like(Q, dtype=dtype) if out is None else out
-        tensors, x, y = [_rotary_tensor(Q, Y, f_q, h, w, q_frame_offset, q_positions, "Q")], [Q], [Y]
+    _same_device(Q, K, q_positions, k_positions, out, k_out)
+
+    def call(s):
+        y = [torch.empty_like(Q, dtype=dtype) if out is None else out]
+        x, n = [Q], 1
         if K is not None:
-            _require(K.shape[-1] == Q.shape[-1], "Q and K have one head_dim")
             y.append(torch.empty_like(K, dtype=dtype) if k_out is None else k_out)
-            x.append(K)
-            tensors.append(_rotary_tensor(K, y[1], f_q if f_kv is None else f_kv, h, w, kv_frame_offset, k_positions, "K"))
-        n = len(x)
-        pointers = ctypes.c_void_p * n
-        st = getattr(lib, entry)(ctypes.byref(r), (MrtRotaryTensor * n)(*tensors), n, pointers(*[t.data_ptr() for t in x]),
+            x, n = [Q, K], 2
+        key = (Q.shape, Q.stride(), Q.dtype, _layout_of(y[0]), _layout_of(K), _layout_of(y[-1]), _layout_of(q_positions),
+               _layout_of(k_positions), f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta,
+               None if split is None else tuple(split), layout, ladder)
+        found = _rotary_problems.get(key)
+        if found is None:
+            _require(layout in ROTARY_LAYOUTS, f"layout is one of {sorted(ROTARY_LAYOUTS)}")
+            _require(ladder in ROTARY_LADDERS, f"ladder is one of {sorted(ROTARY_LADDERS)}")
+            pairs = tuple(rotary_pairs_split(Q.shape[-1]) if split is None else split)
+            _require(len(pairs) == 3, "split: rotary pairs of the frame, height and width axis")
+            r = MrtRotary(Q.shape[-1], (ctypes.c_int * 3)(*pairs), ROTARY_LAYOUTS[layout], ROTARY_LADDERS[ladder], theta)
+            tensors = [_rotary_tensor(Q, y[0], f_q, h, w, q_frame_offset, q_positions, "Q")]
+            if K is not None:
+                _require(K.shape[-1] == Q.shape[-1], "Q and K have one head_dim")
+                tensors.append(_rotary_tensor(K, y[1], f_q if f_kv is None else f_kv, h, w, kv_frame_offset, k_positions, "K"))
+            found = r, (MrtRotaryTensor * n)(*tensors), ctypes.c_void_p * n
+            if len(_rotary_problems) >= _MAX_PROBLEMS:
+                _rotary_problems.clear()
+            _rotary_problems[key] = found
+        r, tensors, pointers = found
+        if q_positions is not None or k_positions is not None:     # (a description that is shared is not written)
+            tensors = type(tensors).from_buffer_copy(tensors)
+            for t, pos in zip(tensors, (q_positions, k_positions)):
+                t.positions = None if pos is None else pos.data_ptr()
+        st = getattr(lib, entry)(ctypes.byref(r), tensors, n, pointers(*[t.data_ptr() for t in x]),
                                  pointers(*[t.data_ptr() for t in y]), s)
-    if st != MRT_OK:
-        _raise(lib, st)
-    return tuple(y) if n > 1 else y[0]
+        if st != MRT_OK:
+            _raise(lib, st)
+        return tuple(y) if n > 1 else y[0]
+    return _run_on(Q, stream, call)
 
 
 def rotary_fwd(Q, K=None, *, f_q=None, f_kv=None, h=None, w=None, q_frame_offset=0, kv_frame_offset=0, theta=10000.0,

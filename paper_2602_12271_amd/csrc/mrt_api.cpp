@@ -950,7 +950,7 @@ static DenseBwdWorkspace dense_bwd_workspace(const DenseBwd& d, bool f32) {
   DenseBwdWorkspace w;
   w.shape = f32 ? f32_dense_bwd_shape(d) : bf16_dense_bwd_shape(d);
   w.stats = round256((size_t)d.B * d.H * ((d.Nq + 31) / 32) * 64 * sizeof(float));
-  const size_t q = w.shape.parts_q > 1 ? (size_t)w.shape.parts_q * d.B * d.H * d.Nq * d.d * sizeof(float) : 0;
+  const size_t q = w.shape.sums_q ? (size_t)w.shape.parts_q * d.B * d.H * d.Nq * d.d * sizeof(float) : 0;
   const size_t kv = w.shape.parts_kv > 1 ? 2 * (size_t)w.shape.parts_kv * d.B * d.KH * d.Nkv * d.d * sizeof(float) : 0;
   w.parts = w.stats;
   w.bytes = w.stats + round256(q > kv ? q : kv);

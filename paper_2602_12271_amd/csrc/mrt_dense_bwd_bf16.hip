@@ -23,8 +23,6 @@
 #include "mrt_dense_train.hpp"
 #include "mrt_bf16_tiles.hpp"
 
-#include <algorithm>
-#include <cmath>
 
 namespace mrt {
 
@@ -483,6 +481,207 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
     }
 }
 
+// ---- few queries -------------------------------------------------------------------------------
+// Up to 32 rows (the queries of all heads that share a head of keys): one launch reads every key and value once and
+// forms all three gradients; memory bounds it.  A wave takes every fourth tile of 32 keys of the workgroup's run, loaded
+// into its own part of LDS a tile ahead, with no meeting of waves.  The operands of S = Q K^T in the other order give S^T,
+// whose gradients are as they stand the operand of dQ^T += K^T dS^T: sixteen products more, but nothing is moved.  dK
+// and dV go through LDS to be stored as whole rows; dQ is summed over the waves, then over the parts.
+template <int D>
+struct Few {
+  static constexpr int TILE = kTileBytes<D>, WAVE = 4 * TILE, ROWS_AT = kWaves * WAVE, STATS_AT = ROWS_AT + 2 * TILE;
+  static constexpr int BYTES = STATS_AT + 3 * 32 * 4;      // two slots of keys and values a wave; Q, dO; -log2(e) lse, -delta, limits
+};
+
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_bf16_dense_bwd_few(DenseBwd p) {
+  constexpr int KS = D / 16, FT = D / 32, RB = 2 * D, PIECES = D / 8, TILE = kTileBytes<D>, LOADS = TILE / 1024;
+  using L = Few<D>;
+  auto swz = [](int row) { return D == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : (row & 2) << 1 | ((row >> 2) & 3); };
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
+  const int parts = p.parts_q, unit = blockIdx.x, part = unit % parts, kh = unit / parts, b = kh / p.KH, hd = kh - b * p.KH;
+  const int rows = p.group * p.Nq, keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), tiles = (p.Nkv + 31) >> 5;
+  const int t0 = (int)((long long)tiles * part / parts), t1 = (int)((long long)tiles * (part + 1) / parts);
+  const u16* Kp = (const u16*)p.K + b * p.k.batch + hd * p.k.head;
+  const u16* Vp = (const u16*)p.V + b * p.v.batch + hd * p.v.head;
+  const unsigned krow = (unsigned)p.k.token * 2u, vrow = (unsigned)p.v.token * 2u, lds0 = (unsigned)(unsigned long long)(const lds_void*)bwd_lds;
+  const int mine = wave * L::WAVE;      // this wave's part of LDS
+
+  // (keys behind the sequence's end are zeros)
+  auto fetch = [&](int tile, int slot) {
+    const int left = tile < t1 ? keys - 32 * tile : 0;
+    const unsigned n = left <= 0 ? 0 : left < 32 ? left : 32;
+    const u32x4 rk = rows_at(Kp + (long long)32 * tile * p.k.token, n ? (n - 1) * krow + RB : 0);
+    const u32x4 rv = rows_at(Vp + (long long)32 * tile * p.v.token, n ? (n - 1) * vrow + RB : 0);
+    const unsigned at = __builtin_amdgcn_readfirstlane(lds0 + mine + slot * 2 * TILE);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int s = j * 64 + lane, row = s / PIECES, piece = (s % PIECES) ^ swz(row);
+      load_lds_16B(rk, at + j * 1024, row * krow + piece * 16);
+      load_lds_16B(rv, at + TILE + j * 1024, row * vrow + piece * 16);
+    }
+  };
+  fetch(t0 + wave, 0);
+
+  // the rows: row r is query r % Nq of head r / Nq of those that share the keys
+  int* const lims = (int*)(bwd_lds + L::STATS_AT) + 64;
+  float* const stats = (float*)(bwd_lds + L::STATS_AT);
+  {
+    constexpr int PER = 32 * PIECES / kThreads;         // pieces of an array a thread moves, all of one row
+    const int r = tid / (PIECES / PER), piece0 = tid % (PIECES / PER) * PER;
+    const bool in = r < rows;
+    const int gh = in ? r / p.Nq : 0, q = in ? r - gh * p.Nq : 0, hq = hd * p.group + gh;
+    const u16* Qp = (const u16*)p.Q + b * p.q.batch + hq * p.q.head + q * p.q.token;
+    const u16* dOp = (const u16*)p.dO + b * p.dout.batch + hq * p.dout.head + q * p.dout.token;
+    const u16* Op = (const u16*)p.O + b * p.o.batch + hq * p.o.head + q * p.o.token;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int piece = piece0 + j;
+      bf16x8 x = ld_global_16B(Qp + 8 * piece), y = ld_global_16B(dOp + 8 * piece);
+      const bf16x8 o = ld_global_16B(Op + 8 * piece);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf((float)o[e], (float)y[e], sum);
+      if (!in) x = y = bf16x8{};
+      char* to = bwd_lds + L::ROWS_AT + r * RB + (piece ^ swz(r)) * 16;
+      *(bf16x8*)to = x;
+      *(bf16x8*)(to + TILE) = y;
+    }
+    sum = row8_sum(sum);                                 // (eight threads to a row)
+    static_assert(PIECES / PER == 8, "");
+    if ((tid & 7) == 0) {
+      const float l = p.lse[((long long)b * p.H + hq) * p.Nq + q];
+      stats[r] = !in || l == -INFINITY ? -INFINITY : -kLog2e * l;
+      stats[32 + r] = in ? -sum : 0.f;
+      lims[r] = in ? dense_last_key(p, q, keys) : 0;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  fetch(t0 + wave + kWaves, 1);
+
+  const float scale2 = p.scale * kLog2e, nlq = stats[c], ndq = stats[32 + c];
+  const int limq = lims[c], free_keys = dense_last_key(p, 0, keys);     // (the limits rise with the query)
+  const int G = lane >> 4, s = lane & 15, trow = 4 * hi + (s >> 2);
+  const int row_at = c * RB + (swz(c) ^ hi) * 16, tr_at = trow * RB + ((2 * (G & 1) + ((s >> 1) & 1)) ^ swz(trow)) * 16 + 8 * (s & 1);
+  auto row_op = [&](int at, int ks) { return *(const bf16x8*)(bwd_lds + at + (row_at ^ (32 * ks))); };
+  auto tr_op = [&](int at, int f, int kk) {
+    const char* lo = bwd_lds + at + (tr_at ^ (64 * f)) + 16 * kk * RB;
+    const char* up = bwd_lds + at + (tr_at ^ (64 * f + 32)) + (16 * kk + 8) * RB;
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(ld_lds_tr((const u16*)lo), ld_lds_tr((const u16*)up), 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  f32x16 dq[FT];
+#pragma unroll
+  for (int f = 0; f < FT; ++f) dq[f] = f32x16{};
+
+  for (int tile = t0 + wave, slot = 0; tile < t1; tile += kWaves, slot ^= 1) {
+    const int kt = mine + slot * 2 * TILE, vt = kt + TILE, key0 = 32 * tile, key = key0 + c;
+    const bool edge = key0 + 32 > free_keys;
+    f32x16 sv = {}, dp, st = {}, dt;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 x = *(const f32x4*)(stats + 32 + 8 * j + 4 * hi);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) { dp[4 * j + r] = x[r]; dt[4 * j + r] = ndq; }
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 k = row_op(kt, ks), v = row_op(vt, ks), q = row_op(L::ROWS_AT, ks), d = row_op(L::ROWS_AT + TILE, ks);
+      sv = mfma32(q, k, sv);
+      dp = mfma32(d, v, dp);
+      st = mfma32(k, q, st);
+      dt = mfma32(v, d, dt);
+    }
+    bf16x8 pb[2], db[2], dbt[2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 nl = *(const f32x4*)(stats + 8 * j + 4 * hi);
+      const int* lr = lims + 8 * j + 4 * hi;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int e = 4 * j + r;
+        float w = exp2_fast(fmaf(sv[e], scale2, nl[r])), wt = exp2_fast(fmaf(st[e], scale2, nlq));
+        float d = w * dp[e], g = wt * dt[e];
+        if (edge) {
+          if (key >= lr[r]) w = d = 0.f;
+          if (key0 + 8 * j + 4 * hi + r >= limq) g = 0.f;
+        }
+        pb[e >> 3][e & 7] = (__bf16)w;
+        db[e >> 3][e & 7] = (__bf16)d;
+        dbt[e >> 3][e & 7] = (__bf16)g;
+      }
+    }
+    f32x16 dv[FT], dk[FT];
+#pragma unroll
+    for (int f = 0; f < FT; ++f) {
+      dv[f] = dk[f] = f32x16{};
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        dv[f] = mfma32(tr_op(L::ROWS_AT + TILE, f, kk), pb[kk], dv[f]);
+        dk[f] = mfma32(tr_op(L::ROWS_AT, f, kk), db[kk], dk[f]);
+        dq[f] = mfma32(tr_op(kt, f, kk), dbt[kk], dq[f]);
+      }
+    }
+    // dK in the place of K, dV in that of V, then row by row to memory
+    const bool live = key < keys;
+#pragma unroll
+    for (int f = 0; f < FT; ++f)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        char* to = bwd_lds + c * RB + (((4 * f + j) ^ swz(c)) * 16) + 8 * hi;
+        f32x4 x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = live ? dk[f][4 * j + e] * p.scale : 0.f;
+          y[e] = live ? dv[f][4 * j + e] : 0.f;
+        }
+        *(bf16x4*)(to + kt) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+        *(bf16x4*)(to + vt) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+      }
+    u32x4 ok[LOADS], ov[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      ok[j] = *(const u32x4*)(bwd_lds + kt + j * 1024 + lane * 16);
+      ov[j] = *(const u32x4*)(bwd_lds + vt + j * 1024 + lane * 16);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");    // the next tile is here, and the last one's rows are written
+    u16* tk = (u16*)p.dK + b * p.dk.batch + hd * p.dk.head;
+    u16* tv = (u16*)p.dV + b * p.dv.batch + hd * p.dv.head;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int q = j * 64 + lane, row = q / PIECES, piece = (q % PIECES) ^ swz(row);
+      const long long r = key0 + row;
+      if (r < p.Nkv) {
+        *(u32x4*)(tk + r * p.dk.token + 8 * piece) = ok[j];
+        *(u32x4*)(tv + r * p.dv.token + 8 * piece) = ov[j];
+      }
+    }
+    fetch(tile + 2 * kWaves, slot);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing is on its way to LDS
+  __syncthreads();
+  // dQ over the waves: [wave][row][D + 4] floats
+  constexpr int LD = D + 4;
+  static_assert(kWaves * 32 * LD * 4 <= L::ROWS_AT, "fits the tiles' place");
+  float* sums = (float*)bwd_lds;
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(f32x4*)(sums + (wave * 32 + c) * LD + 32 * f + 8 * j + 4 * hi) = f32x4{dq[f][4 * j], dq[f][4 * j + 1], dq[f][4 * j + 2], dq[f][4 * j + 3]};
+  __syncthreads();
+  for (int i = tid; i < rows * (D / 4); i += kThreads) {
+    const int r = i / (D / 4), f = 4 * (i % (D / 4)), gh = r / p.Nq;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) x = x + *(const f32x4*)(sums + (w * 32 + r) * LD + f);
+    const long long bh = (long long)b * p.H + hd * p.group + gh;
+    *(f32x4*)(p.pq + (((long long)part * p.B * p.H + bh) * p.Nq + (r - gh * p.Nq)) * D + f) = x * p.scale;
+  }
+}
+
+bool few_queries(const DenseBwd& p) { return (long long)p.group * p.Nq <= 32; }
+
 template <typename Kernel>
 hipError_t launch(Kernel kernel, int rows, int heads, int parts, int lds, const DenseBwd& p, hipStream_t s) {
   const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -492,8 +691,16 @@ hipError_t launch(Kernel kernel, int rows, int heads, int parts, int lds, const 
 }
 template <int D>
 hipError_t run(const DenseBwd& p, hipStream_t s) {
-  constexpr int lq = Stream<D, false>::RING, lkv = Stream<D, true>::RING;
   hipError_t e;
+  if (few_queries(p)) {
+    constexpr int lds = Few<D>::BYTES;
+    e = hipFuncSetAttribute((const void*)k_bf16_dense_bwd_few<D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    k_bf16_dense_bwd_few<D><<<(unsigned)(p.B * p.KH * p.parts_q), kThreads, lds, s>>>(p);
+    e = hipGetLastError();
+    return e != hipSuccess ? e : launch_dense_bwd_join(p, false, MRT_BF16, s);
+  }
+  constexpr int lq = Stream<D, false>::RING, lkv = Stream<D, true>::RING;
   if (p.parts_q == 1) e = launch(k_bf16_dense_bwd_q<D, false>, p.Nq, p.B * p.H, 1, lq, p, s);
   else e = launch(k_bf16_dense_bwd_q<D, true>, p.Nq, p.B * p.H, p.parts_q, lq, p, s);
   if (e == hipSuccess && p.parts_q > 1) e = launch_dense_bwd_join(p, false, MRT_BF16, s);
@@ -505,38 +712,19 @@ hipError_t run(const DenseBwd& p, hipStream_t s) {
 
 }  // namespace
 
-// How many workgroups share the streamed rows of a tile: as many as promise the least time by this model, fitted to 14
-// shapes of 1 to 40 heads, 200 to 10800 tokens.  A step takes t microseconds where a compute unit has one workgroup, 1.5 t
-// where it has two; a join costs a launch and the parts' bytes.  (One head of 4680 tokens: queries 98 -> 14 us and keys
-// 112 -> 12 with 7 parts, of 37 tiles; 5 heads 97 -> 66 and 110 -> 75 with 4; 12 heads, 444 tiles, one part: 3 % less
-// than with two.)
-constexpr long long kMostPartElements = 1 << 27;      // of all parts together
-static int share(long long rows, long long heads, int d, double t, double first, double last, int arrays) {
-  const double cus = compute_units(), longest = std::max(first, last), mean = 0.5 * (first + last);
-  const long long tiles = (rows + kRows - 1) / kRows * heads, elements = rows * heads * d * arrays;
-  auto time = [&](int parts) {
-    const double each = tiles * parts / cus, pairs = floor(each / 2), rest = each - 2 * pairs;
-    const double rounds = 1.5 * pairs + (rest > 1 ? 1.5 : rest > 0 ? 1.0 : 0.0);
-    const double steps = std::max(ceil(longest / parts) * std::min(rounds, 1.5), (mean / parts + 1) * rounds);
-    return steps * t + (parts > 1 ? 5.0 + 8e-6 * elements * parts / 8 : 0.0);
-  };
-  int best = 1;
-  double least = time(1) * 0.95;
-  for (int parts = 2; parts <= 32 && 2 * parts <= longest && elements * parts <= kMostPartElements; ++parts) {
-    const double us = time(parts);
-    if (us < least) { least = us; best = parts; }
-  }
-  return best;
-}
-
+// (steps fitted to 14 shapes of 1 to 40 heads, 200 to 10800 tokens: one head of 4680 tokens, 37 tiles, queries 98 -> 14 us
+// and keys 112 -> 12 with 7 parts; 5 heads 97 -> 66 and 110 -> 75 with 4; 12 heads one part, 3 % less than with two)
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
-  auto steps = [](long long rows) { return (double)((rows + kStep - 1) / kStep); };
-  auto keys = [&](long long q) { return steps(dense_last_key(p, (int)std::min<long long>(q, p.Nq - 1), p.Nkv)); };
-  auto queries = [&](long long k) { return steps((long long)(p.Nq - dense_first_query(p, (int)std::min<long long>(k, p.Nkv - 1))) * p.group); };
-  DenseBwdShape shape;
-  shape.parts_q = share(p.Nq, (long long)p.B * p.H, p.d, p.d == 64 ? 0.43 : 0.66, keys(kRows - 1), keys(p.Nq - 1), 1);
-  shape.parts_kv = share(p.Nkv, (long long)p.B * p.KH, p.d, p.d == 64 ? 0.51 : 0.78, queries(0), queries((p.Nkv - 1) / kRows * (long long)kRows), 2);
-  return shape;
+  if (!few_queries(p)) return dense_bwd_shape(p, kRows, kStep, p.d == 64 ? 0.43 : 0.66, p.d == 64 ? 0.51 : 0.78);
+  // few queries: runs of key tiles that fill the chip in whole rounds (a round costs a workgroup as much as half a tile)
+  const long long cus = compute_units(), heads = (long long)p.B * p.KH, tiles = (p.Nkv + 31) / 32;
+  double least = INFINITY;
+  int best = 1;
+  for (int parts = 1; parts <= 64 && parts <= tiles; ++parts) {
+    const double cost = (double)((heads * parts + cus - 1) / cus) * ((double)((tiles + 4 * parts - 1) / (4 * parts)) + 0.5);
+    if (cost < least) { least = cost; best = parts; }
+  }
+  return {best, 1, true};
 }
 
 hipError_t launch_bf16_dense_bwd(const DenseBwd& p, hipStream_t s) { return p.d == 64 ? run<64>(p, s) : run<128>(p, s); }

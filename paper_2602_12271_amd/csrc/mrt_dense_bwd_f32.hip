@@ -9,7 +9,6 @@
 #include "mrt_dense_train.hpp"
 #include "mrt_f32_rows.hpp"
 
-#include <algorithm>
 
 namespace mrt {
 
@@ -274,9 +273,9 @@ hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStrea
   return hipGetLastError();
 }
 
+// (one head of 576 tokens of 64 features 109 -> 48 us for both launches, 12 heads of 1560 of 128 790 -> 600)
 DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p) {
-  DenseBwdShape shape = {1, 1};
-  return shape;
+  return dense_bwd_shape(p, kRows, kStep, p.d <= 64 ? 1.1 : 2.1, p.d <= 64 ? 1.5 : 2.8);
 }
 
 hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s) {

@@ -2,6 +2,9 @@
 #pragma once
 #include "mrt_internal.hpp"
 
+#include <algorithm>
+#include <cmath>
+
 namespace mrt {
 
 // Geometry of one backward call, by value to every kernel.
@@ -49,7 +52,41 @@ __host__ __device__ inline int dense_first_query(const DenseBwd& p, int k) {
 // Workgroups that share the keys of a query tile, and the queries of a key tile.
 struct DenseBwdShape {
   int parts_q, parts_kv;
+  bool sums_q;           // dQ is summed from parts, even from one
 };
+
+// How many workgroups share the streamed rows of a tile: as many as promise the least time by this model.  A step takes t
+// microseconds where a compute unit has one workgroup, 1.5 t where it has two; a join costs a launch and the parts' bytes.
+constexpr long long kMostPartElements = 1 << 27;      // of all parts together
+inline int dense_bwd_share(long long rows, int tile, long long heads, int d, double t, double first, double last, int arrays) {
+  const double cus = compute_units(), longest = std::max(first, last), mean = 0.5 * (first + last);
+  const long long tiles = (rows + tile - 1) / tile * heads, elements = rows * heads * d * arrays;
+  auto time = [&](int parts) {
+    const double each = tiles * parts / cus, pairs = std::floor(each / 2), rest = each - 2 * pairs;
+    const double rounds = 1.5 * pairs + (rest > 1 ? 1.5 : rest > 0 ? 1.0 : 0.0);
+    const double steps = std::max(std::ceil(longest / parts) * std::min(rounds, 1.5), (mean / parts + 1) * rounds);
+    return steps * t + (parts > 1 ? 5.0 + 1e-6 * elements * parts : 0.0);
+  };
+  int best = 1;
+  double least = time(1) * 0.95;
+  for (int parts = 2; parts <= 32 && 2 * parts <= longest && elements * parts <= kMostPartElements; ++parts) {
+    const double us = time(parts);
+    if (us < least) { least = us; best = parts; }
+  }
+  return best;
+}
+// tile: rows of a workgroup; step: streamed rows; tq, tkv: microseconds a step takes
+inline DenseBwdShape dense_bwd_shape(const DenseBwd& p, int tile, int step, double tq, double tkv) {
+  auto steps = [&](long long n) { return (double)((n + step - 1) / step); };
+  auto keys = [&](long long q) { return steps(dense_last_key(p, (int)std::min<long long>(q, p.Nq - 1), p.Nkv)); };
+  auto queries = [&](long long k) { return steps((long long)(p.Nq - dense_first_query(p, (int)std::min<long long>(k, p.Nkv - 1))) * p.group); };
+  DenseBwdShape shape;
+  shape.parts_q = dense_bwd_share(p.Nq, tile, (long long)p.B * p.H, p.d, tq, keys(tile - 1), keys(p.Nq - 1), 1);
+  shape.parts_kv = dense_bwd_share(p.Nkv, tile, (long long)p.B * p.KH, p.d, tkv, queries(0), queries((p.Nkv - 1) / tile * (long long)tile), 2);
+  shape.sums_q = shape.parts_q > 1;
+  return shape;
+}
+
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p);
 hipError_t launch_bf16_dense_bwd(const DenseBwd& p, hipStream_t s);
 DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p);

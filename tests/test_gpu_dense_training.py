@@ -65,3 +65,34 @@ def test_training_step(name):
     got = run(c, q, k, v, do, kv_len)
     torch.cuda.synchronize()
     print(f"  {name}: {check(c, got, ref, cost)}", flush=True)
+
+
+# up to 32 rows (the queries of all heads that share keys) take a launch of their own
+FEW = {
+    "one-row": Step(1, 700, heads=3, batch=2),
+    "thirty-two-rows": Step(32, 333, heads=2),
+    "thirty-three-rows": Step(33, 333, heads=2),
+    "rows-of-heads": Step(4, 517, heads=8, kv_heads=1, batch=2),
+    "rows-of-heads-d64": Step(5, 130, heads=6, kv_heads=1, dim=64, batch=3),
+    "a-tile-of-keys": Step(3, 32, dim=64),
+    "keys-31": Step(3, 31, heads=1),
+    "keys-129-d64": Step(2, 129, heads=1, dim=64),
+    "causal": Step(20, 300, chunk=1, offset=280, heads=2),
+    "causal-shared": Step(8, 100, chunk=1, offset=40, heads=4, kv_heads=1, dim=64),
+    "chunks": Step(2, 9, 1, 12, chunk=3, offset=3, heads=2),
+    "padded": Step(2, 400, heads=2, batch=4, kv_len=(400, 161, 1, 0)),
+    "padded-causal": Step(6, 120, chunk=1, offset=60, batch=3, kv_len=(120, 64, 0), dim=64),
+    "tokens-outside-heads": Step(3, 210, heads=6, kv_heads=2, batch=2, layout="bnhd"),
+    "many-heads": Step(1, 64, heads=300, dim=64),
+    "long": Step(16, 20011, heads=2, kv_heads=1, dim=64),
+}
+
+
+@pytest.mark.parametrize("name", FEW)
+def test_few_queries(name):
+    c = FEW[name]
+    q, k, v, do, kv_len = tensors(c, seed=4)
+    ref, cost = reference(c, q, k, v, do)
+    got = run(c, q, k, v, do, kv_len)
+    torch.cuda.synchronize()
+    print(f"  {name}: {check(c, got, ref, cost)}", flush=True)
