@@ -258,8 +258,10 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
  * Arithmetic.  MRT_BF16 storage with MRT_COMPUTE_DEFAULT (head_dim 64 or 128): bf16 matrix operands (the
  *   probabilities and the gradients of the logits are rounded to bf16, by 2^-8 of the value at most), fp32
  *   accumulation; gradients within 1e-2 of the exact ones in the 2-norm (typically 3e-3).
- *   Otherwise fp32 throughout, within 1e-5.  The same call gives the same bits every time (no atomics).  O and lse
- *   are those of dense_attn_fwd_ws with the same workspace (dense_attn_workspace_bytes; optional).
+ *   Otherwise fp32 throughout, within 1e-5.  The same call gives the same bits every time (no atomics).
+ * dense_attn_fwd_save makes use of dense_attn_fwd_save_workspace_bytes() bytes of scratch (0: none) where the queries are
+ *   few; without them it does the same work with fewer workgroups.  MRT_BF16: O is that of dense_attn_fwd_ws with the
+ *   same workspace.  Other calls round differently where the queries are few.
  * As in the forward pass an infinite or NaN key, value, query or gradient that is hidden by causal_chunk from some
  *   rows of a run of 256, and seen by others, may show in them all; one behind kv_len never shows.
  * dense_attn_bwd needs dense_attn_bwd_workspace_bytes() bytes of scratch (device, 256-byte aligned, contents
@@ -270,6 +272,7 @@ typedef struct {
   const int* kv_len;
   mrt_strides dout, dq, dk, dv;
 } mrt_dense_train;
+size_t dense_attn_fwd_save_workspace_bytes(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk);
 mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void* O, float* lse, const mrt_problem* p,
                                const mrt_dense_train* t, int causal_chunk, void* workspace, size_t workspace_bytes,
                                void* hip_stream);

@@ -26,7 +26,7 @@ EXPORTED = [
     "monarch_attn_fwd_noalloc",
     "monarch_attn_bwd_saved_workspace_bytes", "monarch_attn_fwd_save", "monarch_attn_bwd_saved",
     "dense_attn_workspace_bytes", "dense_attn_fwd_ws",
-    "dense_attn_fwd_save", "dense_attn_bwd", "dense_attn_bwd_check", "dense_attn_bwd_workspace_bytes",
+    "dense_attn_fwd_save", "dense_attn_fwd_save_workspace_bytes", "dense_attn_bwd", "dense_attn_bwd_check", "dense_attn_bwd_workspace_bytes",
     "mrt_rotary_check", "mrt_rotary_fwd", "mrt_rotary_bwd",
 ]
 NOALLOC_SCRATCH_BYTES = 128 << 20
@@ -123,6 +123,8 @@ def load_library() -> ctypes.CDLL:
     T = ctypes.POINTER(MrtDenseTrain)
     lib.dense_attn_fwd_save.argtypes = [vp, vp, vp, vp, vp, P, T, ci, vp, sz, vp]
     lib.dense_attn_fwd_save.restype = ci
+    lib.dense_attn_fwd_save_workspace_bytes.argtypes = [P, T, ci]
+    lib.dense_attn_fwd_save_workspace_bytes.restype = sz
     lib.dense_attn_bwd_check.argtypes = [P, T, ci]
     lib.dense_attn_bwd_check.restype = ci
     lib.dense_attn_bwd_workspace_bytes.argtypes = [P, T, ci]
@@ -485,8 +487,9 @@ def _train_problem(Q, K, V, O, grads, f_q, f_kv, h, w, causal_chunk, q_frame_off
                         dtype=_dtype_of(Q, "Q"), compute=compute, scale=scale, q_strides=st(Q), k_strides=st(K),
                         v_strides=st(V), o_strides=st(O))
     train = MrtDenseTrain(K.shape[1], None, *[MrtStrides(*st(x)) for x in grads])
-    scratch = 0
-    if grads:
+    if not grads:
+        scratch = dense_attn_fwd_save_workspace_bytes(prob, train, causal_chunk)
+    else:
         scratch = dense_attn_bwd_workspace_bytes(prob, train, causal_chunk)
         if scratch == 0:
             lib = load_library()
@@ -517,19 +520,28 @@ def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_off
 
     Q [batch, heads, tokens, head_dim]; K and V [batch, kv_heads, tokens, head_dim], where kv_heads divides heads.
     lse [batch, heads, tokens], fp32: the natural logarithm of the sum of a row's exponentials, -inf for a row that
-    sees no key (its O is 0).  kv_len (int32 [batch], on the device): keys from there on are padding.  O and lse are
-    those of dense_attn_fwd, scratch memory (`workspace`) and what it decides included."""
+    sees no key (its O is 0).  kv_len (int32 [batch], on the device): keys from there on are padding.
+
+    Calls of few queries share their keys over several workgroups if they have scratch memory
+    (dense_attn_fwd_save_workspace_bytes): `workspace`, or memory of torch's allocator.  Without `workspace` a call under a
+    graph capture, or one whose scratch the allocator refuses, does without, as dense_attn_fwd does; bf16 results are those
+    of dense_attn_fwd."""
     import torch
     lib = load_library()
     _same_device(Q, K, V, out, lse, kv_len, workspace)
 
     def call(s):
         O = torch.empty_like(Q) if out is None else out
-        prob, train, _ = _train_problem(Q, K, V, O, (), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute)
+        prob, train, nbytes = _train_problem(Q, K, V, O, (), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale, compute)
         stats = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if lse is None else lse
         _require_lse(stats, Q)
         train = _with_lengths(train, kv_len, Q.shape[0])
-        scratch = _dense_scratch(prob, causal_chunk, Q, s) if workspace is None else workspace
+        scratch = workspace
+        if scratch is None and nbytes and not torch.cuda.is_current_stream_capturing():
+            try:
+                scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
+            except torch.cuda.OutOfMemoryError:       # a call that fits without its scratch still runs
+                pass
         ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
         st = lib.dense_attn_fwd_save(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), stats.data_ptr(),
                                      ctypes.byref(prob), ctypes.byref(train), causal_chunk, ws, nbytes, s)
@@ -537,6 +549,11 @@ def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_off
             _raise(lib, st)
         return O, stats
     return _run_on(Q, stream, call)
+
+
+def dense_attn_fwd_save_workspace_bytes(prob: MrtProblem, train: MrtDenseTrain, causal_chunk=0) -> int:
+    """Scratch a forward call that keeps its row statistics makes use of (0: none)."""
+    return int(load_library().dense_attn_fwd_save_workspace_bytes(ctypes.byref(prob), ctypes.byref(train), causal_chunk))
 
 
 def dense_attn_bwd_workspace_bytes(prob: MrtProblem, train: MrtDenseTrain, causal_chunk=0) -> int:

@@ -903,6 +903,30 @@ static mrt_status dense_train_check(const mrt_problem* p, const mrt_dense_train*
   return MRT_OK;
 }
 
+// fp32 forward calls of few queries: everything but the tensors, and the workgroups that share a tile's keys (0: the
+// kernels of dense_attn_fwd are ahead).
+static DenseFwd dense_fwd_params(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk) {
+  DenseFwd d;
+  memset(&d, 0, sizeof(d));
+  d.q = p->q; d.k = p->k; d.v = p->v; d.o = p->o;
+  d.kv_len = t ? t->kv_len : nullptr;
+  d.B = p->batch; d.H = p->heads; d.KH = t && t->kv_heads ? t->kv_heads : p->heads; d.group = d.H / d.KH;
+  d.d = p->head_dim;
+  d.Nq = p->f_q * p->h * p->w; d.Nkv = p->f_kv * p->h * p->w; d.hw = p->h * p->w;
+  d.cc = causal_chunk; d.qoff = p->q_frame_offset; d.scale = p->scale;
+  d.parts = f32_dense_fwd_parts(d);
+  return d;
+}
+static size_t dense_fwd_parts_bytes(const DenseFwd& d) {
+  return d.parts > 1 ? (size_t)d.parts * d.B * d.H * d.Nq * (d.d + 2) * sizeof(float) : 0;
+}
+
+size_t dense_attn_fwd_save_workspace_bytes(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk) {
+  if (dense_train_check(p, t, causal_chunk, false) != MRT_OK) return 0;
+  if (p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32) return dense_fwd_parts_bytes(dense_fwd_params(p, t, causal_chunk));
+  return bf16_dense_workspace_bytes(dense_params(p, causal_chunk), p->batch * p->heads);
+}
+
 mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void* O, float* lse, const mrt_problem* p,
                                const mrt_dense_train* t, int causal_chunk, void* workspace, size_t workspace_bytes,
                                void* hip_stream) {
@@ -916,14 +940,24 @@ mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void
       if ((uintptr_t)q % 16) { set_error("bf16 path needs 16-byte aligned tensors"); return MRT_ERR_SHAPE; }
   }
   if ((uintptr_t)workspace % 256) { set_error("workspace must be 256-byte aligned"); return MRT_ERR_WORKSPACE; }
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const int BH = p->batch * p->heads;
+  DenseFwd d;
+  memset(&d, 0, sizeof(d));
+  if (f32) {
+    d = dense_fwd_params(p, t, causal_chunk);
+    if (d.parts > 1 && (!workspace || workspace_bytes < dense_fwd_parts_bytes(d))) d.parts = 0;
+    d.Q = Q; d.K = K; d.V = V; d.O = O; d.lse = lse;
+    d.po = (float*)workspace;
+    d.ml = (float2*)(d.po + (size_t)d.parts * BH * d.Nq * d.d);
+  }
   KParams kp = dense_params(p, causal_chunk);
   kp.Q = Q; kp.K = K; kp.V = V; kp.O = O;
-  const int BH = p->batch * p->heads;
   const int kv_heads = t && t->kv_heads ? t->kv_heads : p->heads;
   const DenseSave save = {lse, t ? t->kv_len : nullptr, p->heads / kv_heads};
-  hipError_t e = timed_launch((hipStream_t)hip_stream, MRT_KERNEL_DENSE, [&] {
-    return f32 ? launch_f32_dense(kp, p->dtype, BH, &save, (hipStream_t)hip_stream)
-               : launch_bf16_dense(kp, BH, workspace, workspace_bytes, &save, (hipStream_t)hip_stream);
+  hipError_t e = timed_launch(s, MRT_KERNEL_DENSE, [&] {
+    if (d.parts > 0) return launch_f32_dense_fwd(d, p->dtype, s);
+    return f32 ? launch_f32_dense(kp, p->dtype, BH, &save, s) : launch_bf16_dense(kp, BH, workspace, workspace_bytes, &save, s);
   });
   if (e != hipSuccess) return hip_fail(e, "dense launch");
   return MRT_OK;

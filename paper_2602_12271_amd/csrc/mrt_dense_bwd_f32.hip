@@ -186,8 +186,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p) {
       }
       if constexpr (PART) {
         const long long to = (((long long)part * n_heads + bh) * n_own + r_own) * d;
-        st4<false>((KV ? p.pk : p.pq) + to, x, v, d);
-        if (KV) st4<false>(p.pv + to, y, v, d);
+        st4<VEC>((KV ? p.pk : p.pq) + to, x, v, d);
+        if (KV) st4<VEC>(p.pv + to, y, v, d);
       } else if constexpr (KV) {
         st4<VEC>((T*)p.dK + b * p.dk.batch + hd * p.dk.head + r_own * p.dk.token, x, v, d);
         st4<VEC>((T*)p.dV + b * p.dv.batch + hd * p.dv.head + r_own * p.dv.token, y, v, d);
@@ -273,7 +273,7 @@ hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStrea
   return hipGetLastError();
 }
 
-// (one head of 576 tokens of 64 features 109 -> 48 us for both launches, 12 heads of 1560 of 128 790 -> 600)
+// (one head of 576 tokens of 64 features 109 -> 34 us for both launches, 12 heads of 1560 of 128 790 -> 593)
 DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p) {
   return dense_bwd_shape(p, kRows, kStep, p.d <= 64 ? 1.1 : 2.1, p.d <= 64 ? 1.5 : 2.8);
 }
