@@ -862,7 +862,7 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
   kp.Q = Q; kp.K = K; kp.V = V; kp.O = O;
   const int BH = p->batch * p->heads;
   hipError_t e = timed_launch((hipStream_t)hip_stream, MRT_KERNEL_DENSE, [&] {
-    return f32 ? launch_f32_dense(kp, p->dtype, BH, nullptr, (hipStream_t)hip_stream)
+    return f32 ? launch_f32_dense(kp, p->dtype, BH, (hipStream_t)hip_stream)
                : launch_bf16_dense(kp, BH, workspace, workspace_bytes, nullptr, (hipStream_t)hip_stream);
   });
   if (e != hipSuccess) return hip_fail(e, "dense launch");
@@ -903,7 +903,7 @@ static mrt_status dense_train_check(const mrt_problem* p, const mrt_dense_train*
   return MRT_OK;
 }
 
-// fp32 forward calls of few queries: everything but the tensors, and the workgroups that share a tile's keys (0: the
+// fp32 forward calls: everything but the tensors, and the workgroups that share a tile's keys (0: the
 // kernels of dense_attn_fwd are ahead).
 static DenseFwd dense_fwd_params(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk) {
   DenseFwd d;
@@ -948,6 +948,7 @@ mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void
     d = dense_fwd_params(p, t, causal_chunk);
     if (d.parts > 1 && (!workspace || workspace_bytes < dense_fwd_parts_bytes(d))) d.parts = 0;
     d.Q = Q; d.K = K; d.V = V; d.O = O; d.lse = lse;
+    if (d.parts == 0 && !f32_dense_fwd_quads(d, p->dtype == MRT_F32 ? 4 : 2)) d.parts = 1;
     d.po = (float*)workspace;
     d.ml = (float2*)(d.po + (size_t)d.parts * BH * d.Nq * d.d);
   }
@@ -957,7 +958,7 @@ mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void
   const DenseSave save = {lse, t ? t->kv_len : nullptr, p->heads / kv_heads};
   hipError_t e = timed_launch(s, MRT_KERNEL_DENSE, [&] {
     if (d.parts > 0) return launch_f32_dense_fwd(d, p->dtype, s);
-    return f32 ? launch_f32_dense(kp, p->dtype, BH, &save, s) : launch_bf16_dense(kp, BH, workspace, workspace_bytes, &save, s);
+    return f32 ? launch_f32_dense_save(kp, p->dtype, BH, save, s) : launch_bf16_dense(kp, BH, workspace, workspace_bytes, &save, s);
   });
   if (e != hipSuccess) return hip_fail(e, "dense launch");
   return MRT_OK;

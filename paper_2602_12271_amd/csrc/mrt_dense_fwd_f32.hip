@@ -191,16 +191,20 @@ hipError_t run(const DenseFwd& p, hipStream_t s) {
 }
 template <typename T>
 hipError_t run_t(const DenseFwd& p, hipStream_t s) {
-  const void* ptrs[4] = {p.Q, p.K, p.V, p.O};
-  const mrt_strides* st[4] = {&p.q, &p.k, &p.v, &p.o};
-  bool vec = p.d % 4 == 0;
-  for (int i = 0; i < 4; ++i)
-    vec = vec && (uintptr_t)ptrs[i] % (4 * sizeof(T)) == 0 && st[i]->token % 4 == 0 && st[i]->head % 4 == 0 && st[i]->batch % 4 == 0;
-  if (vec) return p.d <= 64 ? run<64, T, true>(p, s) : run<128, T, true>(p, s);
+  if (f32_dense_fwd_quads(p, sizeof(T))) return p.d <= 64 ? run<64, T, true>(p, s) : run<128, T, true>(p, s);
   return p.d <= 64 ? run<64, T, false>(p, s) : run<128, T, false>(p, s);
 }
 
 }  // namespace
+
+bool f32_dense_fwd_quads(const DenseFwd& p, size_t bytes) {
+  const void* ptrs[4] = {p.Q, p.K, p.V, p.O};
+  const mrt_strides* st[4] = {&p.q, &p.k, &p.v, &p.o};
+  bool quads = p.d % 4 == 0;
+  for (int i = 0; i < 4; ++i)
+    quads = quads && (uintptr_t)ptrs[i] % (4 * bytes) == 0 && st[i]->token % 4 == 0 && st[i]->head % 4 == 0 && st[i]->batch % 4 == 0;
+  return quads;
+}
 
 // The other kernel takes 32 keys in 5.0 us at 128 features and 2.1 at 64 (one workgroup of 128 queries to a compute unit;
 // two share it at 1.35 times that).

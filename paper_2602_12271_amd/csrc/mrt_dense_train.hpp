@@ -114,7 +114,9 @@ inline DenseBwdShape dense_bwd_shape(const DenseBwd& p, int tile, int step, doub
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p);
 hipError_t launch_bf16_dense_bwd(const DenseBwd& p, hipStream_t s);
 DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p);
-// fp32 forward calls of few queries: workgroups that share a tile's keys, 0 where launch_f32_dense takes less time
+// whether rows move as quads (elements of `bytes`)
+bool f32_dense_fwd_quads(const DenseFwd& p, size_t bytes);
+// fp32 forward calls: workgroups that share a tile's keys, 0 where launch_f32_dense_save takes less time
 int f32_dense_fwd_parts(const DenseFwd& p);
 hipError_t launch_f32_dense_fwd(const DenseFwd& p, int dtype, hipStream_t s);
 hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s);

@@ -15,9 +15,9 @@ hipError_t launch_f32_stage_l(const KParams& kp, int dtype, int nbh, bool last, 
   return dtype == MRT_F32 ? run_l_t<float>(kp, grid, last, s) : run_f32_stage_l_bf16(kp, grid, last, s);
 }
 
-hipError_t launch_f32_dense(const KParams& kp, int dtype, int nbh, const DenseSave* save, hipStream_t s) {
+hipError_t launch_f32_dense(const KParams& kp, int dtype, int nbh, hipStream_t s) {
   dim3 grid((kp.Nq + kDenseQ32 - 1) / kDenseQ32, nbh);
-  return dtype == MRT_F32 ? run_dense_t<float>(kp, grid, save, s) : run_f32_dense_bf16(kp, grid, save, s);
+  return dtype == MRT_F32 ? run_dense_t<float>(kp, grid, s) : run_f32_dense_bf16(kp, grid, s);
 }
 
 }  // namespace mrt

@@ -11,6 +11,6 @@ hipError_t run_f32_stage_l_bf16(const KParams& kp, dim3 grid, bool last, hipStre
   return run_l_t<u16>(kp, grid, last, s);
 }
 
-hipError_t run_f32_dense_bf16(const KParams& kp, dim3 grid, const DenseSave* save, hipStream_t s) { return run_dense_t<u16>(kp, grid, save, s); }
+hipError_t run_f32_dense_bf16(const KParams& kp, dim3 grid, hipStream_t s) { return run_dense_t<u16>(kp, grid, s); }
 
 }  // namespace mrt

@@ -1010,7 +1010,8 @@ constexpr int kDenseWaves32 = 8, kDenseQ32 = 16 * kDenseWaves32;
 
 // MASKED: chunk-causal (a kernel of its own: the shorter chunks' bookkeeping costs 4 % of a
 // call at 64 features)
-// Save = DenseSave: a training step's call (heads that share keys, sequences of their own lengths, row statistics)
+// Save = DenseSave: a training step's call (heads that share keys, row statistics; MASKED: also sequences of their own
+// lengths)
 template <int D, typename TIn, bool VEC, bool MASKED, bool SPLIT, typename Save, typename Again>
 __device__ inline bool dense_32(const Place& at, const KParams& p, const Save& save, float* lds, Again again) {
   constexpr bool SAVE = std::is_same<Save, DenseSave>::value;
@@ -1020,7 +1021,7 @@ __device__ inline bool dense_32(const Place& at, const KParams& p, const Save& s
   int kvh = hd, most_keys = p.Nkv;
   if constexpr (SAVE) {
     kvh = hd / save.group;
-    if (save.kv_len) most_keys = min(max(save.kv_len[b], 0), p.Nkv);
+    if (MASKED && save.kv_len) most_keys = min(max(save.kv_len[b], 0), p.Nkv);
   }
   const TIn* Qp = (const TIn*)p.Q + b * p.qs.batch + hd * p.qs.head;
   const TIn* Kp = (const TIn*)p.K + b * p.ks.batch + kvh * p.ks.head;
@@ -1029,7 +1030,7 @@ __device__ inline bool dense_32(const Place& at, const KParams& p, const Save& s
   Query32<D, SPLIT> q;
   Out32<D, SPLIT> o;
   if constexpr (SAVE)
-    if (most_keys == 0) {       // an empty sequence
+    if (MASKED && most_keys == 0) {       // an empty sequence
       o.clear();
       if (qi < p.Nq) {
         o.template store<VEC>((TIn*)p.O + b * p.os.batch + hd * p.os.head + (long long)qi * p.os.token, 0.f, g, d);
@@ -1240,21 +1241,16 @@ hipError_t run_l_t(const KParams& kp, dim3 grid, bool last, hipStream_t s) {
 }
 
 template <int D, typename TIn, bool VEC>
-hipError_t run_dense(const KParams& kp, dim3 grid, const DenseSave* save, hipStream_t s) {
+hipError_t run_dense(const KParams& kp, dim3 grid, hipStream_t s) {
   constexpr int threads = 64 * kDenseWaves32;
-  if (save) {
-    if (kp.cc > 0 || save->kv_len) k_f32_dense<D, TIn, VEC, true><<<grid, threads, 0, s>>>(kp, *save);
-    else k_f32_dense<D, TIn, VEC, false><<<grid, threads, 0, s>>>(kp, *save);
-  } else {
-    if (kp.cc > 0) k_f32_dense<D, TIn, VEC, true><<<grid, threads, 0, s>>>(kp, NoSave{});
-    else k_f32_dense<D, TIn, VEC, false><<<grid, threads, 0, s>>>(kp, NoSave{});
-  }
+  if (kp.cc > 0) k_f32_dense<D, TIn, VEC, true><<<grid, threads, 0, s>>>(kp, NoSave{});
+  else k_f32_dense<D, TIn, VEC, false><<<grid, threads, 0, s>>>(kp, NoSave{});
   return hipGetLastError();
 }
 template <typename TIn>
-hipError_t run_dense_t(const KParams& kp, dim3 grid, const DenseSave* save, hipStream_t s) {
-  if (vec_ok<TIn>(kp)) return kp.d <= 64 ? run_dense<64, TIn, true>(kp, grid, save, s) : run_dense<128, TIn, true>(kp, grid, save, s);
-  return kp.d <= 64 ? run_dense<64, TIn, false>(kp, grid, save, s) : run_dense<128, TIn, false>(kp, grid, save, s);
+hipError_t run_dense_t(const KParams& kp, dim3 grid, hipStream_t s) {
+  if (vec_ok<TIn>(kp)) return kp.d <= 64 ? run_dense<64, TIn, true>(kp, grid, s) : run_dense<128, TIn, true>(kp, grid, s);
+  return kp.d <= 64 ? run_dense<64, TIn, false>(kp, grid, s) : run_dense<128, TIn, false>(kp, grid, s);
 }
 
 }  // namespace

@@ -151,11 +151,13 @@ mrt_status fwd_run(const void* Q, const void* K, const void* V, void* O, const m
 // bf16 storage, fp32 arithmetic (called by the launchers below)
 hipError_t run_f32_stage_r_bf16(const KParams& kp, dim3 grid, bool first, bool last, hipStream_t s);
 hipError_t run_f32_stage_l_bf16(const KParams& kp, dim3 grid, bool last, hipStream_t s);
-hipError_t run_f32_dense_bf16(const KParams& kp, dim3 grid, const DenseSave* save, hipStream_t s);
+hipError_t run_f32_dense_bf16(const KParams& kp, dim3 grid, hipStream_t s);
 hipError_t launch_f32_stage_r(const KParams& kp, int dtype, int nbh, bool first, bool last,
                               hipStream_t s);
 hipError_t launch_f32_stage_l(const KParams& kp, int dtype, int nbh, bool last, hipStream_t s);
-hipError_t launch_f32_dense(const KParams& kp, int dtype, int nbh, const DenseSave* save, hipStream_t s);
+hipError_t launch_f32_dense(const KParams& kp, int dtype, int nbh, hipStream_t s);
+// with row statistics; rows that move as quads (mrt_f32_save.hip)
+hipError_t launch_f32_dense_save(const KParams& kp, int dtype, int nbh, const DenseSave& save, hipStream_t s);
 
 // backward pass, fp32 (mrt_bwd_f32.hip)
 bool bwd_fits(int b1, int b2, int d);
