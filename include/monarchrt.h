@@ -263,7 +263,8 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
  *   few; without them it does the same work with fewer workgroups.  MRT_BF16: O is that of dense_attn_fwd_ws with the
  *   same workspace.  Other calls round differently where the queries are few.
  * As in the forward pass an infinite or NaN key, value, query or gradient that is hidden by causal_chunk from some
- *   rows of a run of 256, and seen by others, may show in them all; one behind kv_len never shows.
+ *   rows of a run of 256 (with shared keys: of the heads that share them), and seen by others, may show in them all; one
+ *   behind kv_len, or one that the mask hides from every row, never shows.
  * dense_attn_bwd needs dense_attn_bwd_workspace_bytes() bytes of scratch (device, 256-byte aligned, contents
  *   undefined on entry and exit; 0: invalid arguments).  dense_attn_bwd_check applies the same rules as the call.
  *   Thread safety as for monarch_attn_fwd; every launch is on hip_stream. */
@@ -293,10 +294,10 @@ mrt_status dense_attn_bwd(const void* Q, const void* K, const void* V, const voi
  *             of pairs, one ladder shared out over the axes.
  * A tensor [batch, heads, f*h*w tokens, head_dim] has the positions of its grid, frame_offset + frame, row and column,
  *   or, with `positions` (device memory, int32, element strides position_batch, position_axis and 1), its own: a token
- *   of text has the same on every axis.  Angles are formed in 64 bits, exact to 1e-7 for every 32-bit position;
- *   products and sums in fp32, rounded once to the type of Y.
+ *   of text has the same on every axis.  Angles are formed in 64 bits, exact to 1e-7 radians (6e-7 for positions
+ *   beyond 10^8); products and sums in fp32, rounded once to the type of Y.
  * One call rotates one or two tensors (queries and keys, which may differ in heads, frames and types).  Y may be X
- *   itself with the same type and strides; otherwise they do not overlap. */
+ *   itself with the same type and strides; otherwise no output overlaps an input or another output. */
 typedef enum { MRT_ROTARY_ADJACENT = 0, MRT_ROTARY_HALVES = 1 } mrt_rotary_layout;
 typedef enum { MRT_ROTARY_PER_AXIS = 0, MRT_ROTARY_SHARED = 1 } mrt_rotary_ladder;
 typedef struct {

@@ -870,6 +870,12 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
 }
 
 // ---- a training step of the dense attention ----------------------------------------------
+// (by its bits: the library is compiled without regard to NaN in comparisons)
+static bool not_finite(double x) {
+  uint64_t bits;
+  memcpy(&bits, &x, sizeof(bits));
+  return (bits >> 52 & 0x7ff) == 0x7ff;
+}
 static mrt_status dense_train_check(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk, bool backward) {
   mrt_status st = dense_attn_check(p, causal_chunk);
   if (st != MRT_OK) return st;
@@ -879,7 +885,7 @@ static mrt_status dense_train_check(const mrt_problem* p, const mrt_dense_train*
     set_error("kv_heads = %d must divide heads = %d", kv_heads, p->heads);
     return MRT_ERR_SHAPE;
   }
-  if (!(p->scale >= 1e-30f)) { set_error("scale below 1e-30"); return MRT_ERR_UNSUPPORTED; }
+  if (not_finite(p->scale) || p->scale < 1e-30f) { set_error("scale must be finite and at least 1e-30"); return MRT_ERR_UNSUPPORTED; }
   if (!backward) return MRT_OK;
   if (!t) { set_error("the backward call needs the strides of its gradients"); return MRT_ERR_NULL; }
   const mrt_strides* more[4] = {&t->dout, &t->dq, &t->dk, &t->dv};
@@ -933,6 +939,7 @@ mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void
   mrt_status st = dense_train_check(p, t, causal_chunk, false);
   if (st != MRT_OK) return st;
   if (!Q || !K || !V || !O || !lse) { set_error("Q, K, V, O and lse must be non-NULL"); return MRT_ERR_NULL; }
+  if (O == K || O == V) { set_error("O in the place of K or V"); return MRT_ERR_SHAPE; }
   const bool f32 = p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32;
   if (!f32) {
     const void* ptrs[4] = {Q, K, V, O};
@@ -1011,6 +1018,10 @@ mrt_status dense_attn_bwd(const void* Q, const void* K, const void* V, const voi
     set_error("Q, K, V, O, dO, lse, dQ, dK and dV must be non-NULL");
     return MRT_ERR_NULL;
   }
+  const void* given[8] = {dQ, dK, dV, Q, K, V, O, dO};      // the launches read their inputs after they write gradients
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 8; ++j)
+      if (given[i] == given[j]) { set_error("a gradient in the place of an input or of another gradient"); return MRT_ERR_SHAPE; }
   const bool f32 = p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32;
   if (!f32) {
     const void* ptrs[8] = {Q, K, V, O, dO, dQ, dK, dV};
@@ -1048,7 +1059,7 @@ mrt_status mrt_rotary_check(const mrt_rotary* r, const mrt_rotary_tensor* x, int
   }
   if (r->layout != MRT_ROTARY_ADJACENT && r->layout != MRT_ROTARY_HALVES) { set_error("unknown rotary layout"); return MRT_ERR_SHAPE; }
   if (r->ladder != MRT_ROTARY_PER_AXIS && r->ladder != MRT_ROTARY_SHARED) { set_error("unknown rotary ladder"); return MRT_ERR_SHAPE; }
-  if (!(r->theta >= 1.0) || !(r->theta <= 1e12)) { set_error("theta must be 1..1e12"); return MRT_ERR_SHAPE; }
+  if (not_finite(r->theta) || r->theta < 1.0 || r->theta > 1e12) { set_error("theta must be 1..1e12"); return MRT_ERR_SHAPE; }
   if (r->head_dim < 1 || r->head_dim > 256) { set_error("head_dim must be 1..256"); return MRT_ERR_SHAPE; }
   if (total < 1 || 2 * total > r->head_dim) {
     set_error("%d rotary pairs do not fit head_dim = %d", total, r->head_dim);
@@ -1099,6 +1110,10 @@ static mrt_status rotary_run(const mrt_rotary* r, const mrt_rotary_tensor* x, in
       set_error("tensor %d is not aligned to its elements", i);
       return MRT_ERR_SHAPE;
     }
+  }
+  if (n > 1 && (Y[0] == Y[1] || X[0] == Y[1] || X[1] == Y[0])) {
+    set_error("the output of one tensor is that of the other, or the other itself");
+    return MRT_ERR_SHAPE;
   }
   // (in place a repeated launch would turn once more)
   const bool in_place = X[0] == Y[0] || (n > 1 && X[1] == Y[1]);
