@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
   const Unit u = unit_of(p, p.B * p.H, (p.Nq + kRows - 1) / kRows, parts, true);
   const int b = u.bh / p.H, hd = u.bh - b * p.H, kvh = hd / p.group;
   const int q0 = u.tile * kRows, q_last = q0 + kRows < p.Nq ? q0 + kRows - 1 : p.Nq - 1;
-  const int keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), k_end = dense_last_key(p, q_last, keys), nqb = (p.Nq + 31) >> 5;
+  const int keys = __builtin_amdgcn_readfirstlane(dense_seen_keys(p, b)), k_end = dense_last_key(p, q_last, keys), nqb = (p.Nq + 31) >> 5;
   const int all = (k_end + kStep - 1) / kStep;
   const int i0 = PART ? (int)((long long)all * u.part / parts) : 0, i1 = PART ? (int)((long long)all * (u.part + 1) / parts) : all;
 
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
   const Unit u = unit_of(p, p.B * p.KH, (p.Nkv + kRows - 1) / kRows, parts, false);
   const int b = u.bh / p.KH, hd = u.bh - b * p.KH;
   const int k0 = u.tile * kRows, k_last = k0 + kRows < p.Nkv ? k0 + kRows - 1 : p.Nkv - 1;
-  const int keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), nqb = (p.Nq + 31) >> 5;
+  const int keys = __builtin_amdgcn_readfirstlane(dense_seen_keys(p, b)), nqb = (p.Nq + 31) >> 5;
   const int q_first = dense_first_query(p, k0) & ~(kStep - 1);      // of every head that reads these keys
   const int per_head = k0 < keys && q_first < p.Nq ? (p.Nq - q_first + kStep - 1) / kStep : 0, all = per_head * p.group;
   const int i0 = PART ? (int)((long long)all * u.part / parts) : 0, i1 = PART ? (int)((long long)all * (u.part + 1) / parts) : all;
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing is on its way to LDS when the workgroup leaves it
 
   if (key >= p.Nkv) return;
-  const bool live = key < keys;                 // (padding's columns may hold anything)
+  const bool live = key < keys;                 // (the columns of the others may hold anything)
   u16* tk = (u16*)p.dK + b * p.dk.batch + hd * p.dk.head + kr * p.dk.token + 4 * hi;
   u16* tv = (u16*)p.dV + b * p.dv.batch + hd * p.dv.head + kr * p.dv.token + 4 * hi;
   const long long part = (((long long)u.part * p.B * p.KH + u.bh) * p.Nkv + kr) * D + 4 * hi;
@@ -500,14 +500,14 @@ __global__ __launch_bounds__(kThreads) void k_bf16_dense_bwd_few(DenseBwd p) {
   auto swz = [](int row) { return D == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : (row & 2) << 1 | ((row >> 2) & 3); };
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
   const int parts = p.parts_q, unit = blockIdx.x, part = unit % parts, kh = unit / parts, b = kh / p.KH, hd = kh - b * p.KH;
-  const int rows = p.group * p.Nq, keys = __builtin_amdgcn_readfirstlane(dense_keys(p, b)), tiles = (p.Nkv + 31) >> 5;
+  const int rows = p.group * p.Nq, keys = __builtin_amdgcn_readfirstlane(dense_seen_keys(p, b)), tiles = (p.Nkv + 31) >> 5;
   const int t0 = (int)((long long)tiles * part / parts), t1 = (int)((long long)tiles * (part + 1) / parts);
   const u16* Kp = (const u16*)p.K + b * p.k.batch + hd * p.k.head;
   const u16* Vp = (const u16*)p.V + b * p.v.batch + hd * p.v.head;
   const unsigned krow = (unsigned)p.k.token * 2u, vrow = (unsigned)p.v.token * 2u, lds0 = (unsigned)(unsigned long long)(const lds_void*)bwd_lds;
   const int mine = wave * L::WAVE;      // this wave's part of LDS
 
-  // (keys behind the sequence's end are zeros)
+  // (keys that nothing sees are zeros)
   auto fetch = [&](int tile, int slot) {
     const int left = tile < t1 ? keys - 32 * tile : 0;
     const unsigned n = left <= 0 ? 0 : left < 32 ? left : 32;

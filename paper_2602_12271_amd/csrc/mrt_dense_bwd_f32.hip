@@ -32,7 +32,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p) {
   unit /= n_heads;
   const int part = unit % parts, tile = KV ? unit / parts : tiles - 1 - unit / parts;    // under a mask the longest first
   const int b = bh / (KV ? p.KH : p.H), hd = bh - b * (KV ? p.KH : p.H), kvh = KV ? hd : hd / p.group;
-  const int own0 = tile * kRows, keys = dense_keys(p, b), own_last = own0 + kRows < n_own ? own0 + kRows - 1 : n_own - 1;
+  const int own0 = tile * kRows, keys = dense_seen_keys(p, b), own_last = own0 + kRows < n_own ? own0 + kRows - 1 : n_own - 1;
 
   // the streamed rows: queries qfirst .. Nq of every head that shares these keys, or keys 0 .. last
   const int qfirst = KV ? dense_first_query(p, own0) & ~(kStep - 1) : 0;

@@ -59,6 +59,8 @@ __host__ __device__ inline int dense_last_key(const P& p, int q, int keys) {
   const long long lim = (long long)((p.qoff + q / p.hw) / p.cc + 1) * p.cc * p.hw;
   return lim < keys ? (int)lim : keys;
 }
+// Keys that some query of the sequence sees: what the others hold shows nowhere.
+__device__ inline int dense_seen_keys(const DenseBwd& p, int b) { return dense_last_key(p, p.Nq - 1, dense_keys(p, b)); }
 // First query that sees key k (Nq or more: none).
 __host__ __device__ inline int dense_first_query(const DenseBwd& p, int k) {
   if (p.cc == 0) return 0;
