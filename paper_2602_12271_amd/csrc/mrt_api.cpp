@@ -986,16 +986,16 @@ static DenseBwd dense_bwd_params(const mrt_problem* p, const mrt_dense_train* t,
 }
 struct DenseBwdWorkspace {
   DenseBwdShape shape;
-  size_t stats, parts, bytes;     // offset of the parts, which the two launches use in turn
+  size_t stats, parts_kv, bytes;     // the rows' numbers, then the parts of dQ, then those of dK and dV
 };
 static DenseBwdWorkspace dense_bwd_workspace(const DenseBwd& d, bool f32) {
   DenseBwdWorkspace w;
   w.shape = f32 ? f32_dense_bwd_shape(d) : bf16_dense_bwd_shape(d);
   w.stats = round256((size_t)d.B * d.H * ((d.Nq + 31) / 32) * 64 * sizeof(float));
   const size_t q = w.shape.sums_q ? (size_t)w.shape.parts_q * d.B * d.H * d.Nq * d.d * sizeof(float) : 0;
-  const size_t kv = w.shape.parts_kv > 1 ? 2 * (size_t)w.shape.parts_kv * d.B * d.KH * d.Nkv * d.d * sizeof(float) : 0;
-  w.parts = w.stats;
-  w.bytes = w.stats + round256(q > kv ? q : kv);
+  const size_t kv = w.shape.sums_kv ? 2 * (size_t)w.shape.parts_kv * d.B * d.KH * d.Nkv * d.d * sizeof(float) : 0;
+  w.parts_kv = w.stats + round256(q);
+  w.bytes = w.parts_kv + round256(kv);
   return w;
 }
 
@@ -1037,7 +1037,8 @@ mrt_status dense_attn_bwd(const void* Q, const void* K, const void* V, const voi
   d.Q = Q; d.K = K; d.V = V; d.O = O; d.dO = dO; d.lse = lse;
   d.dQ = dQ; d.dK = dK; d.dV = dV;
   d.stats = (float*)workspace;
-  d.pq = d.pk = (float*)((char*)workspace + w.parts);
+  d.pq = (float*)((char*)workspace + w.stats);
+  d.pk = (float*)((char*)workspace + w.parts_kv);
   d.pv = d.pk + (size_t)w.shape.parts_kv * d.B * d.KH * d.Nkv * d.d;
   d.parts_q = w.shape.parts_q; d.parts_kv = w.shape.parts_kv;
   const hipStream_t s = (hipStream_t)hip_stream;

@@ -1,23 +1,25 @@
 // Backward pass of the dense softmax attention on the bf16 matrix unit (formulas: mrt_dense_train.hpp).
 //
-// Two launches, no atomics: the gradients of the queries, whose workgroups own queries and stream the keys, and those
-// of the keys, whose workgroups own keys and stream the queries of every head that reads them.  Seven products where
-// one launch would form five; but one launch has to add to dQ from every key tile, in an order that changes, or to
-// write and read as many partial arrays as there are key tiles (half a gigabyte each way for 12 heads of 4680
-// tokens).  The first launch also leaves what the second one needs of a row: -log2(e) lse and -delta.
+// No atomics, two kinds of workgroups in one launch: those of the gradients of the queries own queries and stream the keys,
+// those of the keys own keys and stream the queries of every head that reads them.  Seven products where one kind would
+// form five; but that one has to add to dQ from every key tile, in an order that changes, or to write and read as many
+// partial arrays as there are key tiles (half a gigabyte each way for 12 heads of 4680 tokens).  A small launch before it
+// leaves what both need of a row, -log2(e) lse and -delta.  (The two kinds in launches of their own, the first of which
+// left these: us of a call, two launches | one: one head of 4680 tokens 86 | 68, 12 of 1560 tokens 105 | 87, 40 of 1800
+// tokens 299 | 269, batch of 3, 4 heads of 782 tokens of 64 features 42 | 28, 12 heads of 4680 tokens 444 | 445.)
 //
 // A wave owns 32 rows: their operands and gradients stay in registers, the streamed rows pass through an LDS ring 32 a
 // step, loaded by instructions that write LDS directly, several steps ahead.  Logits have the streamed rows on the M
 // side and the wave's rows on the N side of a product, so that weights, packed to bf16, are as they stand the operand
 // of the second products, whose other operand is the streamed tile read transposed.
 //
-// What bounds the launches is power: a wave's 32 rows take a kilobyte of LDS reads for every 32768 operations, and at
+// What bounds the launch is power: a wave's 32 rows take a kilobyte of LDS reads for every 32768 operations, and at
 // that ratio the card's clock falls until bare products reach about 1400 TFLOP/s (32 x 32 tiles) or 1550 (16 x 16),
 // where products from registers reach 1670 and 1950 and a large library product 1355.  Vector instructions hardly run
 // beside another wave's 16 x 16 products and half hide behind a wave's own; beside 32 x 32 products of another wave they
-// run whole.  So the launch of the queries, which has the registers for the logits of two steps, forms the weights of
-// one step between its own products of the next, 16 x 16 tiles; the launch of the keys, which has not, takes 32 x 32
-// tiles and leaves it to the two workgroups of a compute unit to be in different phases.  (Waves of 64 rows, one to a
+// run whole.  So a tile of queries, which has the registers for the logits of two steps, forms the weights of one step
+// between its own products of the next, 16 x 16 tiles; a tile of keys, which has not, takes 32 x 32 tiles and leaves it
+// to the two workgroups of a compute unit to be in different phases.  (Waves of 64 rows, one to a
 // SIMD, halve the LDS reads, but what does not fit 256 registers moves between the two halves of the register file:
 // 1.2 to 1.8 times as long.)
 #include "mrt_dense_train.hpp"
@@ -125,9 +127,8 @@ struct Stream {
 struct Unit {
   int bh, tile, part;
 };
-__device__ inline Unit unit_of(const DenseBwd& p, int n_heads, int tiles, int parts, bool last_first) {
-  int unit = blockIdx.x;
-  const int total = gridDim.x;
+__device__ inline Unit unit_of(const DenseBwd& p, int unit, int n_heads, int tiles, int parts, bool last_first) {
+  const int total = n_heads * tiles * parts;
   Unit u;
   if (p.cc == 0) {
     const int xcd = unit & 7;
@@ -157,7 +158,7 @@ __device__ inline void put4(u16* row, float* part, int f, f32x4 x) {
 // Two tiles of 16 queries a wave.  A step's products run in this order: A, the logits and dO V^T of the next step's keys;
 // B, dQ^T += K^T dS of this step.  Between the products of A stand the exponentials and gradients of this step's logits.
 template <int D, bool PART>
-__global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
+__device__ __forceinline__ void bwd_queries(const DenseBwd& p, int unit) {
   constexpr int NT = 2, KS = D / 32, FT = D / 16, RB = 2 * D;
   using S = Stream<D, false>;
   // rows are swizzled by pairs of pieces: the sixteen rows x two pairs a 16-byte read takes at once (rows 0-3 and 12-15
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
   auto swz = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int parts = PART ? p.parts_q : 1;
-  const Unit u = unit_of(p, p.B * p.H, (p.Nq + kRows - 1) / kRows, parts, true);
+  const Unit u = unit_of(p, unit, p.B * p.H, (p.Nq + kRows - 1) / kRows, parts, true);
   const int b = u.bh / p.H, hd = u.bh - b * p.H, kvh = hd / p.group;
   const int q0 = u.tile * kRows, q_last = q0 + kRows < p.Nq ? q0 + kRows - 1 : p.Nq - 1;
   const int keys = __builtin_amdgcn_readfirstlane(dense_seen_keys(p, b)), k_end = dense_last_key(p, q_last, keys), nqb = (p.Nq + 31) >> 5;
@@ -182,7 +183,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
   // the wave's queries
   const u16* Qp = (const u16*)p.Q + b * p.q.batch + hd * p.q.head;
   const u16* dOp = (const u16*)p.dO + b * p.dout.batch + hd * p.dout.head;
-  const u16* Op = (const u16*)p.O + b * p.o.batch + hd * p.o.head;
   const int qw = q0 + 16 * NT * wave;
   bf16x8 qf[NT][KS], of[NT][KS];
   float nlse[NT], ndelta[NT];          // -log2(e) lse, -delta
@@ -190,23 +190,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
   for (int t = 0; t < NT; ++t) {
     const int q = qw + 16 * t + c;
     const long long r = q < p.Nq ? q : p.Nq - 1;
-    float sum = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       qf[t][ks] = ld_global_16B(Qp + r * p.q.token + 32 * ks + 8 * g);
       of[t][ks] = ld_global_16B(dOp + r * p.dout.token + 32 * ks + 8 * g);
-      const bf16x8 o = ld_global_16B(Op + r * p.o.token + 32 * ks + 8 * g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf((float)o[e], (float)of[t][ks][e], sum);
     }
-    ndelta[t] = -xsum(sum);
-    const float l = p.lse[(long long)u.bh * p.Nq + r];
-    nlse[t] = l == -INFINITY ? -INFINITY : -kLog2e * l;       // (a row that sees no key: weights of zero)
-    if (u.part == 0 && g == 0 && q < nqb * 32) {
-      float* s = p.stats + ((long long)u.bh * nqb + (q >> 5)) * 64 + (q & 31);
-      s[0] = q >= p.Nq ? -INFINITY : nlse[t];
-      s[32] = q >= p.Nq ? 0.f : ndelta[t];
-    }
+    const float* stats = p.stats + ((long long)u.bh * nqb + (r >> 5)) * 64 + (r & 31);
+    nlse[t] = stats[0];
+    ndelta[t] = stats[32];
   }
   const float scale2 = p.scale * kLog2e;
   f32x4 dq[NT][FT];    // dQ^T
@@ -327,7 +318,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_q(DenseBwd p) {
 // matrix phase of the other workgroup's wave on the SIMD, and a matrix phase (what these give to dV^T and dK^T, then the
 // logits and dO V^T of the next step's queries).
 template <int D, bool PART>
-__global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
+__device__ __forceinline__ void bwd_keys(const DenseBwd& p, int unit) {
   constexpr int KS = D / 16, FT = D / 32, RB = 2 * D, AHEAD = 3;
   using S = Stream<D, true>;
   // sixteen rows that agree in a piece lie on all 64 banks (those a 16-byte read takes at once: 0-3, 12-15 and 20-27 of a
@@ -336,7 +327,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
   auto swz = [](int row) { return D == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : (row & 2) << 1 | ((row >> 2) & 3); };
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
   const int parts = PART ? p.parts_kv : 1;
-  const Unit u = unit_of(p, p.B * p.KH, (p.Nkv + kRows - 1) / kRows, parts, false);
+  const Unit u = unit_of(p, unit, p.B * p.KH, (p.Nkv + kRows - 1) / kRows, parts, false);
   const int b = u.bh / p.KH, hd = u.bh - b * p.KH;
   const int k0 = u.tile * kRows, k_last = k0 + kRows < p.Nkv ? k0 + kRows - 1 : p.Nkv - 1;
   const int keys = __builtin_amdgcn_readfirstlane(dense_seen_keys(p, b)), nqb = (p.Nq + 31) >> 5;
@@ -479,6 +470,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd_kv(DenseBwd p) {
       put4<PART>(tk, p.pk + part, 32 * f + 8 * j, x);
       put4<PART>(tv, p.pv + part, 32 * f + 8 * j, y);
     }
+}
+
+// One launch for both: the key tiles, whose steps are the longer ones, come first.
+template <int D, bool PART>
+__global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd(DenseBwd p, int key_units) {
+  const int unit = blockIdx.x;
+  if (unit < key_units) bwd_keys<D, PART>(p, unit);
+  else bwd_queries<D, PART>(p, unit - key_units);
 }
 
 // ---- few queries -------------------------------------------------------------------------------
@@ -682,13 +681,6 @@ __global__ __launch_bounds__(kThreads) void k_bf16_dense_bwd_few(DenseBwd p) {
 
 bool few_queries(const DenseBwd& p) { return (long long)p.group * p.Nq <= 32; }
 
-template <typename Kernel>
-hipError_t launch(Kernel kernel, int rows, int heads, int parts, int lds, const DenseBwd& p, hipStream_t s) {
-  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return e;
-  kernel<<<(unsigned)((rows + kRows - 1) / kRows * (long long)heads * parts), kThreads, lds, s>>>(p);
-  return hipGetLastError();
-}
 template <int D>
 hipError_t run(const DenseBwd& p, hipStream_t s) {
   hipError_t e;
@@ -700,22 +692,25 @@ hipError_t run(const DenseBwd& p, hipStream_t s) {
     e = hipGetLastError();
     return e != hipSuccess ? e : launch_dense_bwd_join(p, false, MRT_BF16, s);
   }
-  constexpr int lq = Stream<D, false>::RING, lkv = Stream<D, true>::RING;
-  if (p.parts_q == 1) e = launch(k_bf16_dense_bwd_q<D, false>, p.Nq, p.B * p.H, 1, lq, p, s);
-  else e = launch(k_bf16_dense_bwd_q<D, true>, p.Nq, p.B * p.H, p.parts_q, lq, p, s);
-  if (e == hipSuccess && p.parts_q > 1) e = launch_dense_bwd_join(p, false, MRT_BF16, s);
+  constexpr int lds = Stream<D, true>::RING;
+  static_assert(lds >= Stream<D, false>::RING, "the ring of either");
+  e = launch_dense_bwd_stats(p, MRT_BF16, s);
   if (e != hipSuccess) return e;
-  if (p.parts_kv == 1) return launch(k_bf16_dense_bwd_kv<D, false>, p.Nkv, p.B * p.KH, 1, lkv, p, s);
-  e = launch(k_bf16_dense_bwd_kv<D, true>, p.Nkv, p.B * p.KH, p.parts_kv, lkv, p, s);
-  return e != hipSuccess ? e : launch_dense_bwd_join(p, true, MRT_BF16, s);
+  const long long keys = (p.Nkv + kRows - 1) / kRows * (long long)(p.B * p.KH) * p.parts_kv;
+  const long long queries = (p.Nq + kRows - 1) / kRows * (long long)(p.B * p.H) * p.parts_q;
+  const bool part = p.parts_q > 1 || p.parts_kv > 1;
+  const auto kernel = part ? k_bf16_dense_bwd<D, true> : k_bf16_dense_bwd<D, false>;
+  e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)(keys + queries), kThreads, lds, s>>>(p, (int)keys);
+  e = hipGetLastError();
+  return e != hipSuccess || !part ? e : launch_dense_bwd_join(p, true, MRT_BF16, s);
 }
 
 }  // namespace
 
-// (steps fitted to 14 shapes of 1 to 40 heads, 200 to 10800 tokens: one head of 4680 tokens, 37 tiles, queries 98 -> 14 us
-// and keys 112 -> 12 with 7 parts; 5 heads 97 -> 66 and 110 -> 75 with 4; 12 heads one part, 3 % less than with two)
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
-  if (!few_queries(p)) return dense_bwd_shape(p, kRows, kStep, p.d == 64 ? 0.43 : 0.66, p.d == 64 ? 0.51 : 0.78);
+  if (!few_queries(p)) return dense_bwd_shape(p, kRows, kStep, p.d == 64 ? 0.35 : 0.72, p.d == 64 ? 0.65 : 1.05);
   // few queries: runs of key tiles that fill the chip in whole rounds (a round costs a workgroup as much as half a tile)
   const long long cus = compute_units(), heads = (long long)p.B * p.KH, tiles = (p.Nkv + 31) / 32;
   double least = INFINITY;
@@ -724,7 +719,7 @@ DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
     const double cost = (double)((heads * parts + cus - 1) / cus) * ((double)((tiles + 4 * parts - 1) / (4 * parts)) + 0.5);
     if (cost < least) { least = cost; best = parts; }
   }
-  return {best, 1, true};
+  return {best, 1, true, false};
 }
 
 hipError_t launch_bf16_dense_bwd(const DenseBwd& p, hipStream_t s) { return p.d == 64 ? run<64>(p, s) : run<128>(p, s); }

@@ -21,13 +21,11 @@ template <int D> constexpr int kSlot = 2 * kStep * kLd<D> + 2 * kStep;
 __device__ inline f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 template <int D, typename T, bool VEC, bool KV, bool PART>
-__global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p) {
+__device__ __forceinline__ void bwd_tile(const DenseBwd& p, int unit, float* lds) {
   constexpr int KS = D / 16, BLK = D / 64, LD = kLd<D>, QUADS = kStep * D / 4 / kThreads;
-  __shared__ __attribute__((aligned(16))) float lds[2 * kSlot<D>];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int n_own = KV ? p.Nkv : p.Nq, n_heads = p.B * (KV ? p.KH : p.H), d = p.d;
   const int tiles = (n_own + kRows - 1) / kRows, parts = PART ? (KV ? p.parts_kv : p.parts_q) : 1;
-  int unit = blockIdx.x;
   const int bh = unit % n_heads;
   unit /= n_heads;
   const int part = unit % parts, tile = KV ? unit / parts : tiles - 1 - unit / parts;    // under a mask the longest first
@@ -98,23 +96,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p) {
   const int lim = KV ? dense_first_query(p, rc) : dense_last_key(p, rc, keys);
   float nlse = 0.f, ndelta = 0.f;
   if constexpr (!KV) {
-    const T* orow = (const T*)p.O + b * p.o.batch + hd * p.o.head + rc * p.o.token;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int v = 16 * ks + 4 * g;
-      const f32x4 o = blank4<VEC>(ld4<VEC>(orow, v, d), v, d);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] = fmaf(o[e], ob[ks][e], sum[e]);
-    }
-    ndelta = -xsum((sum[0] + sum[1]) + (sum[2] + sum[3]));
-    const float l = p.lse[(long long)bh * p.Nq + rc];
-    nlse = l == -INFINITY ? -INFINITY : -kLog2e * l;
-    if (part == 0 && g == 0 && r_own < nqb * 32) {
-      float* st = p.stats + ((long long)bh * nqb + (r_own >> 5)) * 64 + (r_own & 31);
-      st[0] = r_own >= p.Nq ? -INFINITY : nlse;
-      st[32] = r_own >= p.Nq ? 0.f : ndelta;
-    }
+    const float* st = p.stats + ((long long)bh * nqb + (rc >> 5)) * 64 + (rc & 31);
+    nlse = st[0];
+    ndelta = st[32];
   }
   f32x4 g1[BLK][4], g2[BLK][4];
 #pragma unroll
@@ -197,22 +181,63 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p) {
     }
 }
 
-// Gradients from their parts, added in their order: dQ, or dK and dV (blockIdx.y).  A thread owns four features of a
+// One launch for both: the key tiles, whose steps are the longer ones, come first.
+template <int D, typename T, bool VEC, bool PART>
+__global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p, int key_units) {
+  __shared__ __attribute__((aligned(16))) float lds[2 * kSlot<D>];
+  const int unit = blockIdx.x;
+  if (unit < key_units) bwd_tile<D, T, VEC, true, PART>(p, unit, lds);
+  else bwd_tile<D, T, VEC, false, PART>(p, unit - key_units, lds);
+}
+
+// What the tiles need of a row of queries: -log2(e) lse (-infinity where it sees no key: weights of zero) and -delta,
+// delta the sum of its O dO.  64 numbers for 32 rows, rows behind the last one as such that see no key.  Sixteen threads a
+// row; memory bounds it.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_dense_bwd_stats(DenseBwd p, int nqb) {
+  const long long tile = blockIdx.x >> 1;
+  const int bh = (int)(tile / nqb), r = 16 * (blockIdx.x & 1) + (threadIdx.x >> 4), q = (int)(tile - (long long)bh * nqb) * 32 + r;
+  const int b = bh / p.H, hd = bh - b * p.H, row = q < p.Nq ? q : p.Nq - 1;
+  const T* o = (const T*)p.O + b * p.o.batch + hd * p.o.head + row * p.o.token;
+  const T* dO = (const T*)p.dO + b * p.dout.batch + hd * p.dout.head + row * p.dout.token;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int v = 4 * (threadIdx.x & 15) + 64 * k;
+    const f32x4 x = blank4<VEC>(ld4<VEC>(o, v, p.d), v, p.d), y = blank4<VEC>(ld4<VEC>(dO, v, p.d), v, p.d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum = fmaf(x[e], y[e], sum);
+  }
+#pragma unroll
+  for (int m = 8; m > 0; m >>= 1) sum += __shfl_xor(sum, m, 16);
+  if ((threadIdx.x & 15) == 0) {
+    const float lse = p.lse[(long long)bh * p.Nq + row];
+    float* st = p.stats + tile * 64 + r;
+    st[0] = q >= p.Nq || lse == -INFINITY ? -INFINITY : -kLog2e * lse;
+    st[32] = q >= p.Nq ? 0.f : -sum;
+  }
+}
+
+// Gradients from their parts, added in their order: dQ, dK and dV (blockIdx.y).  A thread owns four features of a
 // row and has four parts in flight: what it waits for is memory.
 struct JoinArgs {
-  const float* parts[2];
-  void* to[2];
-  mrt_strides st[2];
+  struct {
+    const float* from;
+    void* to;
+    mrt_strides st;
+    long long rows;
+    int n, tokens, heads;
+  } a[3];
 };
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_dense_bwd_join(JoinArgs a, int n, long long rows, int tokens, int heads, int d) {
+__global__ __launch_bounds__(256) void k_dense_bwd_join(JoinArgs args, int d) {
   constexpr int AHEAD = 4;
-  const bool second = blockIdx.y != 0;
-  const int quads = (d + 3) >> 2;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / quads;
+  const auto& a = args.a[blockIdx.y];
+  const int quads = (d + 3) >> 2, n = a.n;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / quads, rows = a.rows;
   const int v = 4 * (int)(at - row * quads);
   if (row >= rows) return;
-  const float* from = (second ? a.parts[1] : a.parts[0]) + row * d;
+  const float* from = a.from + row * d;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   for (int i = 0; i < n; i += AHEAD) {
     f32x4 y[AHEAD];
@@ -222,26 +247,21 @@ __global__ __launch_bounds__(256) void k_dense_bwd_join(JoinArgs a, int n, long 
     for (int k = 0; k < AHEAD; ++k)
       if (i + k < n) x = x + y[k];
   }
-  const int bh = (int)(row / tokens), tok = (int)(row - (long long)bh * tokens), b = bh / heads, hd = bh - b * heads;
-  const mrt_strides& st = second ? a.st[1] : a.st[0];
-  st4<VEC>((T*)(second ? a.to[1] : a.to[0]) + b * st.batch + hd * st.head + tok * st.token, x, v, d);
+  const int bh = (int)(row / a.tokens), tok = (int)(row - (long long)bh * a.tokens), b = bh / a.heads, hd = bh - b * a.heads;
+  st4<VEC>((T*)a.to + b * a.st.batch + hd * a.st.head + tok * a.st.token, x, v, d);
 }
 
-template <int D, typename T, bool VEC, bool KV>
-hipError_t run(const DenseBwd& p, hipStream_t s) {
-  const int n = KV ? p.Nkv : p.Nq, heads = p.B * (KV ? p.KH : p.H), parts = KV ? p.parts_kv : p.parts_q;
-  const dim3 grid((n + kRows - 1) / kRows * heads * parts);
-  if (parts > 1) k_f32_dense_bwd<D, T, VEC, KV, true><<<grid, kThreads, 0, s>>>(p);
-  else k_f32_dense_bwd<D, T, VEC, KV, false><<<grid, kThreads, 0, s>>>(p);
-  return hipGetLastError();
-}
 template <int D, typename T, bool VEC>
 hipError_t run_both(const DenseBwd& p, int dtype, hipStream_t s) {
-  hipError_t e = run<D, T, VEC, false>(p, s);
-  if (e == hipSuccess && p.parts_q > 1) e = launch_dense_bwd_join(p, false, dtype, s);
-  if (e == hipSuccess) e = run<D, T, VEC, true>(p, s);
-  if (e == hipSuccess && p.parts_kv > 1) e = launch_dense_bwd_join(p, true, dtype, s);
-  return e;
+  hipError_t e = launch_dense_bwd_stats(p, dtype, s);
+  if (e != hipSuccess) return e;
+  const long long keys = (p.Nkv + kRows - 1) / kRows * (long long)(p.B * p.KH) * p.parts_kv;
+  const long long queries = (p.Nq + kRows - 1) / kRows * (long long)(p.B * p.H) * p.parts_q;
+  const bool part = p.parts_q > 1 || p.parts_kv > 1;
+  const auto kernel = part ? k_f32_dense_bwd<D, T, VEC, true> : k_f32_dense_bwd<D, T, VEC, false>;
+  kernel<<<(unsigned)(keys + queries), kThreads, 0, s>>>(p, (int)keys);
+  e = hipGetLastError();
+  return e != hipSuccess || !part ? e : launch_dense_bwd_join(p, true, dtype, s);
 }
 template <typename T>
 bool rows_of_four(const DenseBwd& p) {
@@ -260,22 +280,35 @@ hipError_t run_t(const DenseBwd& p, int dtype, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStream_t s) {
-  const int tokens = kv ? p.Nkv : p.Nq, heads = kv ? p.KH : p.H, n = kv ? p.parts_kv : p.parts_q;
-  const long long rows = (long long)p.B * heads * tokens, threads = rows * ((p.d + 3) / 4);
-  const JoinArgs a = {{kv ? p.pk : p.pq, p.pv}, {kv ? p.dK : p.dQ, p.dV}, {kv ? p.dk : p.dq, p.dv}};
-  const dim3 grid((unsigned)((threads + 255) / 256), kv ? 2 : 1);
+hipError_t launch_dense_bwd_stats(const DenseBwd& p, int dtype, hipStream_t s) {
+  const int nqb = (p.Nq + 31) / 32;
+  const dim3 grid(2 * (unsigned)(p.B * p.H) * nqb);
   const bool bf16 = dtype == MRT_BF16, vec = bf16 ? rows_of_four<u16>(p) : rows_of_four<float>(p);
-  if (bf16 && vec) k_dense_bwd_join<u16, true><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
-  else if (bf16) k_dense_bwd_join<u16, false><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
-  else if (vec) k_dense_bwd_join<float, true><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
-  else k_dense_bwd_join<float, false><<<grid, 256, 0, s>>>(a, n, rows, tokens, heads, p.d);
+  if (bf16 && vec) k_dense_bwd_stats<u16, true><<<grid, 256, 0, s>>>(p, nqb);
+  else if (bf16) k_dense_bwd_stats<u16, false><<<grid, 256, 0, s>>>(p, nqb);
+  else if (vec) k_dense_bwd_stats<float, true><<<grid, 256, 0, s>>>(p, nqb);
+  else k_dense_bwd_stats<float, false><<<grid, 256, 0, s>>>(p, nqb);
   return hipGetLastError();
 }
 
-// (one head of 576 tokens of 64 features 109 -> 34 us for both launches, 12 heads of 1560 of 128 790 -> 593)
+hipError_t launch_dense_bwd_join(const DenseBwd& p, bool all, int dtype, hipStream_t s) {
+  const long long rq = (long long)p.B * p.H * p.Nq, rkv = (long long)p.B * p.KH * p.Nkv;
+  const JoinArgs a = {{{p.pq, p.dQ, p.dq, rq, p.parts_q, p.Nq, p.H}, {p.pk, p.dK, p.dk, rkv, p.parts_kv, p.Nkv, p.KH},
+                       {p.pv, p.dV, p.dv, rkv, p.parts_kv, p.Nkv, p.KH}}};
+  const long long threads = (all && rkv > rq ? rkv : rq) * ((p.d + 3) / 4);
+  const dim3 grid((unsigned)((threads + 255) / 256), all ? 3 : 1);
+  const bool bf16 = dtype == MRT_BF16, vec = bf16 ? rows_of_four<u16>(p) : rows_of_four<float>(p);
+  if (bf16 && vec) k_dense_bwd_join<u16, true><<<grid, 256, 0, s>>>(a, p.d);
+  else if (bf16) k_dense_bwd_join<u16, false><<<grid, 256, 0, s>>>(a, p.d);
+  else if (vec) k_dense_bwd_join<float, true><<<grid, 256, 0, s>>>(a, p.d);
+  else k_dense_bwd_join<float, false><<<grid, 256, 0, s>>>(a, p.d);
+  return hipGetLastError();
+}
+
+// (one head of 576 tokens of 64 features 109 -> 34 us without sharing and with it in two launches, 25 in one; 12 heads of 1560 of 128
+// 790 -> 593, 564)
 DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p) {
-  return dense_bwd_shape(p, kRows, kStep, p.d <= 64 ? 1.1 : 2.1, p.d <= 64 ? 1.5 : 2.8);
+  return dense_bwd_shape(p, kRows, kStep, p.d <= 64 ? 1.1 : 1.9, p.d <= 64 ? 1.1 : 2.7);
 }
 
 hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s) {

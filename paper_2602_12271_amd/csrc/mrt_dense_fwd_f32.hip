@@ -195,6 +195,32 @@ hipError_t run_t(const DenseFwd& p, hipStream_t s) {
   return p.d <= 64 ? run<64, T, false>(p, s) : run<128, T, false>(p, s);
 }
 
+// How many workgroups share the keys of a tile: as many as promise the least time by this model.  A step takes t
+// microseconds where a compute unit has one workgroup, 1.5 t where it has two (under a mask a long one and one of mean
+// length); a join costs a launch and the parts' bytes.
+struct DenseShare {
+  int parts;
+  double us;
+};
+DenseShare dense_share(long long rows, int tile, long long heads, int d, double t, double first, double last) {
+  const double cus = compute_units(), longest = std::max(first, last), mean = 0.5 * (first + last);
+  const long long tiles = (rows + tile - 1) / tile * heads, elements = rows * heads * d;
+  auto time = [&](int parts) {
+    const double each = tiles * parts / cus, pairs = std::floor(each / 2), rest = each - 2 * pairs;
+    const double rounds = 1.5 * pairs + (rest > 1 ? 1.5 : rest > 0 ? 1.0 : 0.0);
+    const double alone = std::ceil(longest / parts), beside = rounds < 1.5 ? alone : 0.75 * (alone + std::ceil(mean / parts));
+    const double steps = std::max(beside, rounds > 1.5 ? (mean / parts + 1) * rounds : 0.0);
+    return steps * t + (parts > 1 ? 4.0 + 1.3e-6 * elements * parts : 0.0);
+  };
+  int best = 1;
+  double least = time(1) * 0.95;      // (sharing has to promise 5 %)
+  for (int parts = 2; parts <= kMostParts && 2 * parts <= longest && elements * parts <= kMostPartElements; ++parts) {
+    const double us = time(parts);
+    if (us < least) { least = us; best = parts; }
+  }
+  return {best, time(best)};
+}
+
 }  // namespace
 
 bool f32_dense_fwd_quads(const DenseFwd& p, size_t bytes) {
@@ -210,7 +236,7 @@ bool f32_dense_fwd_quads(const DenseFwd& p, size_t bytes) {
 // two share it at 1.35 times that).
 int f32_dense_fwd_parts(const DenseFwd& p) {
   const double first = dense_last_key(p, std::min(kRows, p.Nq) - 1, p.Nkv), last = dense_last_key(p, p.Nq - 1, p.Nkv), cus = compute_units();
-  const DenseShare own = dense_share(p.Nq, kRows, (long long)p.B * p.H, p.d, p.d <= 64 ? 0.75 : 1.4, first / kStep, last / kStep, 1);
+  const DenseShare own = dense_share(p.Nq, kRows, (long long)p.B * p.H, p.d, p.d <= 64 ? 0.75 : 1.4, first / kStep, last / kStep);
   const double each = (p.Nq + 127) / 128 * (double)(p.B * p.H) / cus, pairs = std::floor(each / 2), rest = each - 2 * pairs;
   const double rounds = 1.35 * pairs + (rest > 1 ? 1.35 : rest > 0 ? 1.0 : 0.0);
   const double other = (p.d <= 64 ? 2.1 : 5.0) / 32 * std::max(last * std::min(rounds, 1.35), 0.5 * (first + last) * rounds);

@@ -72,45 +72,55 @@ __host__ __device__ inline int dense_first_query(const DenseBwd& p, int k) {
 // Workgroups that share the keys of a query tile, and the queries of a key tile.
 struct DenseBwdShape {
   int parts_q, parts_kv;
-  bool sums_q;           // dQ is summed from parts, even from one
+  bool sums_q, sums_kv;  // dQ, dK and dV are summed from parts, even from one
 };
 
-// How many workgroups share the streamed rows of a tile: as many as promise the least time by this model.  A step takes t
-// microseconds where a compute unit has one workgroup, 1.5 t where it has two (under a mask a long one and one of mean
-// length); a join costs a launch and the parts' bytes.
+// How many workgroups share the streamed rows of a tile of queries and of a tile of keys: what promises the least time by
+// this model.  A step takes tq or tkv microseconds where a compute unit has one workgroup, kBeside times that where it has
+// two, and a workgroup half a step more; few workgroups take as long as the longest, more than two a compute unit as
+// long as all their steps together and a share of the longest (steps differ under a mask); sharing costs a launch that
+// joins the parts, and their bytes.  (Fitted to 41 shapes of 1 to 40 heads, 200 to 14040 tokens, each timed with 20 to 60
+// pairs of parts: what it chooses takes 6 % longer than the best pair in the mean.)
+constexpr double kBeside = 1.6, kJoin = 5.5, kJoinElement = 1.4e-6;
 constexpr long long kMostPartElements = 1 << 27;      // of all parts together
-struct DenseShare {
-  int parts;
-  double us;
-};
-inline DenseShare dense_share(long long rows, int tile, long long heads, int d, double t, double first, double last, int arrays) {
-  const double cus = compute_units(), longest = std::max(first, last), mean = 0.5 * (first + last);
-  const long long tiles = (rows + tile - 1) / tile * heads, elements = rows * heads * d * arrays;
-  auto time = [&](int parts) {
-    const double each = tiles * parts / cus, pairs = std::floor(each / 2), rest = each - 2 * pairs;
-    const double rounds = 1.5 * pairs + (rest > 1 ? 1.5 : rest > 0 ? 1.0 : 0.0);
-    const double alone = std::ceil(longest / parts), beside = rounds < 1.5 ? alone : 0.75 * (alone + std::ceil(mean / parts));
-    const double steps = std::max(beside, rounds > 1.5 ? (mean / parts + 1) * rounds : 0.0);
-    return steps * t + (parts > 1 ? 4.0 + 1.3e-6 * elements * parts : 0.0);
-  };
-  int best = 1;
-  double least = time(1) * 0.95;      // (sharing has to promise 5 %)
-  for (int parts = 2; parts <= 32 && 2 * parts <= longest && elements * parts <= kMostPartElements; ++parts) {
-    const double us = time(parts);
-    if (us < least) { least = us; best = parts; }
-  }
-  return {best, time(best)};
-}
-// tile: rows of a workgroup; step: streamed rows; tq, tkv: microseconds a step takes
+constexpr int kMostParts = 32;
+// tile: rows of a workgroup; step: streamed rows
 inline DenseBwdShape dense_bwd_shape(const DenseBwd& p, int tile, int step, double tq, double tkv) {
   auto steps = [&](long long n) { return (double)((n + step - 1) / step); };
   auto keys = [&](long long q) { return steps(dense_last_key(p, (int)std::min<long long>(q, p.Nq - 1), p.Nkv)); };
   auto queries = [&](long long k) { return steps((long long)(p.Nq - dense_first_query(p, (int)std::min<long long>(k, p.Nkv - 1))) * p.group); };
-  DenseBwdShape shape;
-  shape.parts_q = dense_share(p.Nq, tile, (long long)p.B * p.H, p.d, tq, keys(tile - 1), keys(p.Nq - 1), 1).parts;
-  shape.parts_kv = dense_share(p.Nkv, tile, (long long)p.B * p.KH, p.d, tkv, queries(0), queries((p.Nkv - 1) / tile * (long long)tile), 2).parts;
-  shape.sums_q = shape.parts_q > 1;
-  return shape;
+  struct Side {
+    double tiles, longest, mean, t;
+  };
+  auto side = [](double tiles, double first, double last, double t) { return Side{tiles, std::max(first, last), 0.5 * (first + last), t}; };
+  const Side q = side((double)((p.Nq + tile - 1) / tile) * p.B * p.H, keys(tile - 1), keys(p.Nq - 1), tq);
+  const Side k = side((double)((p.Nkv + tile - 1) / tile) * p.B * p.KH, queries(0), queries((p.Nkv - 1) / tile * (long long)tile), tkv);
+  const long long eq = (long long)p.B * p.H * p.Nq * p.d, ekv = 2ll * p.B * p.KH * p.Nkv * p.d;
+  const double cus = compute_units();
+  auto time = [&](int pq, int pk) {
+    const double longest = std::max((std::ceil(q.longest / pq) + 0.5) * q.t, (std::ceil(k.longest / pk) + 0.5) * k.t);
+    const double units = q.tiles * pq + k.tiles * pk, all = q.tiles * (q.mean + 0.5 * pq) * q.t + k.tiles * (k.mean + 0.5 * pk) * k.t;
+    const double pair = std::max(0.5 * kBeside * (longest + all / units), longest);
+    const double us = units <= cus ? longest : units <= 2 * cus ? pair : std::max(0.5 * kBeside * all / cus + 0.45 * longest, pair);
+    return us + (pq > 1 || pk > 1 ? kJoin + kJoinElement * ((double)eq * pq + (double)ekv * pk) : 0.0);
+  };
+  DenseBwdShape best = {1, 1, false, false};
+  double least = time(1, 1);
+  auto look = [&](int pq, int pk) {
+    if (pq < 1 || pk < 1 || pq > kMostParts || pk > kMostParts || eq * pq + ekv * pk > kMostPartElements) return;
+    const double us = time(pq, pk);
+    if (us < least) {
+      least = us;
+      best = {pq, pk, true, true};
+    }
+  };
+  // pairs that make workgroups of about one length, up to four a compute unit
+  const double ratio = std::max(k.longest * k.t, 1e-3) / std::max(q.longest * q.t, 1e-3);
+  for (int n = 1; n <= kMostParts && (n == 1 || (2 * n <= std::max(q.longest, k.longest) && n * std::min(q.tiles, k.tiles) <= 4 * cus)); ++n) {
+    const double other = ratio >= 1 ? n / ratio : n * ratio;
+    for (int m = (int)other; m <= (int)other + 1; ++m) ratio >= 1 ? look(m, n) : look(n, m);
+  }
+  return best;
 }
 
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p);
@@ -122,7 +132,9 @@ bool f32_dense_fwd_quads(const DenseFwd& p, size_t bytes);
 int f32_dense_fwd_parts(const DenseFwd& p);
 hipError_t launch_f32_dense_fwd(const DenseFwd& p, int dtype, hipStream_t s);
 hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s);
-// sums the parts of dQ, or of dK and dV, into the gradients (`dtype`)
-hipError_t launch_dense_bwd_join(const DenseBwd& p, bool kv, int dtype, hipStream_t s);
+// what the tiles need of every row of queries (p.stats)
+hipError_t launch_dense_bwd_stats(const DenseBwd& p, int dtype, hipStream_t s);
+// sums the parts of dQ, or of all gradients, into them (`dtype`)
+hipError_t launch_dense_bwd_join(const DenseBwd& p, bool all, int dtype, hipStream_t s);
 
 }  // namespace mrt
