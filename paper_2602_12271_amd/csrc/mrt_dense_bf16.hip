@@ -99,17 +99,13 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int wq = wave % WQ, wk = wave / WQ;
   const bool second = wave >= kDenseWaves / 2;           // the half that runs one phase behind
-  int most_keys = p.Nkv;
-  auto visible = [&](int q) {
-    const int n = dense_visible(p, q);
-    return SAVE && n > most_keys ? most_keys : n;
-  };
+  auto visible = [&](int q) { return dense_visible(p, q); };
   // Workgroups reach the eight XCDs in turn: hand each XCD a contiguous run of (head, query tile)
   // units, so that the units that stream the same keys share its L2.  (Under a mask that gives the
   // query tiles of a head different key counts the natural order spreads the long ones evenly.)
   const int nx = (p.Nq + WGQ - 1) / WGQ, total = gridDim.x, xcd = blockIdx.x & 7;
   int unit = blockIdx.x;
-  if (dense_visible(p, 0) == dense_visible(p, p.Nq - 1)) unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
+  if (visible(0) == visible(p.Nq - 1)) unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
   const int run = unit / nx, q0 = (unit - run * nx) * WGQ;         // run = (head, part)
   const int bh = PART ? run / parts.n : run, part = PART ? run - bh * parts.n : 0;
   const int b = bh / p.H, hd = bh - b * p.H;
@@ -117,8 +113,8 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
   const int qw0 = q0 + 16 * QT * wq;                      // this wave's first query
   if constexpr (SAVE) {
     kvh = hd / save.group;
-    if (save.kv_len) most_keys = min(max(save.kv_len[b], 0), p.Nkv);
-    if (most_keys == 0) {                                 // an empty sequence
+    if (save.kv_len) p.Nkv = __builtin_amdgcn_readfirstlane(min(max(save.kv_len[b], 0), p.Nkv));
+    if (p.Nkv == 0) {                                     // an empty sequence
       const long long row0 = PART ? ((long long)part * (total / (nx * parts.n)) + bh) * p.Nq : 0;
       for (int i = tid; i < WGQ * D; i += kDenseThreads) {
         const int q = q0 + i / D, f = i % D;
