@@ -15,6 +15,7 @@ from __future__ import annotations
 import argparse
 import ctypes
 import json
+import math
 import os
 import sys
 import time
@@ -249,6 +250,74 @@ def bench_backward(args, wl, lib, pkg, syn, torch, np, host, dev, prob, stream):
     }))
 
 
+def bench_dense_step(args, wl, pkg, syn, torch, np, host, dev):
+    """The dense attention's training step on the workload's tokens: rotary positions of Q and K, the forward call that
+    keeps its row statistics, the backward call, the turn back of the gradients."""
+    Qh, Kh, Vh = host
+    Q, K, V = dev
+    dOh = np.random.default_rng(1234).standard_normal(Qh.shape).astype(np.float32)
+    if wl.dtype == "bf16":
+        dOh = syn.round_to_bf16(dOh)
+    dO = torch.from_numpy(dOh).to(Q.device).to(Q.dtype)
+    grid = dict(f_q=wl.f_q, f_kv=wl.f_kv, h=wl.h, w=wl.w, q_frame_offset=wl.q_frame_offset)
+    mask = dict(grid, causal_chunk=wl.causal_chunk, scale=wl.scale)
+
+    def step():
+        q, k = pkg.rotary_fwd(Q, K, **grid)
+        O, lse = pkg.dense_attn_fwd_save(q, k, V, **mask)
+        dq, dk, dV = pkg.dense_attn_bwd(q, k, V, O, dO, lse, **mask)
+        return (q, k), (O, lse), (dq, dk, dV), pkg.rotary_bwd(dq, dk, **grid)
+
+    steps, warmup = min(args.steps, 50), min(args.warmup, 5)
+    for _ in range(warmup):
+        out = step()
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(steps):
+        out = step()
+    torch.cuda.synchronize()
+    ms = (time.perf_counter() - t0) * 1e3 / steps
+    (q, k), (O, lse), grads, _ = out
+    parts = {}
+    for name, fn in (("rotary_fwd", lambda: pkg.rotary_fwd(Q, K, **grid)), ("fwd_save", lambda: pkg.dense_attn_fwd_save(q, k, V, **mask)),
+                     ("bwd", lambda: pkg.dense_attn_bwd(q, k, V, O, dO, lse, **mask)), ("rotary_bwd", lambda: pkg.rotary_bwd(*grads[:2], **grid))):
+        fn()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(steps):
+            fn()
+        torch.cuda.synchronize()
+        parts[name + "_ms"] = (time.perf_counter() - t0) * 1e3 / steps
+    parity = None
+    if not args.no_cpu_baseline:
+        # head 0 in 64 bits from the rotated inputs
+        a, b, v, g = (x[0, 0].double().cpu() for x in (q, k, V, dO))
+        hw = wl.h * wl.w
+        z = wl.scale * a @ b.t()
+        if wl.causal_chunk:
+            chunk = lambda n, first: (first + torch.arange(n) // hw) // wl.causal_chunk       # noqa: E731
+            z.masked_fill_(chunk(wl.n_kv, 0)[None] > chunk(wl.n_q, wl.q_frame_offset)[:, None], -math.inf)
+        P = torch.softmax(z, -1)
+        o = P @ v
+        dS = P * (g @ v.t() - (g * o).sum(-1, keepdim=True))
+        want = (wl.scale * dS @ b, wl.scale * dS.t() @ a, P.t() @ g)
+        parity = max(float((x[0, 0].double().cpu() - y).norm() / y.norm()) for x, y in zip((*grads, O), (*want, o)))
+    flops = 3.5 * dense_flops(wl)            # two products forward, five backward
+    peak = 2500.0 if wl.dtype == "bf16" else 157.3
+    ach = flops / (ms / 1e3) / 1e12
+    print(json.dumps({
+        "metric": "dense_training_step_ms", "value": ms, "unit": "ms/step", "n_gpus": 1, "steps": steps, "warmup": warmup,
+        "ms_per_step": ms, "higher_is_better": False, "scaling": "weak", "vs_baseline": None, "dtype": wl.dtype,
+        "data": "synthetic",
+        "config": {"workload": f"{wl.name} dense training step: {wl.heads} heads x d{wl.head_dim}, N_q={wl.n_q}, N_kv={wl.n_kv}",
+                   **parts},
+        "roofline": {"bound": "mfma", "achieved": ach, "peak": peak, "unit": "TFLOP/s", "frac": ach / peak,
+                     "algorithmic_gflop": flops / 1e9,
+                     "note": "two products forward and five backward; the kernels form two of the five twice, once per side"},
+        "parity_max_rel_err_head0": parity,
+    }))
+
+
 def measure_forward(wl, env, steps, warmup, *, head_groups=0, settle_s=0.0, with_dense=True, with_oracle=True,
                     oracle_budget_s=0.0, calibration_copy_mb=0, copy_gbs=None):
     """One workload through monarch_attn_fwd: whole-call time (default launch configuration),
@@ -457,8 +526,9 @@ def main():
     ap.add_argument("--also", default=None,
                     help="comma-separated workloads measured after the headline one and reported under "
                          "other_workloads (default: C2,C3,C4 when the headline is C1; 'none' for none)")
-    ap.add_argument("--op", default="fwd", choices=["fwd", "bwd"],
-                    help="fwd: the forward operator (the headline metric); bwd: the backward pass")
+    ap.add_argument("--op", default="fwd", choices=["fwd", "bwd", "dense-step"],
+                    help="fwd: the forward operator (the headline metric); bwd: the backward pass; dense-step: rotary "
+                         "positions and the dense attention's forward and backward pass")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-dense", action="store_true")
     ap.add_argument("--head-groups", type=int, default=0,
@@ -486,13 +556,15 @@ def main():
     env = (np, torch, pkg, binding, syn, lib)
     wl = syn.WORKLOADS[args.workload]
 
-    if args.op == "bwd":
+    if args.op != "fwd":
         dev = torch.device("cuda:0")
         if args.head_groups:
             binding.set_head_groups(args.head_groups)
         tdt = torch.float32 if wl.dtype == "f32" else torch.bfloat16
         Qh, Kh, Vh = syn.make_inputs(wl)
         Q, K, V = (torch.from_numpy(x).to(dev).to(tdt) for x in (Qh, Kh, Vh))
+        if args.op == "dense-step":
+            return bench_dense_step(args, wl, pkg, syn, torch, np, (Qh, Kh, Vh), (Q, K, V))
         prob = binding._torch_problem(Q, K, V, torch.empty_like(Q), wl.f_q, wl.f_kv, wl.h, wl.w,
                                       wl.q_frame_offset, wl.scale, pkg.MRT_COMPUTE_DEFAULT, wl.assign, wl.tile_h)
         stream = torch.cuda.current_stream(dev).cuda_stream
