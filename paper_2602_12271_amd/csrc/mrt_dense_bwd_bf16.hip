@@ -6,7 +6,8 @@
 // partial arrays as there are key tiles (half a gigabyte each way for 12 heads of 4680 tokens).  A small launch before it
 // leaves what both need of a row, -log2(e) lse and -delta.  (The two kinds in launches of their own, the first of which
 // left these: us of a call, two launches | one: one head of 4680 tokens 86 | 68, 12 of 1560 tokens 105 | 87, 40 of 1800
-// tokens 299 | 269, batch of 3, 4 heads of 782 tokens of 64 features 42 | 28, 12 heads of 4680 tokens 444 | 445.)
+// tokens 299 | 269, batch of 3, 4 heads of 782 tokens of 64 features 42 | 28, 12 heads of 4680 tokens 444 | 445, 425 with
+// two workgroups to a tile of queries, which the launch of one kind did not gain by.)
 //
 // A wave owns 32 rows: their operands and gradients stay in registers, the streamed rows pass through an LDS ring 32 a
 // step, loaded by instructions that write LDS directly, several steps ahead.  Logits have the streamed rows on the M
@@ -473,11 +474,11 @@ __device__ __forceinline__ void bwd_keys(const DenseBwd& p, int unit) {
 }
 
 // One launch for both: the key tiles, whose steps are the longer ones, come first.
-template <int D, bool PART>
+template <int D, bool PART_Q, bool PART_KV>
 __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd(DenseBwd p, int key_units) {
   const int unit = blockIdx.x;
-  if (unit < key_units) bwd_keys<D, PART>(p, unit);
-  else bwd_queries<D, PART>(p, unit - key_units);
+  if (unit < key_units) bwd_keys<D, PART_KV>(p, unit);
+  else bwd_queries<D, PART_Q>(p, unit - key_units);
 }
 
 // ---- few queries -------------------------------------------------------------------------------
@@ -690,7 +691,7 @@ hipError_t run(const DenseBwd& p, hipStream_t s) {
     if (e != hipSuccess) return e;
     k_bf16_dense_bwd_few<D><<<(unsigned)(p.B * p.KH * p.parts_q), kThreads, lds, s>>>(p);
     e = hipGetLastError();
-    return e != hipSuccess ? e : launch_dense_bwd_join(p, false, MRT_BF16, s);
+    return e != hipSuccess ? e : launch_dense_bwd_join(p, true, false, MRT_BF16, s);
   }
   constexpr int lds = Stream<D, true>::RING;
   static_assert(lds >= Stream<D, false>::RING, "the ring of either");
@@ -698,19 +699,20 @@ hipError_t run(const DenseBwd& p, hipStream_t s) {
   if (e != hipSuccess) return e;
   const long long keys = (p.Nkv + kRows - 1) / kRows * (long long)(p.B * p.KH) * p.parts_kv;
   const long long queries = (p.Nq + kRows - 1) / kRows * (long long)(p.B * p.H) * p.parts_q;
-  const bool part = p.parts_q > 1 || p.parts_kv > 1;
-  const auto kernel = part ? k_bf16_dense_bwd<D, true> : k_bf16_dense_bwd<D, false>;
+  const bool pq = p.parts_q > 1, pkv = p.parts_kv > 1;
+  const auto kernel = pq ? pkv ? k_bf16_dense_bwd<D, true, true> : k_bf16_dense_bwd<D, true, false>
+                         : pkv ? k_bf16_dense_bwd<D, false, true> : k_bf16_dense_bwd<D, false, false>;
   e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   kernel<<<(unsigned)(keys + queries), kThreads, lds, s>>>(p, (int)keys);
   e = hipGetLastError();
-  return e != hipSuccess || !part ? e : launch_dense_bwd_join(p, true, MRT_BF16, s);
+  return e != hipSuccess || !(pq || pkv) ? e : launch_dense_bwd_join(p, pq, pkv, MRT_BF16, s);
 }
 
 }  // namespace
 
 DenseBwdShape bf16_dense_bwd_shape(const DenseBwd& p) {
-  if (!few_queries(p)) return dense_bwd_shape(p, kRows, kStep, p.d == 64 ? 0.35 : 0.72, p.d == 64 ? 0.65 : 1.05);
+  if (!few_queries(p)) return dense_bwd_shape(p, kRows, kStep, p.d == 64 ? 0.57 : 0.80, p.d == 64 ? 0.59 : 1.08);
   // few queries: runs of key tiles that fill the chip in whole rounds (a round costs a workgroup as much as half a tile)
   const long long cus = compute_units(), heads = (long long)p.B * p.KH, tiles = (p.Nkv + 31) / 32;
   double least = INFINITY;

@@ -182,12 +182,12 @@ __device__ __forceinline__ void bwd_tile(const DenseBwd& p, int unit, float* lds
 }
 
 // One launch for both: the key tiles, whose steps are the longer ones, come first.
-template <int D, typename T, bool VEC, bool PART>
+template <int D, typename T, bool VEC, bool PART_Q, bool PART_KV>
 __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p, int key_units) {
   __shared__ __attribute__((aligned(16))) float lds[2 * kSlot<D>];
   const int unit = blockIdx.x;
-  if (unit < key_units) bwd_tile<D, T, VEC, true, PART>(p, unit, lds);
-  else bwd_tile<D, T, VEC, false, PART>(p, unit - key_units, lds);
+  if (unit < key_units) bwd_tile<D, T, VEC, true, PART_KV>(p, unit, lds);
+  else bwd_tile<D, T, VEC, false, PART_Q>(p, unit - key_units, lds);
 }
 
 // What the tiles need of a row of queries: -log2(e) lse (-infinity where it sees no key: weights of zero) and -delta,
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void k_dense_bwd_stats(DenseBwd p, int nqb) {
   }
 }
 
-// Gradients from their parts, added in their order: dQ, dK and dV (blockIdx.y).  A thread owns four features of a
+// Gradients from their parts, added in their order: those of dQ, dK and dV that have some (blockIdx.y).  A thread owns four features of a
 // row and has four parts in flight: what it waits for is memory.
 struct JoinArgs {
   struct {
@@ -257,11 +257,12 @@ hipError_t run_both(const DenseBwd& p, int dtype, hipStream_t s) {
   if (e != hipSuccess) return e;
   const long long keys = (p.Nkv + kRows - 1) / kRows * (long long)(p.B * p.KH) * p.parts_kv;
   const long long queries = (p.Nq + kRows - 1) / kRows * (long long)(p.B * p.H) * p.parts_q;
-  const bool part = p.parts_q > 1 || p.parts_kv > 1;
-  const auto kernel = part ? k_f32_dense_bwd<D, T, VEC, true> : k_f32_dense_bwd<D, T, VEC, false>;
+  const bool pq = p.parts_q > 1, pkv = p.parts_kv > 1;
+  const auto kernel = pq ? pkv ? k_f32_dense_bwd<D, T, VEC, true, true> : k_f32_dense_bwd<D, T, VEC, true, false>
+                         : pkv ? k_f32_dense_bwd<D, T, VEC, false, true> : k_f32_dense_bwd<D, T, VEC, false, false>;
   kernel<<<(unsigned)(keys + queries), kThreads, 0, s>>>(p, (int)keys);
   e = hipGetLastError();
-  return e != hipSuccess || !part ? e : launch_dense_bwd_join(p, true, dtype, s);
+  return e != hipSuccess || !(pq || pkv) ? e : launch_dense_bwd_join(p, pq, pkv, dtype, s);
 }
 template <typename T>
 bool rows_of_four(const DenseBwd& p) {
@@ -291,12 +292,17 @@ hipError_t launch_dense_bwd_stats(const DenseBwd& p, int dtype, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_dense_bwd_join(const DenseBwd& p, bool all, int dtype, hipStream_t s) {
+hipError_t launch_dense_bwd_join(const DenseBwd& p, bool q, bool kv, int dtype, hipStream_t s) {
   const long long rq = (long long)p.B * p.H * p.Nq, rkv = (long long)p.B * p.KH * p.Nkv;
-  const JoinArgs a = {{{p.pq, p.dQ, p.dq, rq, p.parts_q, p.Nq, p.H}, {p.pk, p.dK, p.dk, rkv, p.parts_kv, p.Nkv, p.KH},
-                       {p.pv, p.dV, p.dv, rkv, p.parts_kv, p.Nkv, p.KH}}};
-  const long long threads = (all && rkv > rq ? rkv : rq) * ((p.d + 3) / 4);
-  const dim3 grid((unsigned)((threads + 255) / 256), all ? 3 : 1);
+  JoinArgs a;
+  int n = 0;
+  if (q) a.a[n++] = {p.pq, p.dQ, p.dq, rq, p.parts_q, p.Nq, p.H};
+  if (kv) {
+    a.a[n++] = {p.pk, p.dK, p.dk, rkv, p.parts_kv, p.Nkv, p.KH};
+    a.a[n++] = {p.pv, p.dV, p.dv, rkv, p.parts_kv, p.Nkv, p.KH};
+  }
+  const long long threads = (q && kv ? std::max(rq, rkv) : q ? rq : rkv) * ((p.d + 3) / 4);
+  const dim3 grid((unsigned)((threads + 255) / 256), n);
   const bool bf16 = dtype == MRT_BF16, vec = bf16 ? rows_of_four<u16>(p) : rows_of_four<float>(p);
   if (bf16 && vec) k_dense_bwd_join<u16, true><<<grid, 256, 0, s>>>(a, p.d);
   else if (bf16) k_dense_bwd_join<u16, false><<<grid, 256, 0, s>>>(a, p.d);
@@ -305,10 +311,10 @@ hipError_t launch_dense_bwd_join(const DenseBwd& p, bool all, int dtype, hipStre
   return hipGetLastError();
 }
 
-// (one head of 576 tokens of 64 features 109 -> 34 us without sharing and with it in two launches, 25 in one; 12 heads of 1560 of 128
-// 790 -> 593, 564)
+// (us without sharing, shared in two launches, and in one: one head of 576 tokens of 64 features 109 | 34 | 25, 12 heads of
+// 1560 tokens of 128 790 | 593 | 550)
 DenseBwdShape f32_dense_bwd_shape(const DenseBwd& p) {
-  return dense_bwd_shape(p, kRows, kStep, p.d <= 64 ? 1.1 : 1.9, p.d <= 64 ? 1.1 : 2.7);
+  return dense_bwd_shape(p, kRows, kStep, p.d <= 64 ? 0.95 : 1.84, p.d <= 64 ? 1.33 : 2.73);
 }
 
 hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s) {

@@ -72,16 +72,18 @@ __host__ __device__ inline int dense_first_query(const DenseBwd& p, int k) {
 // Workgroups that share the keys of a query tile, and the queries of a key tile.
 struct DenseBwdShape {
   int parts_q, parts_kv;
-  bool sums_q, sums_kv;  // dQ, dK and dV are summed from parts, even from one
+  bool sums_q, sums_kv;  // dQ, dK and dV are summed from parts
 };
 
 // How many workgroups share the streamed rows of a tile of queries and of a tile of keys: what promises the least time by
 // this model.  A step takes tq or tkv microseconds where a compute unit has one workgroup, kBeside times that where it has
-// two, and a workgroup half a step more; few workgroups take as long as the longest, more than two a compute unit as
-// long as all their steps together and a share of the longest (steps differ under a mask); sharing costs a launch that
-// joins the parts, and their bytes.  (Fitted to 41 shapes of 1 to 40 heads, 200 to 14040 tokens, each timed with 20 to 60
-// pairs of parts: what it chooses takes 6 % longer than the best pair in the mean.)
-constexpr double kBeside = 1.6, kJoin = 5.5, kJoinElement = 1.4e-6;
+// two, and a workgroup a step more than it has.  Few workgroups take as long as the longest; more than two a compute unit
+// as long as all their steps together and some of the longest, mostly of queries, which come last (steps differ under a
+// mask).  Sharing costs a launch that joins the parts, and their bytes; it evens out more than the model knows, so that a
+// call without it counts 3 % more.  (Fitted to 41 shapes of 1 to 40 heads, 200 to 14040 tokens, each timed with 20
+// to 60 pairs of parts: what it chooses takes 3 % longer than the best pair in the mean.  us of unshared and shared calls:
+// 12 heads of 4680 tokens 456 | 428, two to a tile of queries; one head of 4680 tokens 151 | 67, six and seven.)
+constexpr double kBeside = 1.6, kLastQueries = 0.25, kLastKeys = 0.06, kJoin = 6.0, kJoinElement = 1.35e-6, kUnshared = 1.03;
 constexpr long long kMostPartElements = 1 << 27;      // of all parts together
 constexpr int kMostParts = 32;
 // tile: rows of a workgroup; step: streamed rows
@@ -97,28 +99,32 @@ inline DenseBwdShape dense_bwd_shape(const DenseBwd& p, int tile, int step, doub
   const Side k = side((double)((p.Nkv + tile - 1) / tile) * p.B * p.KH, queries(0), queries((p.Nkv - 1) / tile * (long long)tile), tkv);
   const long long eq = (long long)p.B * p.H * p.Nq * p.d, ekv = 2ll * p.B * p.KH * p.Nkv * p.d;
   const double cus = compute_units();
+  auto elements = [&](int pq, int pk) { return (pq > 1 ? eq * pq : 0) + (pk > 1 ? ekv * pk : 0); };
   auto time = [&](int pq, int pk) {
-    const double longest = std::max((std::ceil(q.longest / pq) + 0.5) * q.t, (std::ceil(k.longest / pk) + 0.5) * k.t);
-    const double units = q.tiles * pq + k.tiles * pk, all = q.tiles * (q.mean + 0.5 * pq) * q.t + k.tiles * (k.mean + 0.5 * pk) * k.t;
+    const double lq = (std::ceil(q.longest / pq) + 1) * q.t, lk = (std::ceil(k.longest / pk) + 1) * k.t, longest = std::max(lq, lk);
+    const double units = q.tiles * pq + k.tiles * pk, all = q.tiles * (q.mean + pq) * q.t + k.tiles * (k.mean + pk) * k.t;
     const double pair = std::max(0.5 * kBeside * (longest + all / units), longest);
-    const double us = units <= cus ? longest : units <= 2 * cus ? pair : std::max(0.5 * kBeside * all / cus + 0.45 * longest, pair);
-    return us + (pq > 1 || pk > 1 ? kJoin + kJoinElement * ((double)eq * pq + (double)ekv * pk) : 0.0);
+    if (units <= cus) return longest;
+    return units <= 2 * cus ? pair : std::max(0.5 * kBeside * all / cus + kLastQueries * lq + kLastKeys * lk, pair);
   };
   DenseBwdShape best = {1, 1, false, false};
-  double least = time(1, 1);
+  double least = kUnshared * time(1, 1);
   auto look = [&](int pq, int pk) {
-    if (pq < 1 || pk < 1 || pq > kMostParts || pk > kMostParts || eq * pq + ekv * pk > kMostPartElements) return;
-    const double us = time(pq, pk);
+    const long long n = elements(pq, pk);
+    if (pq < 1 || pk < 1 || pq > kMostParts || pk > kMostParts || n == 0 || n > kMostPartElements) return;
+    const double us = time(pq, pk) + kJoin + kJoinElement * n;
     if (us < least) {
       least = us;
-      best = {pq, pk, true, true};
+      best = {pq, pk, pq > 1, pk > 1};
     }
   };
-  // pairs that make workgroups of about one length, up to four a compute unit
+  // pairs that make workgroups of about one length, or that share tiles of one kind; up to eight workgroups a compute unit
   const double ratio = std::max(k.longest * k.t, 1e-3) / std::max(q.longest * q.t, 1e-3);
-  for (int n = 1; n <= kMostParts && (n == 1 || (2 * n <= std::max(q.longest, k.longest) && n * std::min(q.tiles, k.tiles) <= 4 * cus)); ++n) {
+  for (int n = 1; n <= kMostParts && 2 * n <= std::max(q.longest, k.longest) && n * std::min(q.tiles, k.tiles) <= 8 * cus; ++n) {
     const double other = ratio >= 1 ? n / ratio : n * ratio;
     for (int m = (int)other; m <= (int)other + 1; ++m) ratio >= 1 ? look(m, n) : look(n, m);
+    if (2 * n <= q.longest) look(n, 1);
+    if (2 * n <= k.longest) look(1, n);
   }
   return best;
 }
@@ -134,7 +140,7 @@ hipError_t launch_f32_dense_fwd(const DenseFwd& p, int dtype, hipStream_t s);
 hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s);
 // what the tiles need of every row of queries (p.stats)
 hipError_t launch_dense_bwd_stats(const DenseBwd& p, int dtype, hipStream_t s);
-// sums the parts of dQ, or of all gradients, into them (`dtype`)
-hipError_t launch_dense_bwd_join(const DenseBwd& p, bool all, int dtype, hipStream_t s);
+// sums the parts of dQ, of dK and dV, or of all three, into them (`dtype`)
+hipError_t launch_dense_bwd_join(const DenseBwd& p, bool q, bool kv, int dtype, hipStream_t s);
 
 }  // namespace mrt
