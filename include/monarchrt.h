@@ -259,6 +259,10 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
  *   probabilities and the gradients of the logits are rounded to bf16, by 2^-8 of the value at most), fp32
  *   accumulation; gradients within 1e-2 of the exact ones in the 2-norm (typically 3e-3).
  *   Otherwise fp32 throughout, within 1e-5.  The same call gives the same bits every time (no atomics).
+ *   The backward call forms a weight from a logit and lse, 32-bit numbers: its relative error is 2^-23 of their magnitude
+ *   (1e-3 at 10^4) on top of the above.
+ * Limits, as for dense_attn_fwd, and: scale at least 1e-30; token strides of the backward call's bf16 tensors at most 2^25
+ *   elements, all strides of bf16 gradients multiples of 8 and their pointers 16-byte aligned.
  * dense_attn_fwd_save makes use of dense_attn_fwd_save_workspace_bytes() bytes of scratch (0: none) where the queries are
  *   few; without them it does the same work with fewer workgroups.  MRT_BF16: O is that of dense_attn_fwd_ws with the
  *   same workspace.  Other calls round differently where the queries are few.

@@ -622,6 +622,9 @@ def _rotary(entry, Q, K, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta
             k_positions, dtype, out, k_out, stream):
     import torch
     lib = load_library()
+    _require(K is not None or (k_out is None and k_positions is None), "k_out and k_positions are for a call with K")
+    for y in (out, k_out):
+        _require(y is None or dtype is None or y.dtype == dtype, "dtype is not that of the given output")
     _same_device(Q, K, q_positions, k_positions, out, k_out)
 
     def call(s):

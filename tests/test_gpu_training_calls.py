@@ -79,6 +79,49 @@ def test_forward_with_and_without_scratch(name):
     assert all(torch.equal(x, y) for x, y in zip(got["torch's"], got["the caller's"]))
 
 
+FULL = {          # fp32 products where the queries fill the GPU, or do without scratch
+    "bf16-rows": Step(150, 150, heads=2, compute=1),
+    "bf16-rows-causal-shared-d64": Step(150, 150, heads=4, kv_heads=2, chunk=1, dim=64, compute=1),
+    "bf16-rows-padded": Step(100, 100, heads=2, batch=3, kv_len=(100, 33, 0), compute=1),
+    "d64": Step(150, 150, heads=2, dim=64, dtype="f32"),
+    "padded-d64": Step(100, 100, heads=2, batch=3, kv_len=(100, 33, 0), dim=64, dtype="f32"),
+    "many-heads": Step(300, 300, heads=32, kv_heads=4, batch=4, dim=64, dtype="f32"),
+    "sharp-d64": Step(150, 150, heads=2, dim=64, dtype="f32", sigma=20.0),
+    "sharp": Step(150, 150, heads=2, dtype="f32", sigma=20.0, chunk=1),
+    "many-heads-causal": Step(260, 260, heads=60, batch=3, chunk=1, dim=32, dtype="f32"),
+}
+
+
+@pytest.mark.parametrize("name", FULL)
+def test_forward_that_shares_nothing(name):
+    c = FULL[name]
+    q, k, v, do, kv_len = tensors(c, seed=14)
+    ref, cost = reference(c, q, k, v, do)
+    o, lse = pkg.dense_attn_fwd_save(q, k, v, kv_len=kv_len, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"), **c.args)
+    torch.cuda.synchronize()
+    print(f"  {name}: {check(c, dict(O=o, lse=lse), ref, cost)}", flush=True)
+
+
+SHARP = {
+    "bf16": Step(150, 150, heads=2, sigma=6.0),
+    "bf16-d64-causal-shared": Step(150, 150, heads=4, kv_heads=2, dim=64, chunk=1, sigma=6.0),
+    "bf16-few": Step(3, 400, heads=2, sigma=6.0),
+    "f32": Step(150, 150, heads=2, sigma=10.0, dtype="f32"),
+    "f32-causal-d64": Step(150, 150, heads=2, sigma=10.0, dtype="f32", dim=64, chunk=1),
+}
+
+
+@pytest.mark.parametrize("name", SHARP)
+def test_sharp_rows(name):
+    """Logits of several hundred: rows whose weight lies on one or two keys."""
+    c = SHARP[name]
+    q, k, v, do, kv_len = tensors(c, seed=15)
+    ref, cost = reference(c, q, k, v, do)
+    got = run(c, q, k, v, do, kv_len)
+    torch.cuda.synchronize()
+    print(f"  {name}: {check(c, got, ref, cost)}", flush=True)
+
+
 CALLS = {
     "bf16": Step(2, 2, 12, 13, heads=3, batch=2),
     "bf16-d64-shared-heads": Step(350, 350, heads=4, kv_heads=2, chunk=1, dim=64),

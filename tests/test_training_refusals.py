@@ -332,3 +332,11 @@ def test_rotary_split():
     for dim in range(2, 257):
         split = pkg.binding.rotary_pairs_split(dim)
         assert sum(split) == dim // 2 and min(split) >= 0 and split[0] - split[2] in (0, 1, 2)
+
+
+def test_rotary_arguments_that_contradict():
+    x = torch.zeros(1, 2, 30, 64)
+    at = torch.zeros(3, 30, dtype=torch.int32)
+    for kw in (dict(k_out=x), dict(k_positions=at), dict(dtype=torch.bfloat16, out=x), dict(K=x, dtype=torch.bfloat16, k_out=x)):
+        with pytest.raises(pkg.MrtError, match="k_out|dtype"):
+            pkg.rotary_fwd(x, f_q=1, h=5, w=6, **kw)
