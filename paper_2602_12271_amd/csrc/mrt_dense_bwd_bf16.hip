@@ -155,6 +155,82 @@ __device__ inline void put4(u16* row, float* part, int f, f32x4 x) {
   else *(bf16x4*)(row + f) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
 }
 
+// ---- what both need of a row ----------------------------------------------------------------------
+// -log2(e) lse (-infinity where a row sees no key: weights of zero) and -delta of 32 rows a workgroup, eight threads a row;
+// rows behind the last one as such that see no key.  Memory bounds it (12 heads of 4680 tokens 7 us;
+// 32 heads of 1531 causal tokens 8.7, 6.6 without what follows).
+//
+// delta = O . dO.  The forward call rounded O to bf16, and where a row sees few keys that is the largest error of its dS:
+// all of it has the same sign, beside roundings of dS that do not (gradients of 10 causal tokens 3.2e-3 of the 2-norm off
+// instead of 2.4e-3, of 16 queries over 4 keys 2.8e-3 instead of 2.2e-3, of 1531 causal tokens 2.48e-3 instead of 2.36e-3).
+// So rows that see at most a tile of keys for each wave form delta as the sum of P dP.
+constexpr int kFewKeys = 32 * kWaves;
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_bf16_dense_bwd_stats(DenseBwd p, int nqb) {
+  constexpr int KS = D / 16;
+  // (the first queries of all heads, which see the fewest keys and take longest, come first)
+  const int heads = p.B * p.H, bh = blockIdx.x % heads, block = blockIdx.x / heads;
+  const long long tile = (long long)bh * nqb + block;
+  const int q0 = 32 * block, b = bh / p.H, hd = bh - b * p.H, kvh = hd / p.group;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const u16* dOp = (const u16*)p.dO + b * p.dout.batch + hd * p.dout.head;
+  float* stats = p.stats + tile * 64;
+  const int keys = __builtin_amdgcn_readfirstlane(dense_seen_keys(p, b)), q_last = q0 + 31 < p.Nq ? q0 + 31 : p.Nq - 1;
+  const int most = dense_last_key(p, q_last, keys);
+  auto negative_lse = [&](int q) {
+    const float l = q < p.Nq ? p.lse[(long long)bh * p.Nq + q] : -INFINITY;
+    return l == -INFINITY ? -INFINITY : -kLog2e * l;
+  };
+  if (most > 0 && most <= kFewKeys) {
+    __shared__ float sums[kWaves][32];
+    const int hi = lane >> 5, c = lane & 31, q = q0 + c, k0 = 32 * wave, lim = q < p.Nq ? dense_last_key(p, q, keys) : 0;
+    const long long qr = q < p.Nq ? q : p.Nq - 1, kr = k0 + c < most ? k0 + c : most - 1;
+    const u16* Qp = (const u16*)p.Q + b * p.q.batch + hd * p.q.head + qr * p.q.token + 8 * hi;
+    const u16* Gp = dOp + qr * p.dout.token + 8 * hi;
+    const u16* Kp = (const u16*)p.K + b * p.k.batch + kvh * p.k.head + kr * p.k.token + 8 * hi;
+    const u16* Vp = (const u16*)p.V + b * p.v.batch + kvh * p.v.head + kr * p.v.token + 8 * hi;
+    const float nl = negative_lse(q), scale2 = p.scale * kLog2e;
+    f32x16 s = {}, dp = {};         // rows: keys k0 + 8 (r >> 2) + 4 hi + (r & 3); columns: queries
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      s = mfma32(ld_global_16B(Kp + 16 * ks), ld_global_16B(Qp + 16 * ks), s);
+      dp = mfma32(ld_global_16B(Vp + 16 * ks), ld_global_16B(Gp + 16 * ks), dp);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = exp2_fast(fmaf(s[r], scale2, nl)) * dp[r];
+      sum += k0 + 8 * (r >> 2) + 4 * hi + (r & 3) < lim ? x : 0.f;
+    }
+    sum += __shfl_xor(sum, 32);
+    if (hi == 0) sums[wave][c] = sum;
+    __syncthreads();
+    if (tid < 32) {
+      stats[c] = nl;
+      stats[32 + c] = -((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]));
+    }
+    return;
+  }
+  constexpr int PER = D / 64;            // 16-byte pieces of a row a thread takes
+  const int r = tid >> 3, q = q0 + r;
+  const long long qr = q < p.Nq ? q : p.Nq - 1;
+  const u16* Op = (const u16*)p.O + b * p.o.batch + hd * p.o.head + qr * p.o.token + 8 * (tid & 7);
+  dOp += qr * p.dout.token + 8 * (tid & 7);
+  const float nl = negative_lse(q);
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const bf16x8 x = ld_global_16B(Op + 64 * j), y = ld_global_16B(dOp + 64 * j);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf((float)x[e], (float)y[e], sum);
+  }
+  sum = row8_sum(sum);
+  if ((tid & 7) == 0) {
+    stats[r] = nl;
+    stats[32 + r] = q < p.Nq ? -sum : 0.f;
+  }
+}
+
 // ---- queries -----------------------------------------------------------------------------------
 // Two tiles of 16 queries a wave.  A step's products run in this order: A, the logits and dO V^T of the next step's keys;
 // B, dQ^T += K^T dS of this step.  Between the products of A stand the exponentials and gradients of this step's logits.
@@ -680,7 +756,8 @@ __global__ __launch_bounds__(kThreads) void k_bf16_dense_bwd_few(DenseBwd p) {
   }
 }
 
-bool few_queries(const DenseBwd& p) { return (long long)p.group * p.Nq <= 32; }
+// (Where a row sees a few keys, what memory costs does not matter, and delta does: see above.)
+bool few_queries(const DenseBwd& p) { return (long long)p.group * p.Nq <= 32 && dense_last_key(p, 0, p.Nkv) > kFewKeys; }
 
 template <int D>
 hipError_t run(const DenseBwd& p, hipStream_t s) {
@@ -695,7 +772,9 @@ hipError_t run(const DenseBwd& p, hipStream_t s) {
   }
   constexpr int lds = Stream<D, true>::RING;
   static_assert(lds >= Stream<D, false>::RING, "the ring of either");
-  e = launch_dense_bwd_stats(p, MRT_BF16, s);
+  const int nqb = (p.Nq + 31) / 32;
+  k_bf16_dense_bwd_stats<D><<<(unsigned)(p.B * p.H) * nqb, kThreads, 0, s>>>(p, nqb);
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long long keys = (p.Nkv + kRows - 1) / kRows * (long long)(p.B * p.KH) * p.parts_kv;
   const long long queries = (p.Nq + kRows - 1) / kRows * (long long)(p.B * p.H) * p.parts_q;

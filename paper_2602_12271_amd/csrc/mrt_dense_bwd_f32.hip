@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p, int k
 // delta the sum of its O dO.  64 numbers for 32 rows, rows behind the last one as such that see no key.  Sixteen threads a
 // row; memory bounds it.
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_dense_bwd_stats(DenseBwd p, int nqb) {
+__global__ __launch_bounds__(256) void k_f32_dense_bwd_stats(DenseBwd p, int nqb) {
   const long long tile = blockIdx.x >> 1;
   const int bh = (int)(tile / nqb), r = 16 * (blockIdx.x & 1) + (threadIdx.x >> 4), q = (int)(tile - (long long)bh * nqb) * 32 + r;
   const int b = bh / p.H, hd = bh - b * p.H, row = q < p.Nq ? q : p.Nq - 1;
@@ -253,7 +253,9 @@ __global__ __launch_bounds__(256) void k_dense_bwd_join(JoinArgs args, int d) {
 
 template <int D, typename T, bool VEC>
 hipError_t run_both(const DenseBwd& p, int dtype, hipStream_t s) {
-  hipError_t e = launch_dense_bwd_stats(p, dtype, s);
+  const int nqb = (p.Nq + 31) / 32;
+  k_f32_dense_bwd_stats<T, VEC><<<2 * (unsigned)(p.B * p.H) * nqb, 256, 0, s>>>(p, nqb);
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long long keys = (p.Nkv + kRows - 1) / kRows * (long long)(p.B * p.KH) * p.parts_kv;
   const long long queries = (p.Nq + kRows - 1) / kRows * (long long)(p.B * p.H) * p.parts_q;
@@ -280,17 +282,6 @@ hipError_t run_t(const DenseBwd& p, int dtype, hipStream_t s) {
 }
 
 }  // namespace
-
-hipError_t launch_dense_bwd_stats(const DenseBwd& p, int dtype, hipStream_t s) {
-  const int nqb = (p.Nq + 31) / 32;
-  const dim3 grid(2 * (unsigned)(p.B * p.H) * nqb);
-  const bool bf16 = dtype == MRT_BF16, vec = bf16 ? rows_of_four<u16>(p) : rows_of_four<float>(p);
-  if (bf16 && vec) k_dense_bwd_stats<u16, true><<<grid, 256, 0, s>>>(p, nqb);
-  else if (bf16) k_dense_bwd_stats<u16, false><<<grid, 256, 0, s>>>(p, nqb);
-  else if (vec) k_dense_bwd_stats<float, true><<<grid, 256, 0, s>>>(p, nqb);
-  else k_dense_bwd_stats<float, false><<<grid, 256, 0, s>>>(p, nqb);
-  return hipGetLastError();
-}
 
 hipError_t launch_dense_bwd_join(const DenseBwd& p, bool q, bool kv, int dtype, hipStream_t s) {
   const long long rq = (long long)p.B * p.H * p.Nq, rkv = (long long)p.B * p.KH * p.Nkv;

@@ -138,8 +138,6 @@ bool f32_dense_fwd_quads(const DenseFwd& p, size_t bytes);
 int f32_dense_fwd_parts(const DenseFwd& p);
 hipError_t launch_f32_dense_fwd(const DenseFwd& p, int dtype, hipStream_t s);
 hipError_t launch_f32_dense_bwd(const DenseBwd& p, int dtype, hipStream_t s);
-// what the tiles need of every row of queries (p.stats)
-hipError_t launch_dense_bwd_stats(const DenseBwd& p, int dtype, hipStream_t s);
 // sums the parts of dQ, of dK and dV, or of all three, into them (`dtype`)
 hipError_t launch_dense_bwd_join(const DenseBwd& p, bool q, bool kv, int dtype, hipStream_t s);
 
