@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256) void k_f32_dense_bwd_stats(DenseBwd p, int nqb
 }
 
 // Gradients from their parts, added in their order: those of dQ, dK and dV that have some (blockIdx.y).  A thread owns four features of a
-// row and has four parts in flight: what it waits for is memory.
+// row and has two or eight parts in flight: what it waits for is memory.
 struct JoinArgs {
   struct {
     const float* from;
@@ -229,26 +229,31 @@ struct JoinArgs {
     int n, tokens, heads;
   } a[3];
 };
-template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_dense_bwd_join(JoinArgs args, int d) {
-  constexpr int AHEAD = 4;
+// (parts have at most 2^27 elements together: 32 bits hold the threads' numbers)
+template <typename T, bool VEC, int AHEAD>
+__global__ __launch_bounds__(kJoinThreads) void k_dense_bwd_join(JoinArgs args, int d) {
   const auto& a = args.a[blockIdx.y];
-  const int quads = (d + 3) >> 2, n = a.n;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / quads, rows = a.rows;
+  const int n = a.n;
+  const unsigned quads = (d + 3) >> 2, at = blockIdx.x * kJoinThreads + threadIdx.x, row = at / quads;
   const int v = 4 * (int)(at - row * quads);
-  if (row >= rows) return;
-  const float* from = a.from + row * d;
+  if (row >= a.rows) return;
+  const float* from = a.from + (long long)row * d;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   for (int i = 0; i < n; i += AHEAD) {
     f32x4 y[AHEAD];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) y[k] = ld4<VEC>(from + (long long)(i + k < n ? i + k : n - 1) * rows * d, v, d);
+    for (int k = 0; k < AHEAD; ++k) y[k] = ld4<VEC>(from + (i + k < n ? i + k : n - 1) * a.rows * d, v, d);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
       if (i + k < n) x = x + y[k];
   }
-  const int bh = (int)(row / a.tokens), tok = (int)(row - (long long)bh * a.tokens), b = bh / a.heads, hd = bh - b * a.heads;
+  const unsigned bh = row / (unsigned)a.tokens, tok = row - bh * a.tokens, b = bh / a.heads, hd = bh - b * a.heads;
   st4<VEC>((T*)a.to + b * a.st.batch + hd * a.st.head + tok * a.st.token, x, v, d);
+}
+template <typename T, bool VEC>
+void join(const JoinArgs& a, int most, dim3 grid, int d, hipStream_t s) {
+  if (most <= 2) k_dense_bwd_join<T, VEC, 2><<<grid, kJoinThreads, 0, s>>>(a, d);
+  else k_dense_bwd_join<T, VEC, 8><<<grid, kJoinThreads, 0, s>>>(a, d);
 }
 
 template <int D, typename T, bool VEC>
@@ -293,12 +298,13 @@ hipError_t launch_dense_bwd_join(const DenseBwd& p, bool q, bool kv, int dtype, 
     a.a[n++] = {p.pv, p.dV, p.dv, rkv, p.parts_kv, p.Nkv, p.KH};
   }
   const long long threads = (q && kv ? std::max(rq, rkv) : q ? rq : rkv) * ((p.d + 3) / 4);
-  const dim3 grid((unsigned)((threads + 255) / 256), n);
+  const dim3 grid((unsigned)((threads + kJoinThreads - 1) / kJoinThreads), n);
+  const int most = std::max(q ? p.parts_q : 0, kv ? p.parts_kv : 0);
   const bool bf16 = dtype == MRT_BF16, vec = bf16 ? rows_of_four<u16>(p) : rows_of_four<float>(p);
-  if (bf16 && vec) k_dense_bwd_join<u16, true><<<grid, 256, 0, s>>>(a, p.d);
-  else if (bf16) k_dense_bwd_join<u16, false><<<grid, 256, 0, s>>>(a, p.d);
-  else if (vec) k_dense_bwd_join<float, true><<<grid, 256, 0, s>>>(a, p.d);
-  else k_dense_bwd_join<float, false><<<grid, 256, 0, s>>>(a, p.d);
+  if (bf16 && vec) join<u16, true>(a, most, grid, p.d, s);
+  else if (bf16) join<u16, false>(a, most, grid, p.d, s);
+  else if (vec) join<float, true>(a, most, grid, p.d, s);
+  else join<float, false>(a, most, grid, p.d, s);
   return hipGetLastError();
 }
 

@@ -138,12 +138,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_fwd(DenseFwd p) {
 
 // O and the statistics from the parts, all against the largest reference.  A thread owns four features of a row.
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_f32_dense_join(DenseFwd p, long long rows) {
-  const int d = p.d, quads = (d + 3) >> 2;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / quads;
+__global__ __launch_bounds__(kJoinThreads) void k_f32_dense_join(DenseFwd p, long long rows) {
+  // (parts have at most 2^27 elements together: 32 bits hold the threads' numbers)
+  const int d = p.d;
+  const unsigned quads = (d + 3) >> 2, at = blockIdx.x * kJoinThreads + threadIdx.x, row = at / quads;
   const int v = 4 * (int)(at - row * quads);
   if (row >= rows) return;
-  constexpr int AHEAD = 4;               // parts in flight: what a thread waits for is memory
+  constexpr int AHEAD = 8;               // parts in flight: what a thread waits for is memory
   float m = kNoKey, sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int i0 = 0; i0 < p.parts; i0 += AHEAD) {
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(256) void k_f32_dense_join(DenseFwd p, long long ro
         o = o + x[k] * f;
       }
   }
-  const int bh = (int)(row / p.Nq), q = (int)(row - (long long)bh * p.Nq), b = bh / p.H, hd = bh - b * p.H;
+  const unsigned bh = row / (unsigned)p.Nq, q = row - bh * p.Nq, b = bh / p.H, hd = bh - b * p.H;
   st4<VEC>((T*)p.O + b * p.o.batch + hd * p.o.head + q * p.o.token, o * (sum > 0.f ? 1.f / sum : 0.f), v, d);
   if (v == 0) p.lse[row] = natural_lse(m, sum);
 }
@@ -186,7 +187,7 @@ hipError_t run(const DenseFwd& p, hipStream_t s) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long long rows = (long long)p.B * p.H * p.Nq;
-  k_f32_dense_join<T, VEC><<<(unsigned)((rows * ((p.d + 3) / 4) + 255) / 256), 256, 0, s>>>(p, rows);
+  k_f32_dense_join<T, VEC><<<(unsigned)((rows * ((p.d + 3) / 4) + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, s>>>(p, rows);
   return hipGetLastError();
 }
 template <typename T>

@@ -85,7 +85,7 @@ struct DenseBwdShape {
 // 12 heads of 4680 tokens 456 | 428, two to a tile of queries; one head of 4680 tokens 151 | 67, six and seven.)
 constexpr double kBeside = 1.6, kLastQueries = 0.25, kLastKeys = 0.06, kJoin = 6.0, kJoinElement = 1.35e-6, kUnshared = 1.03;
 constexpr long long kMostPartElements = 1 << 27;      // of all parts together
-constexpr int kMostParts = 32;
+constexpr int kMostParts = 32, kJoinThreads = 64;
 // tile: rows of a workgroup; step: streamed rows
 inline DenseBwdShape dense_bwd_shape(const DenseBwd& p, int tile, int step, double tq, double tkv) {
   auto steps = [&](long long n) { return (double)((n + step - 1) / step); };
