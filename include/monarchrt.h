@@ -264,8 +264,8 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
  * Limits, as for dense_attn_fwd, and: scale at least 1e-30; token strides of the backward call's bf16 tensors at most 2^25
  *   elements, all strides of bf16 gradients multiples of 8 and their pointers 16-byte aligned.
  * dense_attn_fwd_save makes use of dense_attn_fwd_save_workspace_bytes() bytes of scratch (0: none) where the queries are
- *   few; without them it does the same work with fewer workgroups.  MRT_BF16: O is that of dense_attn_fwd_ws with the
- *   same workspace.  Other calls round differently where the queries are few.
+ *   few; without them it does the same work with fewer workgroups.  Calls that share the keys of a tile differently, and
+ *   dense_attn_fwd under a mask, differ by roundings.
  * As in the forward pass an infinite or NaN key, value, query or gradient that is hidden by causal_chunk from some
  *   rows of a run of 256 (with shared keys: of the heads that share them), and seen by others, may show in them all; one
  *   behind kv_len, or one that the mask hides from every row, never shows.

@@ -524,8 +524,8 @@ def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_off
 
     Calls of few queries share their keys over several workgroups if they have scratch memory
     (dense_attn_fwd_save_workspace_bytes): `workspace`, or memory of torch's allocator.  Without `workspace` a call under a
-    graph capture, or one whose scratch the allocator refuses, does without, as dense_attn_fwd does; bf16 results are those
-    of dense_attn_fwd."""
+    graph capture, or one whose scratch the allocator refuses, does without, as dense_attn_fwd does.  O differs from dense_attn_fwd's by
+    roundings at most."""
     import torch
     lib = load_library()
     _same_device(Q, K, V, out, lse, kv_len, workspace)

@@ -838,7 +838,7 @@ static KParams dense_params(const mrt_problem* p, int causal_chunk) {
 size_t dense_attn_workspace_bytes(const mrt_problem* p, int causal_chunk) {
   if (dense_attn_check(p, causal_chunk) != MRT_OK) return 0;
   if (p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32) return 0;
-  return bf16_dense_workspace_bytes(dense_params(p, causal_chunk), p->batch * p->heads);
+  return bf16_dense_workspace_bytes(dense_params(p, causal_chunk), p->batch * p->heads, false);
 }
 
 mrt_status dense_attn_fwd(const void* Q, const void* K, const void* V, void* O,
@@ -930,7 +930,7 @@ static size_t dense_fwd_parts_bytes(const DenseFwd& d) {
 size_t dense_attn_fwd_save_workspace_bytes(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk) {
   if (dense_train_check(p, t, causal_chunk, false) != MRT_OK) return 0;
   if (p->dtype == MRT_F32 || p->compute == MRT_COMPUTE_F32) return dense_fwd_parts_bytes(dense_fwd_params(p, t, causal_chunk));
-  return bf16_dense_workspace_bytes(dense_params(p, causal_chunk), p->batch * p->heads);
+  return bf16_dense_workspace_bytes(dense_params(p, causal_chunk), p->batch * p->heads, true);
 }
 
 mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void* O, float* lse, const mrt_problem* p,

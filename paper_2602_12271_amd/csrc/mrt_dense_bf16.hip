@@ -478,7 +478,22 @@ struct DenseShape {
   int queries, parts;    // queries per workgroup, workgroups that share the keys of one query tile
 };
 
-DenseShape dense_shape(const KParams& kp, int nbh, bool may_split) {
+// Under a mask the longest tiles go first, which the figures above do not know: a call then takes as long as its longest
+// workgroup, or as all of them on all units and three tenths of the longest (microseconds a step of 64 keys by the number
+// of queries; more where all units work at once).  A call that keeps its row statistics goes by that (128 features; us by
+// the rule above | by this: 16 heads of 1531 causal tokens sharing 2, batch of 2, 55 | 44, 12 heads of 4096 112 | 83, of 12
+// one-frame chunks of 320 102 | 76, 32 heads of 2048 71 | 63, 13 other shapes the same; 64 features would gain 3 % at most);
+// dense_attn_fwd keeps its shapes, and with them the last bits of its results.
+double masked_time(const KParams& kp, int nbh, int queries, int parts) {
+  const double lone = queries == 64 ? 0.71 : queries == 128 ? 1.02 : 1.56, busy = queries == 64 ? 0.85 : queries == 128 ? 1.1 : 1.56;
+  const long long first = dense_visible(kp, std::min(queries, kp.Nq) - 1), last = dense_visible(kp, kp.Nq - 1), pairs = (last + 63) / 64;
+  const double steps = (double)((pairs + parts - 1) / parts), share = (double)(first + last) / (2 * last);
+  const double n = (double)((kp.Nq + queries - 1) / queries) * nbh * parts / compute_units();
+  const double joined = parts > 1 ? 5.5 + 1e-6 * 2 * dense_parts_bytes(kp.Nq * nbh, parts, kp.d) / 5.7 : 0.0;
+  return 7.5 + steps * (n <= 1 ? lone : std::max(lone, n * share * busy + 0.3 * lone)) + joined;
+}
+
+DenseShape dense_shape(const KParams& kp, int nbh, bool may_split, bool save) {
   const long long cus = compute_units(), first = dense_visible(kp, 0), last = dense_visible(kp, kp.Nq - 1);
   auto wgs = [&](int queries) { return (long long)((kp.Nq + queries - 1) / queries) * nbh; };
   DenseShape best;
@@ -492,6 +507,12 @@ DenseShape dense_shape(const KParams& kp, int nbh, bool may_split) {
     auto cost = [&](int queries, long long unit) { return (wgs(queries) + cus - 1) / cus * unit; };
     const long long c256 = cost(256, first == last ? 126 : 112), c128 = cost(128, 79), c64 = cost(64, 61);
     best = {c64 < c128 && c64 < c256 ? 64 : c128 < c256 ? 128 : 256, 1};
+  }
+  const bool masked = save && first != last && kp.d == 128;
+  if (masked) {
+    best.queries = 64;
+    for (int queries : {128, 256})
+      if (masked_time(kp, nbh, queries, 1) <= masked_time(kp, nbh, best.queries, 1)) best.queries = queries;
   }
   if (!may_split || (long long)kp.Nq * nbh > kMostSplitRows) return best;
   const long long pairs = (last + 63) / 64;
@@ -525,12 +546,12 @@ DenseShape dense_shape(const KParams& kp, int nbh, bool may_split) {
     const long long run = std::min(queries, 128);
     return first == last || run <= one.queries || ((long long)kp.cc * kp.hw % run == 0 && (long long)kp.qoff * kp.hw % run == 0);
   };
-  double least = time(one.queries, 1) / 1.06;
+  double least = (masked ? masked_time(kp, nbh, one.queries, 1) : time(one.queries, 1)) / 1.06;
   for (int queries = 64; queries <= (kp.d == 64 ? 128 : 256); queries *= 2) {
     if (!run_ok(queries)) continue;
     for (int parts = 2; parts <= kMostParts && parts <= pairs; ++parts) {
       if (dense_parts_bytes(kp.Nq * nbh, parts, kp.d) > kMostPartsBytes || wgs(queries) * parts > 6 * cus) break;
-      const double us = time(queries, parts);
+      const double us = masked ? masked_time(kp, nbh, queries, parts) : time(queries, parts);
       if (us < least) { least = us; best = {queries, parts}; }
     }
   }
@@ -555,14 +576,14 @@ hipError_t run_dense_shape(const KParams& kp, int nbh, const DenseShape& shape, 
 
 }  // namespace
 
-size_t bf16_dense_workspace_bytes(const KParams& kp, int nbh) {
-  const DenseShape shape = dense_shape(kp, nbh, true);
+size_t bf16_dense_workspace_bytes(const KParams& kp, int nbh, bool save) {
+  const DenseShape shape = dense_shape(kp, nbh, true, save);
   return shape.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d) : 0;
 }
 
 hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseSave* save, hipStream_t s) {
-  DenseShape shape = dense_shape(kp, nbh, workspace != nullptr);
-  if (shape.parts > 1 && workspace_bytes < dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d)) shape = dense_shape(kp, nbh, false);
+  DenseShape shape = dense_shape(kp, nbh, workspace != nullptr, save != nullptr);
+  if (shape.parts > 1 && workspace_bytes < dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d)) shape = dense_shape(kp, nbh, false, save != nullptr);
   const size_t rows = (size_t)kp.Nq * nbh * shape.parts;
   const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), shape.parts};
   return save ? run_dense_shape(kp, nbh, shape, parts, *save, s) : run_dense_shape(kp, nbh, shape, parts, NoSave{}, s);
