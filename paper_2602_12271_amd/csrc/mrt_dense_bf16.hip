@@ -446,7 +446,8 @@ hipError_t run_dense(const KParams& kp, int nbh, const DenseParts& parts, const 
 // tokens 59 | 78 | 122 us, 5 heads 120 | 80 | 123, 12 heads 233 | 159 | 130, 16 heads 294 | 238 | 256).
 // Where a mask gives the query tiles different key counts the short ones fill the last round, and the
 // largest shape, which reads the keys least often, is taken at 112 (24 heads of 12 one-frame chunks of
-// 320 tokens 203 | 173 | 162, 10 heads of 2 chunks of 4680 tokens 575 | 444 | 399).
+// 320 tokens 203 | 173 | 162, 10 heads of 2 chunks of 4680 tokens 575 | 444 | 399, with the tiles head by head, as
+// in all figures down to the last paragraph).
 //
 // 64 features: two workgroups of 64 or 128 queries share a compute unit; a round of up to one per unit
 // costs 40 and 57 us, of up to two 54 and 90 (one head of 4680 tokens 38 | 57, 5 heads 53 | 58, 8 heads
