@@ -454,10 +454,11 @@ def _dtype_of(x, name):
 
 
 def _same_device(first, *others):
-    _require(first.is_cuda, "tensors must be on a GPU")
     at = first.get_device()
+    _require(at >= 0, "tensors must be on a GPU")
     for x in others:
-        _require(x is None or (x.is_cuda and x.get_device() == at), "tensors are on different devices")
+        if x is not None and x.get_device() != at:
+            _require(False, "tensors are on different devices")
 
 
 # (problem, training description without kv_len, backward scratch) of recent calls by their values, like _problems
