@@ -234,14 +234,18 @@ bool f32_dense_fwd_quads(const DenseFwd& p, size_t bytes) {
 }
 
 // The other kernel takes 32 keys in 5.0 us at 128 features and 2.1 at 64 (one workgroup of 128 queries to a compute unit;
-// two share it at 1.35 times that).
+// two share it at 1.35 times that), and a step of its own, of which a quarter is hidden, for every chunk of a mask that ends
+// inside its queries.  This one takes a fifth longer than dense_share says where it fills the chip.  (us, this kernel | the
+// other: 16 heads of 1800 tokens 284 | 270, 12 of 5400 tokens of 64 features in chunks of 1800 595 | 429, 16 of 4096 causal
+// tokens 688 | 1290, 4 of 600 24 | 82.)
 int f32_dense_fwd_parts(const DenseFwd& p) {
   const double first = dense_last_key(p, std::min(kRows, p.Nq) - 1, p.Nkv), last = dense_last_key(p, p.Nq - 1, p.Nkv), cus = compute_units();
   const DenseShare own = dense_share(p.Nq, kRows, (long long)p.B * p.H, p.d, p.d <= 64 ? 0.75 : 1.4, first / kStep, last / kStep);
+  const double ends = p.cc > 0 && first != last ? 24.0 * std::max(0.0, 128.0 / ((double)p.cc * p.hw) - 1) : 0.0;
   const double each = (p.Nq + 127) / 128 * (double)(p.B * p.H) / cus, pairs = std::floor(each / 2), rest = each - 2 * pairs;
-  const double rounds = 1.35 * pairs + (rest > 1 ? 1.35 : rest > 0 ? 1.0 : 0.0);
-  const double other = (p.d <= 64 ? 2.1 : 5.0) / 32 * std::max(last * std::min(rounds, 1.35), 0.5 * (first + last) * rounds);
-  return own.us < other ? own.parts : 0;
+  const double rounds = first == last ? 1.35 * pairs + (rest > 1 ? 1.35 : rest > 0 ? 1.0 : 0.0) : each <= 1 ? 1.0 : std::max(1.35, 0.675 * each + 0.35);
+  const double other = (p.d <= 64 ? 2.1 : 5.0) / 32 * std::max((last + ends) * std::min(rounds, 1.35), (0.5 * (first + last) + ends) * rounds);
+  return 1.2 * own.us < other ? own.parts : 0;
 }
 
 hipError_t launch_f32_dense_fwd(const DenseFwd& p, int dtype, hipStream_t s) {
