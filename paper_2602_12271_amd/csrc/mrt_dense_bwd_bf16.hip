@@ -566,7 +566,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_bf16_dense_bwd(DenseBwd p, int 
 template <int D>
 struct Few {
   static constexpr int TILE = kTileBytes<D>, WAVE = 4 * TILE, ROWS_AT = kWaves * WAVE, STATS_AT = ROWS_AT + 2 * TILE;
-  static constexpr int BYTES = STATS_AT + 3 * 32 * 4;      // two slots of keys and values a wave; Q, dO; -log2(e) lse, -delta, limits
+  // two slots of keys and values a wave; Q, dO; -log2(e) lse, -delta, limits; sums of P dP a wave
+  static constexpr int SUMS_AT = STATS_AT + 3 * 32 * 4, BYTES = SUMS_AT + kWaves * 32 * 4;
 };
 
 template <int D>
@@ -634,13 +635,40 @@ __global__ __launch_bounds__(kThreads) void k_bf16_dense_bwd_few(DenseBwd p) {
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
+  const float scale2 = p.scale * kLog2e, nlq = stats[c];
+  const int limq = lims[c], free_keys = dense_last_key(p, 0, keys);     // (the limits rise with the query)
+  const int row_at = c * RB + (swz(c) ^ hi) * 16;
+  auto row_op = [&](int at, int ks) { return *(const bf16x8*)(bwd_lds + at + (row_at ^ (32 * ks))); };
+  // a sequence of few keys in a tensor of many: delta is the sum of P dP, as in k_bf16_dense_bwd_stats (a run of keys that
+  // the sequence has none of needs no delta)
+  if (keys <= kFewKeys && 32 * t0 < keys) {
+    const int k0 = 32 * wave;
+    const long long kr = k0 + c < keys ? k0 + c : keys - 1;
+    const u16 *Kr = Kp + kr * p.k.token + 8 * hi, *Vr = Vp + kr * p.v.token + 8 * hi;
+    f32x16 sv = {}, dp = {};         // rows: keys, columns: queries
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sv = mfma32(ld_global_16B(Kr + 16 * ks), row_op(L::ROWS_AT, ks), sv);
+      dp = mfma32(ld_global_16B(Vr + 16 * ks), row_op(L::ROWS_AT + TILE, ks), dp);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = exp2_fast(fmaf(sv[r], scale2, nlq)) * dp[r];
+      sum += k0 + 8 * (r >> 2) + 4 * hi + (r & 3) < limq ? x : 0.f;
+    }
+    sum += __shfl_xor(sum, 32);
+    float* sums = (float*)(bwd_lds + L::SUMS_AT);
+    if (hi == 0) sums[wave * 32 + c] = sum;
+    __syncthreads();
+    if (tid < 32) stats[32 + c] = -((sums[c] + sums[32 + c]) + (sums[64 + c] + sums[96 + c]));
+    __syncthreads();
+  }
   fetch(t0 + wave + kWaves, 1);
 
-  const float scale2 = p.scale * kLog2e, nlq = stats[c], ndq = stats[32 + c];
-  const int limq = lims[c], free_keys = dense_last_key(p, 0, keys);     // (the limits rise with the query)
+  const float ndq = stats[32 + c];
   const int G = lane >> 4, s = lane & 15, trow = 4 * hi + (s >> 2);
-  const int row_at = c * RB + (swz(c) ^ hi) * 16, tr_at = trow * RB + ((2 * (G & 1) + ((s >> 1) & 1)) ^ swz(trow)) * 16 + 8 * (s & 1);
-  auto row_op = [&](int at, int ks) { return *(const bf16x8*)(bwd_lds + at + (row_at ^ (32 * ks))); };
+  const int tr_at = trow * RB + ((2 * (G & 1) + ((s >> 1) & 1)) ^ swz(trow)) * 16 + 8 * (s & 1);
   auto tr_op = [&](int at, int f, int kk) {
     const char* lo = bwd_lds + at + (tr_at ^ (64 * f)) + 16 * kk * RB;
     const char* up = bwd_lds + at + (tr_at ^ (64 * f + 32)) + (16 * kk + 8) * RB;
@@ -756,7 +784,7 @@ __global__ __launch_bounds__(kThreads) void k_bf16_dense_bwd_few(DenseBwd p) {
   }
 }
 
-// (Where a row sees a few keys, what memory costs does not matter, and delta does: see above.)
+// (Where the tensor has a few keys, what memory costs does not matter.)
 bool few_queries(const DenseBwd& p) { return (long long)p.group * p.Nq <= 32 && dense_last_key(p, 0, p.Nkv) > kFewKeys; }
 
 template <int D>

@@ -1,0 +1,76 @@
+"""GPU: the dense attention's backward pass where rows see few keys.
+
+delta = dO . O, with O rounded to bf16, is off by up to 2^-8 of sum |dO| |O|, and where a row sees few keys, or keys that
+hardly differ, that is more than all of dS = P (dP - delta): over a single key dS is zero.  Such rows form delta from P and
+dP, and the gradients are held here to a bound in which O does not occur."""
+import dataclasses
+
+import pytest
+import torch
+
+from dense_training import Step, hidden, reference, run, tensors, units
+
+pytestmark = pytest.mark.gpu
+
+
+def alike(c, seed):
+    """Values of a head that differ by a thirty-second of their size: what dO . V has in common cancels in dS, and a delta
+    that is off does not."""
+    q, k, v, do, kv_len = tensors(c, seed=seed)
+    common = torch.randn(c.batch, v.shape[1], 1, c.dim, generator=torch.Generator().manual_seed(seed)).to(v.device)
+    v.copy_(common + 2.0 ** -5 * v.float())
+    return q, k, v, do, kv_len
+
+
+def by_values(c, q, k, v, do):
+    """What a relative error of size 1 of the 32-bit numbers P, dP and delta may cost dQ and dK, entry by entry:
+    with A_ij = sum over features of |dO_i| |V_j|, dS_ij is off by P_ij (A_ij + sum_j P_ij A_ij)."""
+    scale, group = c.args["scale"], c.heads // (c.kv_heads or c.heads)
+    q, k, v, do = (x.double() for x in (q, k, v, do))
+    out = dict(dQ=torch.zeros_like(q), dK=torch.zeros_like(k))
+    for b in range(c.batch):
+        off = hidden(c, b, q.device)
+        for h in range(c.heads):
+            g = h // group
+            s = (scale * (q[b, h] @ k[b, g].t())).masked_fill(off, -torch.inf)
+            p = torch.nan_to_num(torch.softmax(s, -1))
+            a = do[b, h].abs() @ v[b, g].abs().t()
+            ds = p * (a + (p * a).sum(-1, keepdim=True))
+            out["dQ"][b, h] = scale * (ds @ k[b, g].abs())
+            out["dK"][b, g] += scale * (ds.t() @ q[b, h].abs())
+    return out
+
+
+def check_short(c, got, q, k, v, do, sequences):
+    """P, dP and delta are off by units()'s `sums` over the 128 keys that a row sees at most (delta by two, its own sum
+    and that of P dP), the sums of dS K and dS^T Q by another: 4 in all; then dS is rounded as an operand, and the result
+    to its type."""
+    ref, (cost, _) = reference(c, q, k, v, do)
+    values = by_values(c, q, k, v, do)
+    u, sums = units(dataclasses.replace(c, f_kv=min(c.f_kv, 128)))
+    stored = 2.0 ** -8
+    for name in ("dQ", "dK"):
+        want = ref[name]
+        tol = (u * cost[name] + 4 * sums * (1 + u) * values[name]) * (1 + stored) + stored * want.abs() + 1e-30
+        off = ((got[name].double() - want).abs() / tol)[list(sequences)]
+        print(f"  {name}: {float(off.max()):.2f} of what rounding may cost", flush=True)
+        assert off.max() <= 1, name
+
+
+# (up to 32 queries that share keys, in a tensor of many keys, of which the sequences have few)
+CUT = {
+    "one-query": Step(1, 3000, heads=30, batch=5, kv_len=(3000, 1, 2, 4, 128)),
+    "one-query-d64-shared": Step(1, 500, heads=30, kv_heads=5, batch=4, dim=64, kv_len=(1, 3, 33, 500)),
+    "rows": Step(16, 1030, heads=12, batch=4, kv_len=(1, 2, 31, 97)),
+    "rows-causal": Step(16, 400, heads=8, kv_heads=4, batch=4, chunk=1, offset=380, kv_len=(1, 64, 100, 390)),
+    "rows-of-heads": Step(4, 300, heads=16, kv_heads=2, batch=3, dim=64, kv_len=(1, 0, 65)),
+}
+
+
+@pytest.mark.parametrize("name", CUT)
+def test_sequences_cut_to_few_keys(name):
+    c = CUT[name]
+    q, k, v, do, kv_len = alike(c, seed=31)
+    got = run(c, q, k, v, do, kv_len)
+    torch.cuda.synchronize()
+    check_short(c, got, q, k, v, do, [b for b, n in enumerate(c.kv_len) if n <= 128])
