@@ -74,3 +74,29 @@ def test_sequences_cut_to_few_keys(name):
     got = run(c, q, k, v, do, kv_len)
     torch.cuda.synchronize()
     check_short(c, got, q, k, v, do, [b for b, n in enumerate(c.kv_len) if n <= 128])
+
+
+# bf16 tensors, fp32 arithmetic: dS is not rounded, and nothing but the result's rounding and 32-bit sums is left
+IN_F32 = {
+    "causal-10": Step(10, 10, heads=8, chunk=1, compute=1),
+    "causal-100-d64": Step(100, 100, heads=4, chunk=1, dim=64, compute=1),
+    "two-keys": Step(3, 2, heads=30, batch=2, compute=1),
+    "one-key": Step(40, 1, heads=3, compute=1),
+    "queries-50-of-128-shared": Step(50, 128, heads=6, kv_heads=2, dim=64, compute=1),
+    "queries-300-of-90": Step(300, 90, heads=2, compute=1),
+    "frames-dim-40": Step(4, 4, 3, 7, heads=4, chunk=1, dim=40, compute=1),
+    "odd-dim-causal": Step(33, 33, heads=4, chunk=1, dim=37, compute=1),
+    "dim-1": Step(20, 30, heads=4, dim=1, compute=1),
+    "padded": Step(40, 40, heads=6, batch=5, kv_len=(40, 32, 5, 1, 0), compute=1),
+    "cut": Step(17, 2000, heads=4, batch=3, kv_len=(128, 3, 1), compute=1),
+    "tokens-outside-heads": Step(2, 3, 4, 9, heads=4, kv_heads=2, batch=2, layout="bnhd", compute=1),
+}
+
+
+@pytest.mark.parametrize("name", IN_F32)
+def test_bf16_tensors_in_fp32_arithmetic(name):
+    c = IN_F32[name]
+    q, k, v, do, kv_len = alike(c, seed=32)
+    got = run(c, q, k, v, do, kv_len)
+    torch.cuda.synchronize()
+    check_short(c, got, q, k, v, do, range(c.batch))
