@@ -283,6 +283,9 @@ typedef struct {
   mrt_strides dout, dq, dk, dv;
 } mrt_dense_train;
 size_t dense_attn_fwd_save_workspace_bytes(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk);
+/* Which of its kernels a forward call with so much scratch takes: queries of a workgroup, 64, 128 or 256 (0: invalid
+ * arguments).  fp32 calls whose rows are not aligned to four elements take 64.  For tests and measurements. */
+int dense_attn_fwd_save_queries(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk, size_t workspace_bytes);
 mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void* O, float* lse, const mrt_problem* p,
                                const mrt_dense_train* t, int causal_chunk, void* workspace, size_t workspace_bytes,
                                void* hip_stream);

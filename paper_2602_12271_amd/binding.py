@@ -26,7 +26,7 @@ EXPORTED = [
     "monarch_attn_fwd_noalloc",
     "monarch_attn_bwd_saved_workspace_bytes", "monarch_attn_fwd_save", "monarch_attn_bwd_saved",
     "dense_attn_workspace_bytes", "dense_attn_fwd_ws",
-    "dense_attn_fwd_save", "dense_attn_fwd_save_workspace_bytes", "dense_attn_bwd", "dense_attn_bwd_check", "dense_attn_bwd_workspace_bytes",
+    "dense_attn_fwd_save", "dense_attn_fwd_save_workspace_bytes", "dense_attn_fwd_save_queries", "dense_attn_bwd", "dense_attn_bwd_check", "dense_attn_bwd_workspace_bytes",
     "mrt_rotary_check", "mrt_rotary_fwd", "mrt_rotary_bwd",
 ]
 NOALLOC_SCRATCH_BYTES = 128 << 20
@@ -125,6 +125,8 @@ def load_library() -> ctypes.CDLL:
     lib.dense_attn_fwd_save.restype = ci
     lib.dense_attn_fwd_save_workspace_bytes.argtypes = [P, T, ci]
     lib.dense_attn_fwd_save_workspace_bytes.restype = sz
+    lib.dense_attn_fwd_save_queries.argtypes = [P, T, ci, sz]
+    lib.dense_attn_fwd_save_queries.restype = ci
     lib.dense_attn_bwd_check.argtypes = [P, T, ci]
     lib.dense_attn_bwd_check.restype = ci
     lib.dense_attn_bwd_workspace_bytes.argtypes = [P, T, ci]
@@ -555,6 +557,11 @@ def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_off
 def dense_attn_fwd_save_workspace_bytes(prob: MrtProblem, train: MrtDenseTrain, causal_chunk=0) -> int:
     """Scratch a forward call that keeps its row statistics makes use of (0: none)."""
     return int(load_library().dense_attn_fwd_save_workspace_bytes(ctypes.byref(prob), ctypes.byref(train), causal_chunk))
+
+
+def dense_attn_fwd_save_queries(prob: MrtProblem, train: MrtDenseTrain, causal_chunk=0, workspace_bytes=0) -> int:
+    """Queries of a workgroup of that call with so much scratch (64, 128 or 256: one of its kernels each)."""
+    return int(load_library().dense_attn_fwd_save_queries(ctypes.byref(prob), ctypes.byref(train), causal_chunk, workspace_bytes))
 
 
 def dense_attn_bwd_workspace_bytes(prob: MrtProblem, train: MrtDenseTrain, causal_chunk=0) -> int:

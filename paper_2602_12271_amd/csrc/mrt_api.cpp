@@ -933,6 +933,14 @@ size_t dense_attn_fwd_save_workspace_bytes(const mrt_problem* p, const mrt_dense
   return bf16_dense_workspace_bytes(dense_params(p, causal_chunk), p->batch * p->heads, true);
 }
 
+int dense_attn_fwd_save_queries(const mrt_problem* p, const mrt_dense_train* t, int causal_chunk, size_t workspace_bytes) {
+  if (dense_train_check(p, t, causal_chunk, false) != MRT_OK) return 0;
+  if (p->dtype != MRT_F32 && p->compute != MRT_COMPUTE_F32)
+    return bf16_dense_queries(dense_params(p, causal_chunk), p->batch * p->heads, workspace_bytes, true);
+  const DenseFwd d = dense_fwd_params(p, t, causal_chunk);
+  return d.parts == 0 || (d.parts > 1 && workspace_bytes < dense_fwd_parts_bytes(d)) ? 128 : 64;
+}
+
 mrt_status dense_attn_fwd_save(const void* Q, const void* K, const void* V, void* O, float* lse, const mrt_problem* p,
                                const mrt_dense_train* t, int causal_chunk, void* workspace, size_t workspace_bytes,
                                void* hip_stream) {

@@ -575,6 +575,12 @@ hipError_t run_dense_shape(const KParams& kp, int nbh, const DenseShape& shape, 
                          : run_dense_d<64, false>(kp, nbh, shape.queries, parts, save, s);
 }
 
+// with `bytes` of scratch
+DenseShape dense_call_shape(const KParams& kp, int nbh, size_t bytes, bool save) {
+  const DenseShape shape = dense_shape(kp, nbh, bytes > 0, save);
+  return shape.parts > 1 && bytes < dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d) ? dense_shape(kp, nbh, false, save) : shape;
+}
+
 }  // namespace
 
 size_t bf16_dense_workspace_bytes(const KParams& kp, int nbh, bool save) {
@@ -582,9 +588,12 @@ size_t bf16_dense_workspace_bytes(const KParams& kp, int nbh, bool save) {
   return shape.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d) : 0;
 }
 
+int bf16_dense_queries(const KParams& kp, int nbh, size_t workspace_bytes, bool save) {
+  return dense_call_shape(kp, nbh, workspace_bytes, save).queries;
+}
+
 hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseSave* save, hipStream_t s) {
-  DenseShape shape = dense_shape(kp, nbh, workspace != nullptr, save != nullptr);
-  if (shape.parts > 1 && workspace_bytes < dense_parts_bytes(kp.Nq * nbh, shape.parts, kp.d)) shape = dense_shape(kp, nbh, false, save != nullptr);
+  const DenseShape shape = dense_call_shape(kp, nbh, workspace ? workspace_bytes : 0, save != nullptr);
   const size_t rows = (size_t)kp.Nq * nbh * shape.parts;
   const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), shape.parts};
   return save ? run_dense_shape(kp, nbh, shape, parts, *save, s) : run_dense_shape(kp, nbh, shape, parts, NoSave{}, s);

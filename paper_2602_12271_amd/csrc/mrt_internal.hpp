@@ -188,6 +188,7 @@ bool bf16_stage_l_out_streams(const KParams& kp);   // its last-iteration kernel
 // workspace: null, or scratch for the parts of a call whose keys are split (used if it holds
 // bf16_dense_workspace_bytes(), 0 for a call that is not split)
 size_t bf16_dense_workspace_bytes(const KParams& kp, int nbh, bool save);
+int bf16_dense_queries(const KParams& kp, int nbh, size_t workspace_bytes, bool save);   // of a workgroup
 // save: null, or what a training step keeps
 hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseSave* save, hipStream_t s);
 
