@@ -123,15 +123,17 @@ struct Stream {
 };
 
 // Unit of work of a workgroup: a tile of a (batch, head)'s own rows and one of `parts` runs of the streamed ones.
-// Without a mask every XCD gets a contiguous run of units, so that those that stream the same rows share its L2;
-// under a mask, where tiles differ in length, the longest go first.
+// Where every query sees every key (no mask, or a chunk against its cache) every XCD gets a contiguous run of units, so that
+// those that stream the same rows share its L2; under a mask, where tiles differ in length, the longest go first.  (The
+// cache of 32760 keys in the second order 2687 us instead of 2686, of 64 features 1580 instead of 1576, one frame of 1560
+// tokens and 3 heads against 8 frames 129 instead of 127: that order is for the calls it is meant for.)
 struct Unit {
   int bh, tile, part;
 };
 __device__ inline Unit unit_of(const DenseBwd& p, int unit, int n_heads, int tiles, int parts, bool last_first) {
   const int total = n_heads * tiles * parts;
   Unit u;
-  if (p.cc == 0) {
+  if (dense_last_key(p, 0, p.Nkv) == p.Nkv) {
     const int xcd = unit & 7;
     unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (unit >> 3);
     u.tile = unit % tiles;
