@@ -226,7 +226,8 @@ mrt_status monarch_attn_bwd_saved(const void* Q, const void* K, const void* V, c
 
 /* Dense baseline  O = softmax(scale * Q K^T + mask) V  (Sec. 2.2), flash-style, no workspace.
  * causal_chunk > 0 masks, per token, keys whose frame's chunk is later than the query frame's
- * chunk (query frames offset by q_frame_offset).  O may be Q itself, as for monarch_attn_fwd. */
+ * chunk (query frames offset by q_frame_offset; q_frame_offset + f_q below 2^31).  O may be Q itself, as for
+ * monarch_attn_fwd. */
 mrt_status dense_attn_check(const mrt_problem* p, int causal_chunk);
 mrt_status dense_attn_fwd(const void* Q, const void* K, const void* V, void* O,
                           const mrt_problem* p, int causal_chunk, void* hip_stream);

@@ -821,6 +821,11 @@ mrt_status dense_attn_check(const mrt_problem* p, int causal_chunk) {
   mrt_status st = check_common(p);
   if (st != MRT_OK) return st;
   if (causal_chunk < 0) { set_error("causal_chunk < 0"); return MRT_ERR_SHAPE; }
+  // (the kernels count frames, and one beyond the last, in 32 bits)
+  if (causal_chunk > 0 && (long long)p->q_frame_offset + p->f_q > 0x7fffffffll) {
+    set_error("q_frame_offset + f_q must be below 2^31 under a mask");
+    return MRT_ERR_SHAPE;
+  }
   return MRT_OK;
 }
 
