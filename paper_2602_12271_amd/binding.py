@@ -517,6 +517,11 @@ def _require_lse(lse, Q):
              "lse is fp32 [batch, heads, tokens], contiguous")
 
 
+def _require_scratch(workspace):
+    """(the library writes as many bytes from its address on as it is told that there are)"""
+    _require(workspace is None or workspace.is_contiguous(), "workspace must be contiguous", MRT_ERR_WORKSPACE)
+
+
 def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0, kv_len=None,
                         compute=MRT_COMPUTE_DEFAULT, out=None, lse=None, workspace=None, stream=None):
     """Forward call of a training step of the dense attention: (O, lse) for dense_attn_bwd.
@@ -532,6 +537,7 @@ def dense_attn_fwd_save(Q, K, V, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_off
     import torch
     lib = load_library()
     _same_device(Q, K, V, out, lse, kv_len, workspace)
+    _require_scratch(workspace)
 
     def call(s):
         O = torch.empty_like(Q) if out is None else out
@@ -577,6 +583,7 @@ def dense_attn_bwd(Q, K, V, O, dO, lse, *, f_q, f_kv, h, w, causal_chunk=0, q_fr
     import torch
     lib = load_library()
     _same_device(Q, K, V, O, dO, lse, kv_len, workspace, *(out or ()))
+    _require_scratch(workspace)
     _require_lse(lse, Q)
 
     def call(s):
