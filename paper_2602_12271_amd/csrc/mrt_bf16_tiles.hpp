@@ -47,6 +47,8 @@ __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
 // fma) and exponentiated with the hardware exp2, which saves a multiply per element.
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// a row's log-sum-exp from its reference and sum, which are base 2
+__device__ inline float natural_lse(float m, float sum) { return sum > 0.f ? kLn2 * m + logf(sum) : -INFINITY; }
 __device__ inline float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
 // Reductions over the four 16-lane rows of a wave, per lane column (lane & 15): the lanes that hold

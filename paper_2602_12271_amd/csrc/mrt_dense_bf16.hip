@@ -84,9 +84,6 @@ struct DenseParts {
   int n;
 };
 
-// A row's log-sum-exp from its reference and sum, which are base 2.
-__device__ inline float natural_lse(float m, float sum) { return sum > 0.f ? kLn2 * m + logf(sum) : -INFINITY; }
-
 // (64 features: two workgroups to a compute unit)
 // Save = DenseSave: a training step's call (heads that share keys, sequences of their own lengths, row statistics)
 template <int D, int QT, int WK, bool PART, typename Save>

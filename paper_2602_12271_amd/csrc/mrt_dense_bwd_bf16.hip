@@ -80,11 +80,11 @@ struct Stream {
   const u16 *a, *b;
   const float* stats;
   long long at, bt, anext, bnext;       // elements from row to row, and from the end of a head's rows to the next head's
-  int steps, per_head, left, left0, snext;
+  int steps, left, left0, snext;
   unsigned to, lds0, arow, brow;
   int wave, lane;
 
-  // n steps of rows from `row` on, `left` of them; the rows of a head end after per_head steps
+  // n steps of rows from `row` on, `left` of them; KV: then left0 rows of the next head
   __device__ inline void start(const u16* a_, long long at_, const u16* b_, long long bt_, const float* stats_, int n, int left_, int wave_, int lane_) {
     a = a_; b = b_; at = at_; bt = bt_; stats = stats_;
     steps = n; left = left_; wave = wave_; lane = lane_;

@@ -19,7 +19,6 @@ template <int D> constexpr int kLd = D + 4;                          // LDS row 
 template <int D> constexpr int kSlot = 2 * kStep * kLd<D>;
 
 __device__ inline f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
-__device__ inline float natural_lse(float m, float sum) { return sum > 0.f ? kLn2 * m + logf(sum) : -INFINITY; }
 
 template <int D, typename T, bool VEC, bool PART>
 __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_fwd(DenseFwd p) {

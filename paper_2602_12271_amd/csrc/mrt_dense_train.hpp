@@ -18,7 +18,7 @@ struct DenseBwd {
   const void *Q, *K, *V, *O, *dO;
   void *dQ, *dK, *dV;
   const float* lse;      // [batch][heads][Nq], natural logarithm; -inf: a row that sees no key
-  float* stats;          // [batch][heads][ceil(Nq / 32)][2][32]: -log2(e) lse, -delta (the launch of the queries writes them)
+  float* stats;          // [batch][heads][ceil(Nq / 32)][2][32]: -log2(e) lse, -delta (a launch before the tiles' writes them)
   float *pq, *pk, *pv;   // parts of dQ [part][batch heads][Nq][d], of dK and dV [part][batch kv_heads][Nkv][d]
   mrt_strides q, k, v, o, dout, dq, dk, dv;
   const int* kv_len;     // [batch] or null
