@@ -82,6 +82,8 @@ struct DenseParts {
   float* o;     // [part][bh][q][D]
   float2* ml;   // [part][bh][q]
   int n;
+  unsigned heads;   // of the batch
+  bool even;        // every query sees the same keys
 };
 
 // (64 features: two workgroups to a compute unit)
@@ -102,15 +104,17 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
   // tiles of a head different key counts the longest of all heads go first, or a long one is the last to
   // start (us, head by head | longest first, 128 features: 16 heads of 8192 causal tokens 452 | 271, 32 of
   // 4096 253 | 156, 12 of 14040 tokens in chunks of 4680 846 | 756, 32 of 2048 75 | 70; 64 features 549 | 465).
-  const int nx = (p.Nq + WGQ - 1) / WGQ, total = gridDim.x, xcd = blockIdx.x & 7, runs = total / nx;
+  // (The host says which, and how many heads there are: to find both out took a masked call of 7 us another 0.4.)
+  const int nx = (p.Nq + WGQ - 1) / WGQ, total = gridDim.x, xcd = blockIdx.x & 7;
   int run, tile;                                                   // run = (head, part)
-  if (visible(0) == visible(p.Nq - 1)) {
+  if (parts.even) {
     const int unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
     run = unit / nx;
     tile = unit - run * nx;
   } else {
-    tile = nx - 1 - blockIdx.x / runs;
-    run = blockIdx.x - (nx - 1 - tile) * runs;
+    const unsigned runs = PART ? parts.heads * parts.n : parts.heads, round = blockIdx.x / runs;
+    tile = nx - 1 - (int)round;
+    run = (int)(blockIdx.x - round * runs);
   }
   const int q0 = tile * WGQ;
   const int bh = PART ? run / parts.n : run, part = PART ? run - bh * parts.n : 0;
@@ -121,7 +125,7 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
     kvh = hd / save.group;
     if (save.kv_len) p.Nkv = __builtin_amdgcn_readfirstlane(min(max(save.kv_len[b], 0), p.Nkv));
     if (p.Nkv == 0) {                                     // an empty sequence
-      const long long row0 = PART ? ((long long)part * (total / (nx * parts.n)) + bh) * p.Nq : 0;
+      const long long row0 = PART ? ((long long)part * parts.heads + bh) * p.Nq : 0;
       for (int i = tid; i < WGQ * D; i += kDenseThreads) {
         const int q = q0 + i / D, f = i % D;
         if (q >= p.Nq) break;
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
     }
   }
   if constexpr (PART) {
-    const long long row0 = ((long long)part * (total / (nx * parts.n)) + bh) * p.Nq;
+    const long long row0 = ((long long)part * parts.heads + bh) * p.Nq;
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
       const int qi = qw0 + 16 * q + c;
@@ -592,7 +596,8 @@ int bf16_dense_queries(const KParams& kp, int nbh, size_t workspace_bytes, bool 
 hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseSave* save, hipStream_t s) {
   const DenseShape shape = dense_call_shape(kp, nbh, workspace ? workspace_bytes : 0, save != nullptr);
   const size_t rows = (size_t)kp.Nq * nbh * shape.parts;
-  const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), shape.parts};
+  const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), shape.parts, (unsigned)nbh,
+                            dense_visible(kp, 0) == dense_visible(kp, kp.Nq - 1)};
   return save ? run_dense_shape(kp, nbh, shape, parts, *save, s) : run_dense_shape(kp, nbh, shape, parts, NoSave{}, s);
 }
 
