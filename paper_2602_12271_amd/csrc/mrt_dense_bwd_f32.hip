@@ -20,6 +20,35 @@ template <int D> constexpr int kSlot = 2 * kStep * kLd<D> + 2 * kStep;
 
 __device__ inline f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+__device__ inline f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+// features v .. v + 7 of a row as they are stored, zeros from d on (EIGHT: in one access, rows of whole eights)
+template <bool VEC, bool EIGHT>
+__device__ inline bf16x8 ld8(const u16* row, int v, int d) {
+  if constexpr (EIGHT) {
+    typedef __attribute__((ext_vector_type(8), aligned(8))) __bf16 eight;
+    const eight x = *(const eight*)(row + (v < d ? v : 0));
+    return v < d ? (bf16x8)x : bf16x8{};
+  }
+  uint2 x[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h, v += 4) {
+    if constexpr (VEC) {
+      x[h] = *(const uint2*)(row + (v < d ? v : 0));
+      if (v >= d) x[h] = make_uint2(0, 0);
+    } else {
+      unsigned y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e] = row[v + e < d ? v + e : 0];
+        if (v + e >= d) y[e] = 0;
+      }
+      x[h] = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+    }
+  }
+  return __builtin_bit_cast(bf16x8, x);
+}
+
 template <int D, typename T, bool VEC, bool KV, bool PART>
 __device__ __forceinline__ void bwd_tile(const DenseBwd& p, int unit, float* lds) {
   constexpr int KS = D / 16, BLK = D / 64, LD = kLd<D>, QUADS = kStep * D / 4 / kThreads;
@@ -196,15 +225,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_f32_dense_bwd(DenseBwd p, int k
 //
 // bf16 storage: O was rounded to bf16, and where rows see few keys delta then costs as much as the rounding of the results
 // (10 causal tokens of 128 features: dQ and dK 2.3e-3 of the 2-norm off instead of 1.7e-3, 100 of them 1.9e-3 instead of
-// 1.7e-3), where their values are alike several times as much.  So sixteen rows that see at most kFewKeys keys form delta as
-// the sum of P dP, two tiles of sixteen keys a wave.
-constexpr int kFewKeys = 128;
+// 1.7e-3), where their values are alike several times as much.  So 32 rows that all see at most kFewKeys keys form delta as
+// the sum of P dP, a tile of 32 keys a wave.  Products of bf16 numbers are exact in 32 bits, so that the bf16 matrix unit
+// forms the same sums as the fp32 one.  The loads bound it: whole rows of eights as 16 bytes (64 heads of 100 causal tokens
+// of 128 features, us of the launch: 9.6, in eights of 8 bytes 15.3; with fp32 products, sixteen rows a workgroup, the
+// heads one by one 16.1; 3.3 with dO . O).
+constexpr int kFewKeys = 32 * kWaves;
 template <int D, typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_f32_dense_bwd_stats(DenseBwd p, int nqb) {
-  const long long tile = blockIdx.x >> 1;
-  const int bh = (int)(tile / nqb), r0 = 16 * (blockIdx.x & 1), q0 = (int)(tile - (long long)bh * nqb) * 32 + r0;
+  // (heads in turn: where there are eight or more, the workgroups of one reach the same XCD, whose L2 has its keys)
+  const unsigned heads = p.B * p.H, block = blockIdx.x / heads;
+  const int bh = blockIdx.x - block * heads, r0 = 16 * (block & 1), q0 = (int)(block >> 1) * 32;
   const int b = bh / p.H, hd = bh - b * p.H;
-  float* st = p.stats + tile * 64 + r0;
+  float* st = p.stats + ((long long)bh * nqb + (block >> 1)) * 64;
   const T* Op = (const T*)p.O + b * p.o.batch + hd * p.o.head;
   const T* dOp = (const T*)p.dO + b * p.dout.batch + hd * p.dout.head;
   auto negative_lse = [&](int q) {
@@ -212,54 +245,48 @@ __global__ __launch_bounds__(kThreads) void k_f32_dense_bwd_stats(DenseBwd p, in
     return lse == -INFINITY ? -INFINITY : -kLog2e * lse;
   };
   if constexpr (sizeof(T) == 2) {
-    const int keys = dense_seen_keys(p, b), most = dense_last_key(p, q0 + 15 < p.Nq ? q0 + 15 : p.Nq - 1, keys);
+    const int keys = dense_seen_keys(p, b), most = dense_last_key(p, q0 + 31 < p.Nq ? q0 + 31 : p.Nq - 1, keys);
     if (most > 0 && most <= kFewKeys) {
+      if (r0 > 0) return;                // (all rows are the other workgroup's)
       constexpr int KS = D / 16;
-      __shared__ float sums[kWaves][16];
-      const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-      const int q = q0 + c, lim = q < p.Nq ? dense_last_key(p, q, keys) : 0;
-      const long long row = q < p.Nq ? q : p.Nq - 1;
-      const T* Qr = (const T*)p.Q + b * p.q.batch + hd * p.q.head + row * p.q.token;
-      const T* Gr = dOp + row * p.dout.token;
-      const T* Kp = (const T*)p.K + b * p.k.batch + hd / p.group * p.k.head;
-      const T* Vp = (const T*)p.V + b * p.v.batch + hd / p.group * p.v.head;
+      __shared__ float sums[kWaves][32];
+      const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
+      const int q = q0 + c, k0 = 32 * wave, lim = q < p.Nq ? dense_last_key(p, q, keys) : 0;
+      const long long qr = q < p.Nq ? q : p.Nq - 1, kr = k0 + c < most ? k0 + c : most - 1;
+      const T* Qr = (const T*)p.Q + b * p.q.batch + hd * p.q.head + qr * p.q.token;
+      const T* Gr = dOp + qr * p.dout.token;
+      const T* Kr = (const T*)p.K + b * p.k.batch + hd / p.group * p.k.head + kr * p.k.token;
+      const T* Vr = (const T*)p.V + b * p.v.batch + hd / p.group * p.v.head + kr * p.v.token;
       const float nl = negative_lse(q), scale2 = p.scale * kLog2e;
-      float sum = 0.f;
-      for (int k0 = 16 * wave; k0 < most; k0 += 16 * kWaves) {
-        const long long kr = k0 + c < most ? k0 + c : most - 1;
-        f32x4 s[4], dp[4];               // rows: keys k0 + 4 g + r; columns: queries
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = dp[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x16 s = {}, dp = {};            // rows: keys k0 + 8 (r >> 2) + 4 hi + (r & 3); columns: queries
+      auto products = [&](auto eight) {
+        constexpr bool E = VEC && decltype(eight)::value;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const int v = 16 * ks + 4 * g;
-          const f32x4 k = blank4<VEC>(ld4<VEC>(Kp + kr * p.k.token, v, p.d), v, p.d), x = blank4<VEC>(ld4<VEC>(Vp + kr * p.v.token, v, p.d), v, p.d);
-          const f32x4 y = blank4<VEC>(ld4<VEC>(Qr, v, p.d), v, p.d), z = blank4<VEC>(ld4<VEC>(Gr, v, p.d), v, p.d);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[e] = mfma4(k[e], y[e], s[e]);
-            dp[e] = mfma4(x[e], z[e], dp[e]);
-          }
+          const int v = 16 * ks + 8 * hi;
+          s = mfma32(ld8<VEC, E>(Kr, v, p.d), ld8<VEC, E>(Qr, v, p.d), s);
+          dp = mfma32(ld8<VEC, E>(Vr, v, p.d), ld8<VEC, E>(Gr, v, p.d), dp);
         }
-        const f32x4 w = (s[0] + s[1]) + (s[2] + s[3]), a = (dp[0] + dp[1]) + (dp[2] + dp[3]);
+      };
+      if (p.d % 8 == 0) products(std::true_type{});
+      else products(std::false_type{});
+      float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float term = exp2_fast(fmaf(w[r], scale2, nl)) * a[r];
-          sum += k0 + 4 * g + r < lim ? term : 0.f;
-        }
+      for (int r = 0; r < 16; ++r) {
+        const float x = exp2_fast(fmaf(s[r], scale2, nl)) * dp[r];
+        sum += k0 + 8 * (r >> 2) + 4 * hi + (r & 3) < lim ? x : 0.f;
       }
-      sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
-      if (g == 0) sums[wave][c] = sum;
+      if (hi == 0) sums[wave][c] = sum;
       __syncthreads();
-      if (tid < 16) {
+      if (tid < 32) {
         st[c] = nl;
         st[32 + c] = -((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]));
       }
       return;
     }
   }
-  const int r = threadIdx.x >> 4, q = q0 + r, row = q < p.Nq ? q : p.Nq - 1;
+  const int r = r0 + (threadIdx.x >> 4), q = q0 + r, row = q < p.Nq ? q : p.Nq - 1;
   const T *o = Op + row * p.o.token, *dO = dOp + row * p.dout.token;
   float sum = 0.f;
 #pragma unroll
