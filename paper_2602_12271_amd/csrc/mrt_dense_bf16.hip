@@ -83,7 +83,7 @@ struct DenseParts {
   float2* ml;   // [part][bh][q]
   int n;
   unsigned heads;   // of the batch
-  bool even;        // every query sees the same keys
+  unsigned runs;    // heads x n where queries see different numbers of keys, else 0
 };
 
 // (64 features: two workgroups to a compute unit)
@@ -107,14 +107,14 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
   // (The host says which, and how many heads there are: to find both out took a masked call of 7 us another 0.4.)
   const int nx = (p.Nq + WGQ - 1) / WGQ, total = gridDim.x, xcd = blockIdx.x & 7;
   int run, tile;                                                   // run = (head, part)
-  if (parts.even) {
+  if (parts.runs == 0) {
     const int unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
     run = unit / nx;
     tile = unit - run * nx;
   } else {
-    const unsigned runs = PART ? parts.heads * parts.n : parts.heads, round = blockIdx.x / runs;
+    const unsigned round = blockIdx.x / parts.runs;
     tile = nx - 1 - (int)round;
-    run = (int)(blockIdx.x - round * runs);
+    run = (int)(blockIdx.x - round * parts.runs);
   }
   const int q0 = tile * WGQ;
   const int bh = PART ? run / parts.n : run, part = PART ? run - bh * parts.n : 0;
@@ -596,8 +596,9 @@ int bf16_dense_queries(const KParams& kp, int nbh, size_t workspace_bytes, bool 
 hipError_t launch_bf16_dense(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseSave* save, hipStream_t s) {
   const DenseShape shape = dense_call_shape(kp, nbh, workspace ? workspace_bytes : 0, save != nullptr);
   const size_t rows = (size_t)kp.Nq * nbh * shape.parts;
+  const bool even = dense_visible(kp, 0) == dense_visible(kp, kp.Nq - 1);
   const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), shape.parts, (unsigned)nbh,
-                            dense_visible(kp, 0) == dense_visible(kp, kp.Nq - 1)};
+                            even ? 0u : (unsigned)nbh * shape.parts};
   return save ? run_dense_shape(kp, nbh, shape, parts, *save, s) : run_dense_shape(kp, nbh, shape, parts, NoSave{}, s);
 }
 
