@@ -100,3 +100,20 @@ def test_bf16_tensors_in_fp32_arithmetic(name):
     got = run(c, q, k, v, do, kv_len)
     torch.cuda.synchronize()
     check_short(c, got, q, k, v, do, range(c.batch))
+
+
+@pytest.mark.parametrize("dim,shift", [(40, 4), (64, 4), (128, 4), (128, 12), (64, 1), (37, 3)])
+def test_rows_that_begin_anywhere(dim, shift):
+    """Rows of bf16 numbers in fp32 arithmetic that begin at 8 or 2 bytes, the last of them at the end of its memory."""
+    c = Step(40, 40, heads=3, kv_heads=1, batch=2, chunk=1, dim=dim, compute=1)
+    wide = []
+    for x in alike(c, seed=33)[:4]:
+        b, h, n, d = x.shape
+        memory = torch.full((b, n, h, d + shift), 7.0, dtype=x.dtype, device="cuda")
+        memory[..., shift:] = x.transpose(1, 2)
+        wide.append(memory[..., shift:].transpose(1, 2))
+    q, k, v, do = wide
+    assert q.data_ptr() % 16 and q.stride(3) == 1
+    got = run(c, q, k, v, do, None)
+    torch.cuda.synchronize()
+    check_short(c, got, q, k, v, do, range(c.batch))
