@@ -259,12 +259,13 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
  * Arithmetic.  MRT_BF16 storage with MRT_COMPUTE_DEFAULT (head_dim 64 or 128): bf16 matrix operands (the
  *   probabilities and the gradients of the logits are rounded to bf16, by 2^-8 of the value at most), fp32
  *   accumulation; gradients within 1e-2 of the exact ones in the 2-norm of a head (typically 2.4e-3).
- *   Otherwise fp32 products and sums: within 1e-5 in fp32 storage; in bf16 storage the results are rounded (1.7e-3), and
- *   rows that see more than 128 keys take delta = dO . O from the rounded O: within 5e-3, typically 1.7e-3.
+ *   Otherwise fp32 products and sums: within 1e-5 in fp32 storage; in bf16 storage the results are rounded: within 5e-3,
+ *   typically 1.7e-3.
  *   The same call gives the same bits every time (no atomics).
- *   In bf16 storage the rounding of O moves delta of rows of more than 128 keys by up to 2^-8 of sum |dO| |O|, which counts for
- *   more where dO V^T hardly differs over the keys that weigh: values with a large common part, or a row's weight on one
- *   key (logits of hundreds, 3 rows over 400 keys: dQ and dK 2.5e-2 off).
+ *   In bf16 storage O comes rounded: delta = dO . O is off by up to 2^-8 of sum |dO| |O|.  Blocks of 32 rows that all see at
+ *   most 128 keys form delta from P and dO V^T instead; on the others this counts for more than the above where dO V^T
+ *   hardly differs over the keys that weigh: values with a large common part, or a row's weight on one key (logits of
+ *   hundreds, 3 rows over 400 keys: dQ and dK 2.5e-2 off).
  *   The backward call forms a weight from a logit and lse, 32-bit numbers: its relative error is 2^-23 of their magnitude
  *   (1e-3 at 10^4) on top of the above.
  * Limits, as for dense_attn_fwd, and: scale at least 1e-30; token strides of the backward call's bf16 tensors at most 2^25
