@@ -259,8 +259,8 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
  * Arithmetic.  MRT_BF16 storage with MRT_COMPUTE_DEFAULT (head_dim 64 or 128): bf16 matrix operands (the
  *   probabilities and the gradients of the logits are rounded to bf16, by 2^-8 of the value at most), fp32
  *   accumulation; gradients within 1e-2 of the exact ones in the 2-norm of a head (typically 2.4e-3).
- *   Otherwise fp32 products and sums: within 1e-5 in fp32 storage; in bf16 storage the results are rounded: within 5e-3,
- *   typically 1.7e-3.
+ *   Otherwise fp32 products and sums: within 1e-5 in fp32 storage; in bf16 storage the results are rounded: within 5e-3
+ *   from 8 features on (2e-2 below), typically 1.7e-3.
  *   The same call gives the same bits every time (no atomics).
  *   In bf16 storage O comes rounded: delta = dO . O is off by up to 2^-8 of sum |dO| |O|.  Blocks of 32 rows that all see at
  *   most 128 keys form delta from P and dO V^T instead; on the others this counts for more than the above where dO V^T
