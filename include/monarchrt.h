@@ -336,6 +336,90 @@ mrt_status mrt_rotary_fwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n
 mrt_status mrt_rotary_bwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n, const void* const* dY, void* const* dX,
                       void* hip_stream);
 
+/* Root-mean-square norms of queries and keys, a row x of every head by itself, and their rotary positions in one pass:
+ *     y = turn(x w / sqrt(mean(x x) + eps))
+ *   t          shapes, positions, strides and types as for mrt_rotary_fwd.  Backward: t.x and t.x_dtype describe X (the norm's
+ *              input) and t.y and t.y_dtype dY; dX has the type of X and the strides dx.
+ *   weight     device memory, [head_dim], or a row for every head, weight_head elements apart (0: one that they share); NULL: ones.
+ *   dweight    backward: device memory, fp32, [head_dim], or [heads, head_dim] where every head has a weight: the sum over
+ *              batch, tokens and the heads that share it; NULL: not wanted.  Fully overwritten.
+ * Statistics, products and sums in fp32, rounded once to the type of the result; the same call gives the same bits.  A row of zeros
+ *   gives zeros, and a gradient scaled by 1 / sqrt(eps).  A row whose sum of squares passes the range of fp32 (entries beyond 1e18)
+ *   is not supported: what it gives is unspecified, other rows are as ever.
+ * eps: 1e-30 .. 1e30.  Y may be X itself with the same type and strides; otherwise no output overlaps an input or another output.
+ * The backward call recomputes the statistics from X; it needs mrt_norm_rotary_bwd_workspace_bytes() bytes of scratch (device,
+ *   256-byte aligned, contents undefined on entry and exit; 0: none, or invalid arguments) where gradients of weights are wanted. */
+typedef struct {
+  mrt_rotary_tensor t;
+  const void* weight;
+  mrt_dtype weight_dtype;
+  long long weight_head;
+  mrt_strides dx;
+  float* dweight;
+} mrt_norm_tensor;
+mrt_status mrt_norm_rotary_check(const mrt_rotary* r, double eps, const mrt_norm_tensor* x, int n, int backward);
+mrt_status mrt_norm_rotary_fwd(const mrt_rotary* r, double eps, const mrt_norm_tensor* x, int n, const void* const* X,
+                      void* const* Y, void* hip_stream);
+size_t mrt_norm_rotary_bwd_workspace_bytes(const mrt_rotary* r, const mrt_norm_tensor* x, int n);
+mrt_status mrt_norm_rotary_bwd(const mrt_rotary* r, double eps, const mrt_norm_tensor* x, int n, const void* const* X,
+                      const void* const* dY, void* const* dX, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* A cache of keys and values in 8 bits, and the dense attention over it.
+ * Codes [batch, heads, capacity, head_dim], e4m3 (four significant bits, up to 448) or whole numbers of -127 .. 127, and a power
+ * of two 2^(byte - 127) for every `block` tokens of a (batch, head), in bytes [batch, heads, ceil(capacity / block)].  A value is
+ * code x power, a bf16 number exactly.  Keys and values each have codes and powers of their own.
+ *   k, v                  element (byte) strides of the codes, multiples of 16; head_dim is contiguous
+ *   k_scale_batch ...     strides of the power bytes; blocks are contiguous
+ *   heads                 key heads; head_dim: a multiple of 16, up to 256 (the attention: 64 or 128)
+ *   block                 16, 32, 64 or 128; capacity: 1 .. 2^24 tokens
+ * Code pointers are 16-byte aligned.
+ *
+ * mrt_cache8_write appends or replaces rows: K and V [batch, heads, tokens, head_dim] go to the tokens at .. at + tokens - 1, and
+ *   what was behind them in the last block they touch is no longer part of the cache (its codes stay as they were, its scale
+ *   does not).  Rows of the first block before `at` keep their values.  The scale of a block is the smallest power of two that brings
+ *   its largest finite magnitude, new rows and kept ones, to 448 (127) or below, within 2^-124 .. 2^119; codes are the nearest, ties
+ *   to even.  So a value is off by at most 2^-4 of itself (e4m3; 2^-10 of the scale below 2^-6 of it), or by half the scale, 2^-7 of
+ *   the block's largest magnitude (whole numbers).  Where the scale grows kept rows are rounded again: an e4m3 code only where it turns
+ *   subnormal, a whole number by less than one unit of the final scale in all, however often.  Infinite and larger magnitudes become the largest code; NaN stays NaN in e4m3
+ *   and becomes 0 in whole numbers.
+ * mrt_cache8_read writes the values of the tokens at .. at + tokens - 1 to K and V, [batch, heads, tokens, head_dim], bf16 or fp32,
+ *   exactly; zeros for tokens outside the cache.
+ *   at_each      device memory, int [batch], or NULL: the first token of every sequence, in the place of `at`.  Rows that it brings
+ *                outside 0 .. capacity - 1 are left out.  (`at` on the host has to leave all rows inside.)
+ *   tokens_each  device memory, int [batch], or NULL (write only): rows of every sequence that are there (taken as 0 .. tokens): a
+ *                padded batch.  With 0 nothing of the sequence changes.
+ *   k, v         element strides of K and V: rows are moved 16 bytes at a time, pointers and strides are multiples of that.
+ * dense_attn_fwd_cache8: dense_attn_fwd_save over the first f_kv*h*w tokens of a cache: queries and O bf16, MRT_COMPUTE_DEFAULT,
+ *   p->k and p->v not looked at.  kv_len: device memory, int [batch], or NULL, as mrt_dense_train.kv_len; masks, shared key heads,
+ *   lse, rows that see no key, and infinities (NaN codes) as there.  Values meet the matrix unit unrounded; probabilities are rounded
+ *   to bf16.  dense_attn_fwd_cache8_workspace_bytes: scratch that the call makes use of (0: none); without it the call does the same work
+ *   with fewer workgroups, and its results differ by roundings.  The same call gives the same bits every time.
+ *   Limits, as for dense_attn_fwd_save, and: heads / key heads whole. */
+typedef enum { MRT_CACHE_E4M3 = 0, MRT_CACHE_INT8 = 1 } mrt_cache_format;
+typedef struct {
+  int batch, heads, head_dim;
+  int capacity, block;
+  mrt_cache_format format;
+  mrt_strides k, v;
+  long long k_scale_batch, k_scale_head, v_scale_batch, v_scale_head;
+  void *k_codes, *v_codes;              /* device memory, like the next two */
+  unsigned char *k_scales, *v_scales;
+} mrt_cache8;
+typedef struct {
+  int tokens, at;
+  const int* at_each;
+  const int* tokens_each;
+  mrt_strides k, v;
+  mrt_dtype dtype;
+} mrt_cache8_rows;
+mrt_status mrt_cache8_check(const mrt_cache8* c, const mrt_cache8_rows* r);
+mrt_status mrt_cache8_write(const mrt_cache8* c, const mrt_cache8_rows* r, const void* K, const void* V, void* hip_stream);
+mrt_status mrt_cache8_read(const mrt_cache8* c, const mrt_cache8_rows* r, void* K, void* V, void* hip_stream);
+mrt_status dense_attn_cache8_check(const mrt_problem* p, const mrt_cache8* c, int causal_chunk);
+size_t dense_attn_fwd_cache8_workspace_bytes(const mrt_problem* p, const mrt_cache8* c, int causal_chunk);
+mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, float* lse, const mrt_problem* p, const int* kv_len,
+                                 int causal_chunk, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Number of head groups monarch_attn_fwd and monarch_attn_bwd run concurrently: 1..4, or 0 (default) to let the library
  * choose per call (one group unless the launches are long and their grids small).  With more than one
  * group the library forks helper HIP streams from hip_stream and joins them back before it
@@ -355,10 +439,10 @@ void mrt_set_head_groups(int n);
  * mrt_profile_read waits for the recorded events, writes up to `capacity` (elapsed milliseconds
  * per launch, kernel kind) pairs in launch order, forgets them and returns how many it wrote.
  * Kernel kind = one of MRT_KERNEL_STAGE_R / MRT_KERNEL_STAGE_L / MRT_KERNEL_DENSE, MRT_KERNEL_DENSE_BWD
- * (all launches of a dense_attn_bwd call) or MRT_KERNEL_ROTARY, or-ed with
+ * (all launches of a dense_attn_bwd call), MRT_KERNEL_ROTARY (norms with them, too) or MRT_KERNEL_CACHE, or-ed with
  * MRT_KERNEL_FIRST (first iteration: alpha_R is Q itself) and MRT_KERNEL_LAST (last iteration:
  * stage R also forms Y, stage L forms O). */
-enum { MRT_KERNEL_STAGE_R = 1, MRT_KERNEL_STAGE_L = 2, MRT_KERNEL_DENSE = 4, MRT_KERNEL_DENSE_BWD = 8, MRT_KERNEL_ROTARY = 64,
+enum { MRT_KERNEL_STAGE_R = 1, MRT_KERNEL_STAGE_L = 2, MRT_KERNEL_DENSE = 4, MRT_KERNEL_DENSE_BWD = 8, MRT_KERNEL_ROTARY = 64, MRT_KERNEL_CACHE = 128,
        MRT_KERNEL_FIRST = 16, MRT_KERNEL_LAST = 32 };
 void mrt_profile_enable(int repeats);
 int mrt_profile_read(float* ms, int* kind, int capacity);

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmonarchrt.so")
@@ -28,11 +28,14 @@ EXPORTED = [
     "dense_attn_workspace_bytes", "dense_attn_fwd_ws",
     "dense_attn_fwd_save", "dense_attn_fwd_save_workspace_bytes", "dense_attn_fwd_save_queries", "dense_attn_bwd", "dense_attn_bwd_check", "dense_attn_bwd_workspace_bytes",
     "mrt_rotary_check", "mrt_rotary_fwd", "mrt_rotary_bwd",
+    "mrt_norm_rotary_check", "mrt_norm_rotary_fwd", "mrt_norm_rotary_bwd", "mrt_norm_rotary_bwd_workspace_bytes",
+    "mrt_cache8_check", "mrt_cache8_write", "mrt_cache8_read",
+    "dense_attn_cache8_check", "dense_attn_fwd_cache8", "dense_attn_fwd_cache8_workspace_bytes",
 ]
 NOALLOC_SCRATCH_BYTES = 128 << 20
 ASSIGNMENTS = {"fh_w": 0, "w_fh": 1, "fw_h": 2, "h_fw": 3, "f_hw": 4, "hw_f": 5}
 KERNEL_STAGE_R, KERNEL_STAGE_L, KERNEL_DENSE, KERNEL_FIRST, KERNEL_LAST = 1, 2, 4, 16, 32
-KERNEL_DENSE_BWD, KERNEL_ROTARY = 8, 64
+KERNEL_DENSE_BWD, KERNEL_ROTARY, KERNEL_CACHE = 8, 64, 128
 ROTARY_LAYOUTS = {"adjacent": 0, "halves": 1}
 ROTARY_LADDERS = {"axis": 0, "shared": 1}
 
@@ -67,6 +70,25 @@ class MrtRotaryTensor(ctypes.Structure):
                 ("w", ctypes.c_int), ("frame_offset", ctypes.c_int), ("x", MrtStrides), ("y", MrtStrides),
                 ("x_dtype", ctypes.c_int), ("y_dtype", ctypes.c_int), ("positions", ctypes.c_void_p),
                 ("position_batch", ctypes.c_longlong), ("position_axis", ctypes.c_longlong)]
+
+
+class MrtNormTensor(ctypes.Structure):
+    _fields_ = [("t", MrtRotaryTensor), ("weight", ctypes.c_void_p), ("weight_dtype", ctypes.c_int),
+                ("weight_head", ctypes.c_longlong), ("dx", MrtStrides), ("dweight", ctypes.c_void_p)]
+
+
+class MrtCache8(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("capacity", ctypes.c_int),
+                ("block", ctypes.c_int), ("format", ctypes.c_int), ("k", MrtStrides), ("v", MrtStrides),
+                ("k_scale_batch", ctypes.c_longlong), ("k_scale_head", ctypes.c_longlong),
+                ("v_scale_batch", ctypes.c_longlong), ("v_scale_head", ctypes.c_longlong),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class MrtCache8Rows(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int), ("at", ctypes.c_int), ("at_each", ctypes.c_void_p), ("tokens_each", ctypes.c_void_p),
+                ("k", MrtStrides), ("v", MrtStrides), ("dtype", ctypes.c_int)]
 
 
 class MrtError(RuntimeError):
@@ -138,6 +160,23 @@ def load_library() -> ctypes.CDLL:
     lib.mrt_rotary_check.restype = ci
     for f in (lib.mrt_rotary_fwd, lib.mrt_rotary_bwd):
         f.argtypes = [R, X, ci, vp, vp, vp]
+        f.restype = ci
+    N = ctypes.POINTER(MrtNormTensor)
+    cd = ctypes.c_double
+    lib.mrt_norm_rotary_check.argtypes = [R, cd, N, ci, ci]
+    lib.mrt_norm_rotary_fwd.argtypes = [R, cd, N, ci, vp, vp, vp]
+    lib.mrt_norm_rotary_bwd.argtypes = [R, cd, N, ci, vp, vp, vp, vp, sz, vp]
+    lib.mrt_norm_rotary_bwd_workspace_bytes.argtypes = [R, N, ci]
+    lib.mrt_norm_rotary_bwd_workspace_bytes.restype = sz
+    C, W = ctypes.POINTER(MrtCache8), ctypes.POINTER(MrtCache8Rows)
+    lib.mrt_cache8_check.argtypes = [C, W]
+    lib.mrt_cache8_write.argtypes = lib.mrt_cache8_read.argtypes = [C, W, vp, vp, vp]
+    lib.dense_attn_cache8_check.argtypes = [P, C, ci]
+    lib.dense_attn_fwd_cache8_workspace_bytes.argtypes = [P, C, ci]
+    lib.dense_attn_fwd_cache8_workspace_bytes.restype = sz
+    lib.dense_attn_fwd_cache8.argtypes = [vp, C, vp, vp, P, vp, ci, vp, sz, vp]
+    for f in (lib.mrt_norm_rotary_check, lib.mrt_norm_rotary_fwd, lib.mrt_norm_rotary_bwd, lib.mrt_cache8_check,
+              lib.mrt_cache8_write, lib.mrt_cache8_read, lib.dense_attn_cache8_check, lib.dense_attn_fwd_cache8):
         f.restype = ci
     lib.mrt_status_string.argtypes = [ci]
     lib.mrt_status_string.restype = ctypes.c_char_p
@@ -702,3 +741,307 @@ def rotary_bwd(dQ, dK=None, *, f_q=None, f_kv=None, h=None, w=None, q_frame_offs
     the arguments of that call.  dtype: of the results, e.g. bf16 for the fp32 gradients of monarch_attn_bwd."""
     return _rotary("mrt_rotary_bwd", dQ, dK, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder,
                    q_positions, k_positions, dtype, out, k_out, stream)
+
+
+# ---- norms of queries and keys with their rotary positions ---------------------------------------
+# (description, tensors without addresses) of recent calls by their values, like _problems
+_norm_problems: dict = {}
+
+
+def _norm_weight(weight, x, name):
+    if weight is None:
+        return None, MRT_F32, 0
+    d = x.shape[-1]
+    _require(weight.shape in ((d,), (x.shape[1], d)) and (d == 1 or weight.stride(-1) == 1),
+             f"{name}: the weight is [{d}] or [{x.shape[1]}, {d}], head_dim contiguous")
+    return weight, _dtype_of(weight, name + "'s weight"), weight.stride(0) if weight.dim() == 2 and x.shape[1] > 1 else 0
+
+
+def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder, positions):
+    """x, y, dx: the norm's input, its result (or the gradient of that) and the gradient of x, of one or two tensors."""
+    key = (tuple([_layout_of(t) for t in (*x, *y, *dx, *weights, *positions)]), len(x), f_q, f_kv, h, w, q_frame_offset,
+           kv_frame_offset, theta, None if split is None else tuple(split), layout, ladder)
+    found = _norm_problems.get(key)
+    if found is not None:
+        return found
+    _require(layout in ROTARY_LAYOUTS, f"layout is one of {sorted(ROTARY_LAYOUTS)}")
+    _require(ladder in ROTARY_LADDERS, f"ladder is one of {sorted(ROTARY_LADDERS)}")
+    pairs = tuple(rotary_pairs_split(x[0].shape[-1]) if split is None else split)
+    _require(len(pairs) == 3, "split: rotary pairs of the frame, height and width axis")
+    r = MrtRotary(x[0].shape[-1], (ctypes.c_int * 3)(*pairs), ROTARY_LAYOUTS[layout], ROTARY_LADDERS[ladder], theta)
+    tensors = []
+    for i, name in zip(range(len(x)), "QK"):
+        _require(x[i].shape[-1] == x[0].shape[-1], "Q and K have one head_dim")
+        t = _rotary_tensor(x[i], y[i], (f_q if i == 0 or f_kv is None else f_kv), h, w, kv_frame_offset if i else q_frame_offset,
+                           positions[i], name)
+        _, dtype, apart = _norm_weight(weights[i], x[i], name)
+        strides = MrtStrides()
+        if dx:
+            _require(dx[i].shape == x[i].shape and dx[i].dtype == x[i].dtype and dx[i].stride(3) == 1,
+                     f"{name}: the gradient has its shape and type, head_dim contiguous")
+            strides = MrtStrides(*dx[i].stride()[:3])
+        tensors.append(MrtNormTensor(t, None, dtype, apart, strides, None))
+    found = r, (MrtNormTensor * len(x))(*tensors), ctypes.c_void_p * len(x)
+    if len(_norm_problems) >= _MAX_PROBLEMS:
+        _norm_problems.clear()
+    _norm_problems[key] = found
+    return found
+
+
+def _norm_tensors(tensors, weights, positions, dweights=()):
+    """The description with the call's addresses (one that is shared is not written)."""
+    tensors = type(tensors).from_buffer_copy(tensors)
+    for i, t in enumerate(tensors):
+        if weights[i] is not None:
+            t.weight = weights[i].data_ptr()
+        if positions[i] is not None:
+            t.t.positions = positions[i].data_ptr()
+        if dweights and dweights[i] is not None:
+            t.dweight = dweights[i].data_ptr()
+    return tensors
+
+
+def norm_rotary_fwd(Q, K=None, q_weight=None, k_weight=None, *, eps=1e-6, f_q=None, f_kv=None, h=None, w=None, q_frame_offset=0,
+                    kv_frame_offset=0, theta=10000.0, split=None, layout="adjacent", ladder="axis", q_positions=None,
+                    k_positions=None, dtype=None, out=None, k_out=None, stream=None):
+    """Root-mean-square norms of Q and K, [batch, heads, tokens, head_dim], every head of a token by itself, and their rotary
+    positions, in one launch: (Q', K'), or Q' where K is None.
+
+    q_weight / k_weight: [head_dim], or [heads, head_dim] for a weight of every head, fp32 or bf16; None: ones.  The other
+    arguments are those of rotary_fwd.  Statistics and products in fp32, rounded once to `dtype` (that of Q and K by
+    default)."""
+    lib = load_library()
+    import torch
+    _require(K is not None or (k_out is None and k_positions is None and k_weight is None),
+             "k_out, k_positions and k_weight are for a call with K")
+    for y in (out, k_out):
+        _require(y is None or dtype is None or y.dtype == dtype, "dtype is not that of the given output")
+    _same_device(Q, K, q_weight, k_weight, q_positions, k_positions, out, k_out)
+
+    def call(s):
+        x, y = [Q], [torch.empty_like(Q, dtype=dtype) if out is None else out]
+        if K is not None:
+            x.append(K)
+            y.append(torch.empty_like(K, dtype=dtype) if k_out is None else k_out)
+        weights, positions = (q_weight, k_weight), (q_positions, k_positions)
+        r, tensors, pointers = _norm_problem(x, y, (), weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
+                                             layout, ladder, positions)
+        tensors = _norm_tensors(tensors, weights, positions)
+        st = lib.mrt_norm_rotary_fwd(ctypes.byref(r), eps, tensors, len(x), pointers(*[t.data_ptr() for t in x]),
+                                     pointers(*[t.data_ptr() for t in y]), s)
+        if st != MRT_OK:
+            _raise(lib, st)
+        return tuple(y) if len(y) > 1 else y[0]
+    return _run_on(Q, stream, call)
+
+
+def norm_rotary_bwd(Q, K, q_weight, k_weight, dQ, dK=None, *, eps=1e-6, f_q=None, f_kv=None, h=None, w=None, q_frame_offset=0,
+                    kv_frame_offset=0, theta=10000.0, split=None, layout="adjacent", ladder="axis", q_positions=None,
+                    k_positions=None, out=None, k_out=None, workspace=None, stream=None):
+    """Gradients with respect to norm_rotary_fwd's inputs, from those of its results, dQ and dK: (dQ, dK, dq_weight,
+    dk_weight), with the arguments of that call.  K and dK are None together.  Gradients of Q and K have their types (those
+    that come in may have others); gradients of weights are fp32 in the weights' shapes, summed over batch, tokens and the
+    heads that share them, None where there is no weight.  out / k_out: where the gradients of Q and K belong.
+    workspace: scratch (torch's by default)."""
+    lib = load_library()
+    import torch
+    _require((K is None) == (dK is None) and (K is not None or (k_out is None and k_positions is None and k_weight is None)),
+             "K and dK come together; k_out, k_positions and k_weight are for a call with K")
+    _same_device(Q, K, q_weight, k_weight, dQ, dK, q_positions, k_positions, out, k_out, workspace)
+    _require_scratch(workspace)
+
+    def call(s):
+        x, g, dx = [Q], [dQ], [torch.empty_like(Q) if out is None else out]
+        if K is not None:
+            x.append(K)
+            g.append(dK)
+            dx.append(torch.empty_like(K) if k_out is None else k_out)
+        weights, positions = (q_weight, k_weight), (q_positions, k_positions)
+        r, tensors, pointers = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
+                                             layout, ladder, positions)
+        dw = [None if u is None else torch.empty(u.shape, dtype=torch.float32, device=Q.device) for u in weights]
+        tensors = _norm_tensors(tensors, weights, positions, dw)
+        nbytes = lib.mrt_norm_rotary_bwd_workspace_bytes(ctypes.byref(r), tensors, len(x))
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if workspace is None and nbytes else workspace
+        ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
+        st = lib.mrt_norm_rotary_bwd(ctypes.byref(r), eps, tensors, len(x), pointers(*[t.data_ptr() for t in x]),
+                                     pointers(*[t.data_ptr() for t in g]), pointers(*[t.data_ptr() for t in dx]), ws, nbytes, s)
+        if st != MRT_OK:
+            _raise(lib, st)
+        return dx[0], dx[1] if K is not None else None, dw[0], dw[1]
+    return _run_on(Q, stream, call)
+
+
+# ---- a cache of keys and values in 8 bits --------------------------------------------------------
+class Cache8(NamedTuple):
+    """K, V: codes [batch, heads, capacity, head_dim], torch.float8_e4m3fn or torch.int8.  K_scale, V_scale: uint8
+    [batch, heads, ceil(capacity / block)], the exponent + 127 of the power of two that `block` tokens share."""
+    K: object
+    V: object
+    K_scale: object
+    V_scale: object
+    block: int
+
+
+def cache8(batch, heads, capacity, head_dim, *, format="e4m3", block=64, device="cuda"):
+    """An empty cache (all values zero).  format: "e4m3" or "int8"."""
+    import torch
+    _require(format in ("e4m3", "int8"), "format is e4m3 or int8")
+    _require(block in (16, 32, 64, 128), "block is 16, 32, 64 or 128")
+    dtype = torch.float8_e4m3fn if format == "e4m3" else torch.int8
+    codes = [torch.zeros(batch, heads, capacity, head_dim, dtype=torch.uint8, device=device).view(dtype) for _ in range(2)]
+    scales = [torch.full((batch, heads, -(-capacity // block)), 3, dtype=torch.uint8, device=device) for _ in range(2)]
+    return Cache8(*codes, *scales, block)
+
+
+# descriptions of recent caches without addresses, by their values, like _problems
+_caches: dict = {}
+
+
+def _cache8_of(c):
+    key = (c.K.shape, c.K.stride(), c.K.dtype, c.V.shape, c.V.stride(), c.V.dtype, _layout_of(c.K_scale), _layout_of(c.V_scale), c.block,
+           type(c.block))
+    found = _caches.get(key)
+    if found is None:
+        import torch
+        _require(c.K.dim() == 4 and c.V.shape == c.K.shape and c.K.dtype == c.V.dtype and
+                 c.K.dtype in (torch.float8_e4m3fn, torch.int8),
+                 "K and V of a cache are [batch, heads, capacity, head_dim], torch.float8_e4m3fn or torch.int8")
+        _require(type(c.block) is int and c.block in (16, 32, 64, 128), "block is 16, 32, 64 or 128")
+        B, H, n, d = c.K.shape
+        blocks = -(-n // c.block)
+        for x in (c.K_scale, c.V_scale):
+            _require(x.dtype == torch.uint8 and x.shape == (B, H, blocks) and (blocks == 1 or x.stride(2) == 1),
+                     f"scales of the cache are uint8 [{B}, {H}, {blocks}], blocks contiguous")
+        _require(c.K.stride(3) == 1 and c.V.stride(3) == 1, "head_dim must be contiguous")
+        found = MrtCache8(B, H, d, n, c.block, 0 if c.K.dtype == torch.float8_e4m3fn else 1, MrtStrides(*c.K.stride()[:3]),
+                          MrtStrides(*c.V.stride()[:3]), *c.K_scale.stride()[:2], *c.V_scale.stride()[:2])
+        if len(_caches) >= _MAX_PROBLEMS:
+            _caches.clear()
+        _caches[key] = found
+    found = MrtCache8.from_buffer_copy(found)
+    found.k_codes, found.v_codes = c.K.data_ptr(), c.V.data_ptr()
+    found.k_scales, found.v_scales = c.K_scale.data_ptr(), c.V_scale.data_ptr()
+    return found
+
+
+def _cache8_rows(cache, K, V, at, lengths):
+    import torch
+    B, H, _, d = cache.K.shape
+    _require(K.dim() == 4 and K.shape == V.shape and K.shape[:2] == (B, H) and K.shape[3] == d and K.dtype == V.dtype,
+             f"K and V are [{B}, {H}, tokens, {d}] of one type")
+    _require(K.stride(3) == 1 and V.stride(3) == 1, "head_dim must be contiguous")
+    each = []
+    for name, x in (("at", None if type(at) is int else at), ("lengths", lengths)):
+        _require(x is None or (isinstance(x, torch.Tensor) and x.dtype == torch.int32 and x.shape == (B,) and x.is_contiguous()),
+                 f"{name}: int32 [{B}], contiguous" + (", or a number" if name == "at" else ""))
+        each.append(None if x is None else x.data_ptr())
+    return MrtCache8Rows(K.shape[2], at if type(at) is int else 0, *each, MrtStrides(*K.stride()[:3]), MrtStrides(*V.stride()[:3]),
+                         _dtype_of(K, "K"))
+
+
+def cache8_write(cache, K, V, *, at=0, lengths=None, stream=None):
+    """Rows K and V, [batch, heads, tokens, head_dim], fp32 or bf16, into the cache, from token `at` on: a number, or int32
+    [batch] on the device (rows outside the cache are then left out).  lengths (int32 [batch], on the device): rows of every
+    sequence that are there.  Rows before `at` keep their values; what was behind the new ones in their last block is no longer
+    part of the cache.  The rounding is in the header's comment."""
+    lib = load_library()
+    _same_device(K, V, cache.K, cache.V, cache.K_scale, cache.V_scale, None if type(at) is int else at, lengths)
+
+    def call(s):
+        c, rows = _cache8_of(cache), _cache8_rows(cache, K, V, at, lengths)
+        st = lib.mrt_cache8_write(ctypes.byref(c), ctypes.byref(rows), K.data_ptr(), V.data_ptr(), s)
+        if st != MRT_OK:
+            _raise(lib, st)
+    _run_on(K, stream, call)
+
+
+def cache8_read(cache, tokens, *, at=0, dtype=None, out=None, v_out=None, stream=None):
+    """The cache's values (K, V) of `tokens` tokens from `at` on (a number, or int32 [batch] on the device: tokens outside the
+    cache give zeros), [batch, heads, tokens, head_dim], bf16 (the default) or fp32, exactly: for an attention that takes them so."""
+    lib = load_library()
+    import torch
+    for y in (out, v_out):
+        _require(y is None or dtype is None or y.dtype == dtype, "dtype is not that of the given output")
+    _same_device(cache.K, cache.V, cache.K_scale, cache.V_scale, None if type(at) is int else at, out, v_out)
+
+    def call(s):
+        B, H, _, d = cache.K.shape
+        given = dtype if dtype is not None else out.dtype if out is not None else v_out.dtype if v_out is not None else torch.bfloat16
+        K, V = [torch.empty(B, H, tokens, d, dtype=given, device=cache.K.device) if y is None else y for y in (out, v_out)]
+        _require(K.shape[2] == tokens, f"the output has {K.shape[2]} tokens, not {tokens}")
+        c, rows = _cache8_of(cache), _cache8_rows(cache, K, V, at, None)
+        st = lib.mrt_cache8_read(ctypes.byref(c), ctypes.byref(rows), K.data_ptr(), V.data_ptr(), s)
+        if st != MRT_OK:
+            _raise(lib, st)
+        return K, V
+    return _run_on(cache.K, stream, call)
+
+
+# (problem, scratch) of recent calls by their values, like _problems
+_cache8_problems: dict = {}
+
+
+def _cache8_problem(Q, O, cache, c, f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale):
+    key = (Q.shape, Q.stride(), Q.dtype, O.shape, O.stride(), O.dtype, cache.K.shape, cache.K.stride(), cache.V.stride(), cache.K.dtype,
+           f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)
+    found = _cache8_problems.get(key)
+    if found is None:
+        _require(Q.dim() == 4 and O.shape == Q.shape and O.dtype == Q.dtype and Q.stride(3) == 1 and O.stride(3) == 1,
+                 "Q and O are [batch, heads, tokens, head_dim] of one type, head_dim contiguous")
+        B, H, nq, d = Q.shape
+        _require(nq == f_q * h * w, f"Q has {nq} tokens, the grid {f_q * h * w}")
+        prob = make_problem(batch=B, heads=H, head_dim=d, f_q=f_q, f_kv=f_kv, h=h, w=w, q_frame_offset=q_frame_offset,
+                            dtype=_dtype_of(Q, "Q"), scale=scale, q_strides=Q.stride()[:3], o_strides=O.stride()[:3])
+        lib = load_library()
+        nbytes = int(lib.dense_attn_fwd_cache8_workspace_bytes(ctypes.byref(prob), ctypes.byref(c), causal_chunk))
+        if nbytes == 0:
+            st = lib.dense_attn_cache8_check(ctypes.byref(prob), ctypes.byref(c), causal_chunk)
+            if st != MRT_OK:
+                _raise(lib, st)
+        if len(_cache8_problems) >= _MAX_PROBLEMS:
+            _cache8_problems.clear()
+        _cache8_problems[key] = found = prob, nbytes
+    return found
+
+
+def dense_attn_fwd_cache8_workspace_bytes(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0) -> int:
+    """Scratch that dense_attn_fwd_cache8 makes use of with these arguments (0: none)."""
+    return _cache8_problem(Q, Q, cache, _cache8_of(cache), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)[1]
+
+
+def dense_attn_fwd_cache8(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0, kv_len=None, out=None,
+                          lse=None, workspace=None, stream=None):
+    """Dense attention of bf16 queries [batch, heads, tokens, head_dim] over the first f_kv h w tokens of a cache, whose heads
+    divide those of Q: (O, lse), as dense_attn_fwd_save gives them.  kv_len (int32 [batch], on the device): tokens that each
+    sequence has.  The cache's values take part exactly; the probabilities are rounded to bf16.
+
+    Calls of few queries share their keys over several workgroups if they have scratch memory
+    (dense_attn_fwd_cache8_workspace_bytes): `workspace`, or memory of torch's allocator.  Without `workspace` a call under a
+    graph capture, or one whose scratch the allocator refuses, does without and takes longer; results differ by roundings."""
+    lib = load_library()
+    import torch
+    _same_device(Q, cache.K, cache.V, cache.K_scale, cache.V_scale, out, lse, kv_len, workspace)
+    _require_scratch(workspace)
+
+    def call(s):
+        O = torch.empty_like(Q) if out is None else out
+        c = _cache8_of(cache)
+        prob, nbytes = _cache8_problem(Q, O, cache, c, f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)
+        stats = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if lse is None else lse
+        _require_lse(stats, Q)
+        _require(kv_len is None or (kv_len.dtype == torch.int32 and kv_len.shape == Q.shape[:1] and kv_len.is_contiguous()),
+                 f"kv_len: int32 [{Q.shape[0]}], contiguous")
+        scratch = workspace
+        if scratch is None and nbytes and not torch.cuda.is_current_stream_capturing():
+            try:
+                scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
+            except torch.cuda.OutOfMemoryError:       # a call that fits without its scratch still runs
+                pass
+        ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
+        st = lib.dense_attn_fwd_cache8(Q.data_ptr(), ctypes.byref(c), O.data_ptr(), stats.data_ptr(), ctypes.byref(prob),
+                                       None if kv_len is None else kv_len.data_ptr(), causal_chunk, ws, nbytes, s)
+        if st != MRT_OK:
+            _raise(lib, st)
+        return O, stats
+    return _run_on(Q, stream, call)

@@ -15,7 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["mrt_api.cpp", "mrt_static.hip", "mrt_f32.hip", "mrt_f32_bf16io.hip", "mrt_f32_save.hip", "mrt_bf16.hip", "mrt_dense_bf16.hip", "mrt_bwd_f32.hip", "mrt_bwd_bf16.hip",
-           "mrt_bwd_waves_bf16.hip", "mrt_dense_bwd_bf16.hip", "mrt_dense_bwd_f32.hip", "mrt_dense_fwd_f32.hip", "mrt_rotary.hip"]
+           "mrt_bwd_waves_bf16.hip", "mrt_dense_bwd_bf16.hip", "mrt_dense_bwd_f32.hip", "mrt_dense_fwd_f32.hip", "mrt_rotary.hip",
+           "mrt_norm_rotary.hip", "mrt_cache8.hip", "mrt_dense_cache8.hip"]
 OUT = os.path.join(HERE, "libmonarchrt.so")
 
 FLAGS = [

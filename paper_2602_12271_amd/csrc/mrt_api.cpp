@@ -8,8 +8,10 @@
 #include <mutex>
 #include <vector>
 
+#include "mrt_cache8.hpp"
 #include "mrt_dense_train.hpp"
 #include "mrt_internal.hpp"
+#include "mrt_norm_rotary.hpp"
 #include "mrt_rotary.hpp"
 
 namespace mrt {
@@ -1146,6 +1148,237 @@ mrt_status mrt_rotary_fwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n
 mrt_status mrt_rotary_bwd(const mrt_rotary* r, const mrt_rotary_tensor* x, int n, const void* const* dY, void* const* dX,
                       void* hip_stream) {
   return rotary_run(r, x, n, dY, dX, true, hip_stream);
+}
+
+// ---- norms with rotary positions ----------------------------------------------------------
+mrt_status mrt_norm_rotary_check(const mrt_rotary* r, double eps, const mrt_norm_tensor* x, int n, int backward) {
+  if (!r || !x) { set_error("norm description is NULL"); return MRT_ERR_NULL; }
+  if (n < 1 || n > 2) { set_error("a norm call takes one or two tensors, got %d", n); return MRT_ERR_SHAPE; }
+  const mrt_rotary_tensor t[2] = {x[0].t, x[n - 1].t};
+  mrt_status st = mrt_rotary_check(r, t, n);
+  if (st != MRT_OK) return st;
+  if (not_finite(eps) || eps < 1e-30 || eps > 1e30) { set_error("eps must be 1e-30..1e30"); return MRT_ERR_SHAPE; }
+  for (int i = 0; i < n; ++i) {
+    if (x[i].t.heads > 65535) { set_error("tensor %d: more than 65535 heads", i); return MRT_ERR_SHAPE; }
+    if (x[i].weight_dtype != MRT_F32 && x[i].weight_dtype != MRT_BF16) { set_error("tensor %d: unknown weight type", i); return MRT_ERR_SHAPE; }
+    if (x[i].weight_head != 0 && x[i].weight_head < r->head_dim) {
+      set_error("tensor %d: weights of heads must be 0 or at least head_dim elements apart", i);
+      return MRT_ERR_SHAPE;
+    }
+    if (!backward) continue;
+    if (x[i].dx.token < r->head_dim || x[i].dx.head < 1 || x[i].dx.batch < 1) {
+      set_error("tensor %d: token stride of dX must be >= head_dim, head/batch strides >= 1", i);
+      return MRT_ERR_SHAPE;
+    }
+    if (x[i].dweight && !x[i].weight) { set_error("tensor %d: a gradient of weights that are not there", i); return MRT_ERR_SHAPE; }
+  }
+  return MRT_OK;
+}
+
+size_t mrt_norm_rotary_bwd_workspace_bytes(const mrt_rotary* r, const mrt_norm_tensor* x, int n) {
+  if (mrt_norm_rotary_check(r, 1.0, x, n, 1) != MRT_OK) return 0;
+  size_t parts = 0;
+  for (int i = 0; i < n; ++i)
+    if (x[i].dweight) parts += x[i].t.heads > kMostNormParts ? x[i].t.heads : kMostNormParts;
+  return parts * r->head_dim * sizeof(float);
+}
+
+static size_t type_size(mrt_dtype t) { return t == MRT_F32 ? 4 : 2; }
+
+static mrt_status norm_rotary_run(const mrt_rotary* r, double eps, const mrt_norm_tensor* x, int n, const void* const* X,
+                                  const void* const* dY, void* const* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const bool backward = dY != nullptr;
+  mrt_status st = mrt_norm_rotary_check(r, eps, x, n, backward);
+  if (st != MRT_OK) return st;
+  if (!X || !out) { set_error("X and the results must be non-NULL"); return MRT_ERR_NULL; }
+  bool in_place = false;
+  for (int i = 0; i < n; ++i) {
+    const mrt_rotary_tensor& t = x[i].t;
+    if (!X[i] || !out[i] || (backward && !dY[i])) { set_error("tensor %d is NULL", i); return MRT_ERR_NULL; }
+    const size_t xs = type_size(t.x_dtype), ys = type_size(t.y_dtype);
+    if ((uintptr_t)X[i] % xs || (uintptr_t)out[i] % (backward ? xs : ys) || (backward && (uintptr_t)dY[i] % ys) ||
+        (uintptr_t)x[i].weight % type_size(x[i].weight_dtype) || (backward && (uintptr_t)x[i].dweight % 4)) {
+      set_error("tensor %d is not aligned to its elements", i);
+      return MRT_ERR_SHAPE;
+    }
+    if (!backward && X[i] == out[i]) {
+      in_place = true;
+      if (t.x_dtype != t.y_dtype || memcmp(&t.x, &t.y, sizeof(mrt_strides))) {
+        set_error("tensor %d in place: both sides need one type and the same strides", i);
+        return MRT_ERR_SHAPE;
+      }
+    }
+    for (int k = 0; k < n; ++k) {
+      if ((out[i] == X[k] && (backward || k != i)) || (backward && out[i] == dY[k]) || (k != i && out[i] == out[k]) ||
+          out[i] == x[k].weight || (backward && (out[i] == (void*)x[k].dweight || (x[i].dweight && (x[i].dweight == x[k].weight ||
+          (const void*)x[i].dweight == X[k] || (const void*)x[i].dweight == dY[k] || (k != i && x[i].dweight == x[k].dweight)))))) {
+        set_error("tensor %d: an output in the place of an input or of another output", i);
+        return MRT_ERR_SHAPE;
+      }
+    }
+  }
+  if (backward) {
+    const size_t need = mrt_norm_rotary_bwd_workspace_bytes(r, x, n);
+    if (need && (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < need)) {
+      set_error("workspace: %zu bytes, 256-byte aligned, are needed", need);
+      return MRT_ERR_WORKSPACE;
+    }
+  }
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const hipError_t e = timed_launch(
+      s, MRT_KERNEL_ROTARY, [&] { return launch_norm_rotary(*r, (float)eps, x, n, X, dY, out, (float*)workspace, s); }, !in_place);
+  if (e != hipSuccess) return hip_fail(e, "norm launch");
+  return MRT_OK;
+}
+
+mrt_status mrt_norm_rotary_fwd(const mrt_rotary* r, double eps, const mrt_norm_tensor* x, int n, const void* const* X,
+                      void* const* Y, void* hip_stream) {
+  return norm_rotary_run(r, eps, x, n, X, nullptr, Y, nullptr, 0, hip_stream);
+}
+
+mrt_status mrt_norm_rotary_bwd(const mrt_rotary* r, double eps, const mrt_norm_tensor* x, int n, const void* const* X,
+                      const void* const* dY, void* const* dX, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!dY) { set_error("dY must be non-NULL"); return MRT_ERR_NULL; }
+  return norm_rotary_run(r, eps, x, n, X, dY, dX, workspace, workspace_bytes, hip_stream);
+}
+
+// ---- a cache of 8 bits -------------------------------------------------------------------
+// r: null for what does not depend on rows
+mrt_status mrt_cache8_check(const mrt_cache8* c, const mrt_cache8_rows* r) {
+  if (!c) { set_error("cache is NULL"); return MRT_ERR_NULL; }
+  if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) { set_error("a tensor of the cache is NULL"); return MRT_ERR_NULL; }
+  if (c->batch < 1 || c->heads < 1 || (long long)c->batch * c->heads > 65535) {
+    set_error("cache: batch and heads must be >= 1, batch x heads at most 65535");
+    return MRT_ERR_SHAPE;
+  }
+  if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16) { set_error("cache: head_dim must be a multiple of 16, 16..256"); return MRT_ERR_SHAPE; }
+  if (c->capacity < 1 || c->capacity > (1 << 24)) { set_error("cache: capacity must be 1..2^24 tokens"); return MRT_ERR_SHAPE; }
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) { set_error("cache: block must be 16, 32, 64 or 128"); return MRT_ERR_SHAPE; }
+  if (c->format != MRT_CACHE_E4M3 && c->format != MRT_CACHE_INT8) { set_error("cache: unknown format"); return MRT_ERR_SHAPE; }
+  for (const mrt_strides* st : {&c->k, &c->v})
+    if (st->token < c->head_dim || st->head < 1 || st->batch < 1 || st->token % 16 || st->head % 16 || st->batch % 16) {
+      set_error("cache: strides of the codes must be multiples of 16, positive, the token's at least head_dim");
+      return MRT_ERR_SHAPE;
+    }
+  if (c->k_scale_batch < 1 || c->k_scale_head < 1 || c->v_scale_batch < 1 || c->v_scale_head < 1) {
+    set_error("cache: strides of the scales must be >= 1");
+    return MRT_ERR_SHAPE;
+  }
+  if ((uintptr_t)c->k_codes % 16 || (uintptr_t)c->v_codes % 16) { set_error("cache: codes must be 16-byte aligned"); return MRT_ERR_SHAPE; }
+  if (c->k_codes == c->v_codes || c->k_scales == c->v_scales) { set_error("cache: keys and values in one place"); return MRT_ERR_SHAPE; }
+  if (!r) return MRT_OK;
+  if (r->tokens < 1 || r->tokens > (1 << 24)) { set_error("rows: tokens must be 1..2^24"); return MRT_ERR_SHAPE; }
+  if (!r->at_each && (r->at < 0 || (long long)r->at + r->tokens > c->capacity)) {
+    set_error("rows: tokens %d..%lld of a cache of %d", r->at, (long long)r->at + r->tokens - 1, c->capacity);
+    return MRT_ERR_SHAPE;
+  }
+  if (r->dtype != MRT_F32 && r->dtype != MRT_BF16) { set_error("rows: unknown dtype"); return MRT_ERR_SHAPE; }
+  const int step = r->dtype == MRT_F32 ? 4 : 8;
+  for (const mrt_strides* st : {&r->k, &r->v})
+    if (st->token < c->head_dim || st->head < 1 || st->batch < 1 || st->token % step || st->head % step || st->batch % step) {
+      set_error("rows: strides must be multiples of 16 bytes, positive, the token's at least head_dim");
+      return MRT_ERR_SHAPE;
+    }
+  return MRT_OK;
+}
+
+static mrt_status cache8_run(const mrt_cache8* c, const mrt_cache8_rows* r, void* K, void* V, bool reads, void* hip_stream) {
+  if (!r) { set_error("rows are NULL"); return MRT_ERR_NULL; }
+  mrt_status st = mrt_cache8_check(c, r);
+  if (st != MRT_OK) return st;
+  if (!K || !V) { set_error("K and V must be non-NULL"); return MRT_ERR_NULL; }
+  if ((uintptr_t)K % 16 || (uintptr_t)V % 16) { set_error("rows must be 16-byte aligned"); return MRT_ERR_SHAPE; }
+  if (reads && r->tokens_each) { set_error("rows: tokens_each is for writing"); return MRT_ERR_SHAPE; }
+  if (reads && K == V) { set_error("K and V in one place"); return MRT_ERR_SHAPE; }
+  for (const void* x : {c->k_codes, c->v_codes, (void*)c->k_scales, (void*)c->v_scales})
+    if (x == K || x == V) { set_error("rows in the place of the cache"); return MRT_ERR_SHAPE; }
+  int shift = 4;
+  while (1 << shift < c->block) ++shift;
+  Cache8Call call;
+  call.side[0] = {(unsigned char*)c->k_codes, c->k_scales, K, c->k, r->k, c->k_scale_batch, c->k_scale_head};
+  call.side[1] = {(unsigned char*)c->v_codes, c->v_scales, V, c->v, r->v, c->v_scale_batch, c->v_scale_head};
+  call.batch = c->batch; call.heads = c->heads; call.d = c->head_dim; call.capacity = c->capacity; call.shift = shift;
+  call.tokens = r->tokens; call.at = r->at; call.at_each = r->at_each; call.tokens_each = r->tokens_each;
+  const bool e4m3 = c->format == MRT_CACHE_E4M3;
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const hipError_t e = timed_launch(s, MRT_KERNEL_CACHE, [&] {
+    return reads ? launch_cache8_read(call, e4m3, r->dtype, s) : launch_cache8_write(call, e4m3, r->dtype, s);
+  });
+  if (e != hipSuccess) return hip_fail(e, "cache launch");
+  return MRT_OK;
+}
+
+mrt_status mrt_cache8_write(const mrt_cache8* c, const mrt_cache8_rows* r, const void* K, const void* V, void* hip_stream) {
+  return cache8_run(c, r, (void*)K, (void*)V, false, hip_stream);
+}
+
+mrt_status mrt_cache8_read(const mrt_cache8* c, const mrt_cache8_rows* r, void* K, void* V, void* hip_stream) {
+  return cache8_run(c, r, K, V, true, hip_stream);
+}
+
+// p with the strides of the cache's codes for those of K and V
+static mrt_problem cache8_problem(const mrt_problem* p, const mrt_cache8* c) {
+  mrt_problem q = *p;
+  q.k = c->k;
+  q.v = c->v;
+  return q;
+}
+
+mrt_status dense_attn_cache8_check(const mrt_problem* p, const mrt_cache8* c, int causal_chunk) {
+  if (!p) { set_error("problem is NULL"); return MRT_ERR_NULL; }
+  mrt_status st = mrt_cache8_check(c, nullptr);
+  if (st != MRT_OK) return st;
+  const mrt_problem q = cache8_problem(p, c);
+  mrt_dense_train t;
+  memset(&t, 0, sizeof(t));
+  t.kv_heads = c->heads;
+  st = dense_train_check(&q, &t, causal_chunk, false);
+  if (st != MRT_OK) return st;
+  if (p->dtype != MRT_BF16 || p->compute != MRT_COMPUTE_DEFAULT) {
+    set_error("the attention over a cache of 8 bits takes bf16 queries and MRT_COMPUTE_DEFAULT");
+    return MRT_ERR_UNSUPPORTED;
+  }
+  if (c->batch != p->batch || c->head_dim != p->head_dim) { set_error("the cache has another batch or head_dim"); return MRT_ERR_SHAPE; }
+  if ((long long)p->f_kv * p->h * p->w > c->capacity) { set_error("more keys than the cache holds"); return MRT_ERR_SHAPE; }
+  return MRT_OK;
+}
+
+size_t dense_attn_fwd_cache8_workspace_bytes(const mrt_problem* p, const mrt_cache8* c, int causal_chunk) {
+  if (dense_attn_cache8_check(p, c, causal_chunk) != MRT_OK) return 0;
+  const mrt_problem q = cache8_problem(p, c);
+  return dense_cache8_workspace_bytes(dense_params(&q, causal_chunk), p->batch * p->heads, p->heads / c->heads);
+}
+
+mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, float* lse, const mrt_problem* p, const int* kv_len,
+                                 int causal_chunk, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  mrt_status st = dense_attn_cache8_check(p, c, causal_chunk);
+  if (st != MRT_OK) return st;
+  if (!Q || !O || !lse) { set_error("Q, O and lse must be non-NULL"); return MRT_ERR_NULL; }
+  if ((uintptr_t)Q % 16 || (uintptr_t)O % 16) { set_error("bf16 path needs 16-byte aligned tensors"); return MRT_ERR_SHAPE; }
+  for (const void* x : {c->k_codes, c->v_codes, (void*)c->k_scales, (void*)c->v_scales})
+    if (x == O || x == lse) { set_error("an output in the place of the cache"); return MRT_ERR_SHAPE; }
+  if (O == lse || Q == lse) { set_error("lse in the place of Q or O"); return MRT_ERR_SHAPE; }
+  if ((uintptr_t)workspace % 256) { set_error("workspace must be 256-byte aligned"); return MRT_ERR_WORKSPACE; }
+  const mrt_problem q = cache8_problem(p, c);
+  KParams kp = dense_params(&q, causal_chunk);
+  kp.Q = Q; kp.K = c->k_codes; kp.V = c->v_codes; kp.O = O;
+  const hipStream_t s = (hipStream_t)hip_stream;
+  const int BH = p->batch * p->heads;
+  int shift = 4;
+  while (1 << shift < c->block) ++shift;
+  auto run = [&](auto cache) {
+    cache.lse = lse; cache.kv_len = kv_len; cache.group = p->heads / c->heads;
+    cache.k_exp = c->k_scales; cache.v_exp = c->v_scales;
+    cache.ke_batch = c->k_scale_batch; cache.ke_head = c->k_scale_head;
+    cache.ve_batch = c->v_scale_batch; cache.ve_head = c->v_scale_head;
+    cache.shift = shift;
+    return launch_dense_cache8(kp, BH, workspace, workspace_bytes, cache, s);
+  };
+  const hipError_t e = timed_launch(s, MRT_KERNEL_DENSE, [&] {
+    return c->format == MRT_CACHE_E4M3 ? run(DenseCache8<true>()) : run(DenseCache8<false>());
+  });
+  if (e != hipSuccess) return hip_fail(e, "dense launch");
+  return MRT_OK;
 }
 
 #ifdef MRT_TRACE

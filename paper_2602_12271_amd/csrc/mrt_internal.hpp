@@ -127,6 +127,12 @@ struct DenseSave {
   int group;            // heads that share one head of K and V
 };
 struct NoSave {};
+// A forward call over a cache of 8 bits: keys and values are codes (KParams: strides in bytes), e4m3 or whole numbers.
+template <bool E4M3> struct DenseCache8 : DenseSave {
+  const unsigned char *k_exp, *v_exp;             // exponents + 127 of the blocks of a (batch, key head)
+  long long ke_batch, ke_head, ve_batch, ve_head; // their strides
+  int shift;                                      // log2 of the tokens of a block
+};
 
 struct Plan {
   KParams kp;          // everything but the pointers

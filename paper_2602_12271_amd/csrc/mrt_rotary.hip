@@ -6,15 +6,13 @@
 // whose whole part is dropped exactly before the rest goes to 32 bits.  So no position is too far (a 32-bit angle
 // at position 10^6 is off by 0.06 radians), and nothing is read from a table.
 #include "mrt_rotary.hpp"
+#include "mrt_rotary_rows.hpp"
 #include "mrt_bf16_tiles.hpp"
-
-#include <cmath>
 
 namespace mrt {
 
 namespace {
 
-constexpr int kMostPairs = 128;
 constexpr int kThreadsRot = 256;
 
 struct RotaryTensor {
@@ -34,32 +32,6 @@ struct RotaryArgs {
   int split_block;              // first block of the second tensor
   int heads_a_thread, adjacent;
 };
-
-// (runs of eight fp32 numbers are two accesses of 16 bytes)
-template <typename T, int V> struct Run {
-  typedef __attribute__((ext_vector_type(V), aligned(V * sizeof(T) < 16 ? V * sizeof(T) : 16))) T type;
-};
-template <typename T> struct Run<T, 1> { typedef T type; };
-
-template <typename T, int V>
-__device__ inline void load_run(const T* at, float (&x)[V]) {
-  const typename Run<T, V>::type v = *(const typename Run<T, V>::type*)at;
-  if constexpr (V == 1) x[0] = (float)v;
-  else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) x[e] = (float)v[e];
-  }
-}
-template <typename T, int V>
-__device__ inline void store_run(T* at, const float (&x)[V]) {
-  typename Run<T, V>::type v;
-  if constexpr (V == 1) v = (T)x[0];
-  else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = (T)x[e];
-  }
-  *(typename Run<T, V>::type*)at = v;
-}
 
 // V: elements of one access.  HALVES: a thread's accesses are V elements and their V partners; with V = 1 these may
 // be adjacent ones, in rows whose pairs are not aligned.  AHEAD: heads whose loads are in flight at once.
@@ -185,15 +157,7 @@ hipError_t launch_rotary(const mrt_rotary& r, const mrt_rotary_tensor* x, int n,
   a.end0 = r.pairs[0];
   a.end1 = r.pairs[0] + r.pairs[1];
   a.adjacent = r.layout == MRT_ROTARY_ADJACENT;
-  // powers of the ladder's ratio in 64 significant bits: a product a pair instead of a pow
-  const long double turn = (inverse ? -0.5L : 0.5L) / 3.14159265358979323846264338327950288L;
-  for (int axis = 0, p = 0; axis < 3; ++axis) {
-    const int count = r.ladder == MRT_ROTARY_SHARED ? a.pairs : r.pairs[axis];
-    if (r.pairs[axis] == 0) continue;
-    const long double ratio = powl((long double)r.theta, -1.0L / count);
-    long double at = r.ladder == MRT_ROTARY_SHARED ? turn * powl(ratio, p) : turn;
-    for (int i = 0; i < r.pairs[axis]; ++i, at *= ratio) a.turns[p++] = (double)at;
-  }
+  rotary_turns(r, inverse, a.turns);
   // one launch for both tensors if they have the same types and alignment
   const int v0 = run_length(r, x[0], X[0], Y[0], a.pairs), v1 = n > 1 ? run_length(r, x[1], X[1], Y[1], a.pairs) : v0;
   const bool together = n > 1 && x[0].x_dtype == x[1].x_dtype && x[0].y_dtype == x[1].y_dtype && v0 == v1;

@@ -1,0 +1,276 @@
+"""GPU: rows into a cache of 8 bits and out of it, against the definition in 64 bits on the host.  Everything is exact: a
+scale is a power of two, a code the nearest of an exact quotient, a value a bf16 number."""
+import math
+
+import pytest
+import torch
+
+import paper_2602_12271_amd as pkg
+from decoding import LARGEST, HostCache, code_values
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def rows(gen, batch, heads, tokens, dim, dtype, spread=2.0):
+    """Rows whose sizes differ by powers of e: blocks whose scales have to grow and to shrink."""
+    size = torch.exp(spread * torch.randn(batch, heads, tokens, 1, generator=gen))
+    return (torch.randn(batch, heads, tokens, dim, generator=gen) * size).to(dtype)
+
+
+def hosts(cache):
+    B, H, n, d = cache.K.shape
+    format = "e4m3" if cache.K.dtype == torch.float8_e4m3fn else "int8"
+    return [[[HostCache(n, d, cache.block, format) for _ in range(H)] for _ in range(B)] for _ in range(2)]
+
+
+def check(cache, host, ends):
+    """Codes and scales of the first ends[b] tokens of every sequence, and what a read gives of them."""
+    format = "e4m3" if cache.K.dtype == torch.float8_e4m3fn else "int8"
+    table = code_values(format)
+    most = max(max(ends), 1)
+    read = [x.cpu().double() for x in pkg.cache8_read(cache, most, dtype=F32)]
+    read16 = [x.cpu().double() for x in pkg.cache8_read(cache, most)]
+    for i, (codes, scales) in enumerate(((cache.K, cache.K_scale), (cache.V, cache.V_scale))):
+        codes, scales = codes.view(torch.uint8).cpu().long(), scales.cpu().long()
+        for b, end in enumerate(ends):
+            blocks = -(-end // cache.block)
+            for h in range(cache.K.shape[1]):
+                want = host[i][b][h]
+                assert torch.equal(scales[b, h, :blocks], want.bytes[:blocks]), (i, b, h)
+                got, exact = table[codes[b, h, :end]], want.codes[:end]
+                assert torch.equal(got.isnan(), exact.isnan()) and torch.equal(got.nan_to_num(), exact.nan_to_num()), (i, b, h)
+                value = want.values(torch.arange(end))
+                for x in (read[i], read16[i]):
+                    assert torch.equal(x[b, h, :end].nan_to_num(), value.nan_to_num()), (i, b, h)
+                    assert torch.equal(x[b, h, :end].isnan(), value.isnan())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+@pytest.mark.parametrize("dim", [16, 64, 80, 128, 256])
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+def test_appended_runs(format, dim, block, dtype):
+    """Runs of 1 to several hundred rows, one behind the other: most begin inside a block; the last one ends the cache."""
+    gen = torch.Generator().manual_seed(dim + block)
+    runs = [1, 1, 5, block, 2 * block + 3, 1, 300, 17]
+    room = sum(runs)
+    cache = pkg.cache8(2, 2, room, dim, format=format, block=block)
+    host, at = hosts(cache), 0
+    for n in runs:
+        new = [rows(gen, 2, 2, n, dim, dtype) for _ in range(2)]
+        pkg.cache8_write(cache, *[x.cuda() for x in new], at=at)
+        for i in range(2):
+            for b in range(2):
+                for h in range(2):
+                    host[i][b][h].write(new[i][b, h], at)
+        at += n
+        if n != 1:
+            check(cache, host, [at, at])
+    check(cache, host, [at, at])
+
+
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+@pytest.mark.parametrize("seed", range(4))
+def test_sequences_of_their_own(format, seed):
+    """First tokens and numbers of rows on the device: before the cache, behind it, none, more than there are; then over
+    rows that are there (a chunk that is denoised again).  What a sequence has no part in keeps its bytes."""
+    gen = torch.Generator().manual_seed(seed)
+    room, n, block = 300, 70, 32
+    cache = pkg.cache8(6, 3, room, 64, format=format, block=block)
+    host, ends = hosts(cache), [0] * 6
+    full = [rows(gen, 6, 3, 200, 64, BF16) for _ in range(2)]
+    pkg.cache8_write(cache, *[x.cuda() for x in full])
+    for i in range(2):
+        for b in range(6):
+            for h in range(3):
+                host[i][b][h].write(full[i][b, h], 0)
+    ends = [200] * 6
+    check(cache, host, ends)
+    before = [x.view(torch.uint8).clone() for x in cache[:4]]
+    at = [int(x) for x in torch.randint(0, 200, (3,), generator=gen)] + [-40, 260, 150]
+    count = [n, 200, 1, n, n, 0]
+    new = [rows(gen, 6, 3, n, 64, BF16) for _ in range(2)]
+    number = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    pkg.cache8_write(cache, *[x.cuda() for x in new], at=number(at), lengths=number(count))
+    for b in range(6):
+        m = min(max(count[b], 0), n)
+        if m == 0:
+            continue
+        ends[b] = min(at[b] + m, room)
+        for i in range(2):
+            for h in range(3):
+                host[i][b][h].write(new[i][b, h, :m], at[b])
+    check(cache, host, ends)
+    after = [x.view(torch.uint8) for x in cache[:4]]
+    torch.cuda.synchronize()
+    for x, y in zip(before, after):
+        assert torch.equal(x[5], y[5]), "a sequence without rows changed"
+        if x.dim() == 4:
+            for b in range(5):      # codes outside the blocks that are written, and behind the last row
+                first = max(at[b], 0) // block * block
+                assert torch.equal(x[b, :, :first], y[b, :, :first]) and torch.equal(x[b, :, ends[b]:], y[b, :, ends[b]:])
+
+
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_special_rows(format, dtype):
+    """A block each: zeros of both signs, the largest numbers, subnormal ones, infinities, NaN, magnitudes at and beside a
+    scale's limit, ties between codes, every code."""
+    top, tiny = torch.finfo(dtype).max, torch.finfo(dtype).smallest_normal
+    edge = LARGEST[format]
+    table = code_values(format)
+    table = table[torch.isfinite(table) & (table.abs() <= edge)]
+    middles = (table.sort().values[:-1] + table.sort().values[1:]) / 2
+    beside = torch.tensor([edge, -edge, edge * (1 + 2.0 ** -7 if dtype == BF16 else 1 + 2.0 ** -22), 1.0, edge / 2])
+    blocks = [torch.zeros(16), -torch.zeros(16), torch.tensor([top, -top, 1.0]), torch.tensor([tiny, -tiny / 2, tiny / 64]),
+              torch.tensor([math.inf, 1.0, -2.0e38]), torch.tensor([-math.inf, math.nan, 5.0]), torch.tensor([math.nan, 3.0, -0.1]),
+              torch.full((16,), math.nan), beside, beside[:2] * 2.0 ** 60, beside[2:3] * 2.0 ** -100, table, middles, middles * 2.0 ** -30,
+              torch.tensor([2.0 ** 127, 1.0]), torch.tensor([1.76 * 2.0 ** 119, 1.0])]
+    n = 16
+    x = torch.zeros(len(blocks) * n, 16)
+    for i, values in enumerate(blocks):
+        x[i * n:(i + 1) * n].view(-1)[:values.numel()] = values.float()
+    x = x.to(dtype)
+    cache = pkg.cache8(1, 1, x.shape[0], 16, format=format, block=16)
+    host = hosts(cache)
+    pkg.cache8_write(cache, x[None, None].cuda(), x[None, None].flip(-1).contiguous().cuda())
+    host[0][0][0].write(x, 0)
+    host[1][0][0].write(x.flip(-1), 0)
+    check(cache, host, [x.shape[0]])
+
+
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+def test_every_code_is_read(format):
+    cache = pkg.cache8(1, 1, 256, 16, format=format, block=16)
+    codes = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 16)
+    for x in (cache.K, cache.V):
+        x.view(torch.uint8).copy_(codes[None, None])
+    for byte in (3, 100, 127, 180, 246):
+        cache.K_scale.fill_(byte)
+        cache.V_scale.fill_(byte)
+        want = code_values(format)[:, None].repeat(1, 16) * 2.0 ** (byte - 127)
+        for dtype in (BF16, F32):
+            for x in pkg.cache8_read(cache, 256, dtype=dtype):
+                x = x.cpu().double()[0, 0]
+                assert torch.equal(x.isnan(), want.isnan()) and torch.equal(x.nan_to_num(), want.nan_to_num()), (byte, dtype)
+
+
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+def test_growing_scales(format):
+    """Rows that grow one by one by a factor of 1.5: what the first ones of the block are off in the end, against the header's
+    bound: e4m3 codes that stay normal do not move; whole numbers by less than one unit of the final scale."""
+    n, dim = 32, 64
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(n, dim, generator=gen) * 1.5 ** torch.arange(n)[:, None] * (0.05 if format == "e4m3" else 1.0)
+    cache = pkg.cache8(1, 1, n, dim, format=format, block=n)
+    for t in range(n):
+        pkg.cache8_write(cache, x[None, None, t:t + 1].cuda(), x[None, None, t:t + 1].cuda(), at=t)
+    got = pkg.cache8_read(cache, n, dtype=F32)[0].cpu().double()[0, 0]
+    scale = 2.0 ** (int(cache.K_scale[0, 0, 0]) - 127)
+    off = (got - x.double()).abs()
+    if format == "e4m3":
+        assert (off <= (x.abs() * 2.0 ** -4).clamp(min=scale * 2.0 ** -9)).all()     # (subnormal: rounded twice or more, half a step each)
+    else:
+        assert (off < scale).all()
+
+
+def test_read_ranges():
+    gen = torch.Generator().manual_seed(4)
+    cache = pkg.cache8(3, 2, 150, 48, block=16)
+    new = [rows(gen, 3, 2, 150, 48, F32) for _ in range(2)]
+    pkg.cache8_write(cache, *[x.cuda() for x in new])
+    whole = pkg.cache8_read(cache, 150)
+    part = pkg.cache8_read(cache, 33, at=71)
+    at = [-10, 130, 1000]
+    each = pkg.cache8_read(cache, 33, at=torch.tensor(at, dtype=torch.int32, device="cuda"))
+    memory = torch.full((3, 33, 2, 56), 7.0, dtype=BF16, device="cuda")
+    places = [memory.clone() for _ in range(2)]
+    views = [m.transpose(1, 2)[..., :48] for m in places]
+    pkg.cache8_read(cache, 33, at=71, out=views[0], v_out=views[1])
+    torch.cuda.synchronize()
+    for w, p, e, v, m in zip(whole, part, each, views, places):
+        assert torch.equal(p, w[:, :, 71:104]) and torch.equal(v, p) and (m[..., 48:] == 7).all()
+        for b in range(3):
+            for t in range(33):
+                token = at[b] + t
+                want = w[b, :, token] if 0 <= token < 150 else torch.zeros_like(w[b, :, 0])
+                assert torch.equal(e[b, :, t], want)
+
+
+def test_layouts():
+    """Codes with tokens outside of heads, scales inside a larger tensor, rows as a projection leaves them."""
+    gen = torch.Generator().manual_seed(5)
+    new = [rows(gen, 2, 3, 100, 64, BF16) for _ in range(2)]
+    plain = pkg.cache8(2, 3, 130, 64, block=32)
+    pkg.cache8_write(plain, *[x.cuda() for x in new], at=21)
+    codes = [torch.full((2, 130, 3, 80), 9, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    views = [c.view(torch.float8_e4m3fn).transpose(1, 2)[..., :64] for c in codes]
+    bytes_ = torch.full((2, 2, 3, 9), 3, dtype=torch.uint8, device="cuda")
+    cache = pkg.Cache8(*views, bytes_[:, 0, :, 2:7], bytes_[:, 1, :, 2:7], 32)
+    packed = torch.stack([x.transpose(1, 2) for x in new], 2).cuda()                # [batch, tokens, K and V, heads, dim]
+    pkg.cache8_write(cache, packed[:, :, 0].transpose(1, 2), packed[:, :, 1].transpose(1, 2), at=21)
+    torch.cuda.synchronize()
+    for x, y in zip(plain[:2], cache[:2]):
+        assert torch.equal(x.view(torch.uint8)[:, :, 21:121], y.contiguous().view(torch.uint8)[:, :, 21:121])
+    for x, y in zip(plain[2:4], cache[2:4]):
+        assert torch.equal(x[:, :, :4], y[:, :, :4])
+    assert all((c[..., 64:] == 9).all() for c in codes) and (bytes_[..., :2] == 3).all() and (bytes_[..., 7:] == 3).all()
+    assert all((c[:, 121:, :, :64] == 9).all() for c in codes)
+
+
+def test_streams_and_graph():
+    """Written and read on two streams of its own each; captured, with first tokens that move between replays."""
+    gen = torch.Generator().manual_seed(6)
+    caches = [pkg.cache8(2, 2, 200, 64) for _ in range(3)]
+    new = [[rows(gen, 2, 2, 50, 64, BF16).cuda() for _ in range(2)] for _ in range(6)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for s, c in zip(streams, caches):
+        pkg.cache8_write(c, *new[0], at=30, stream=s.cuda_stream)
+        pkg.cache8_write(c, *new[1], at=80, stream=s.cuda_stream)
+        got.append(pkg.cache8_read(c, 100, at=30, stream=s.cuda_stream))
+    pkg.cache8_write(caches[2], *new[0], at=30)
+    pkg.cache8_write(caches[2], *new[1], at=80)
+    want = pkg.cache8_read(caches[2], 100, at=30)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for g in got for x, y in zip(g, want))
+
+    at = torch.tensor([10, 20], dtype=torch.int32, device="cuda")
+    held = [x.clone() for x in new[2]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pkg.cache8_write(caches[0], *held, at=at)
+        out = pkg.cache8_read(caches[0], 50, at=at)
+    for replay in range(4):
+        for x, y in zip(held, new[2 + replay]):
+            x.copy_(y)
+        at.add_(13)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        pkg.cache8_write(caches[1], *held, at=at)
+        want = pkg.cache8_read(caches[1], 50, at=at)
+        torch.cuda.synchronize()
+        # (the first replay writes over what both have alike)
+        assert all(torch.equal(x, y) for x, y in zip(out, want)), replay
+
+
+def test_far_addresses():
+    """Codes of a cache whose tokens lie 2^24 bytes apart, past 2^31 in all."""
+    gen = torch.Generator().manual_seed(7)
+    far, n = 1 << 24, 140
+    memory = torch.empty(n * far, dtype=torch.uint8, device="cuda")
+    assert memory.numel() > 1 << 31
+    near = pkg.cache8(1, 2, n, 64)
+    codes = [memory.as_strided((1, 2, n, 64), (n * far, 64, far, 1), i * 4096).view(torch.int8).view(torch.float8_e4m3fn) for i in range(2)]
+    cache = pkg.Cache8(*codes, near.K_scale.clone(), near.V_scale.clone(), 64)
+    new = [rows(gen, 1, 2, n, 64, BF16).cuda() for _ in range(2)]
+    for c in (near, cache):
+        pkg.cache8_write(c, *[x[:, :, :100] for x in new])
+        pkg.cache8_write(c, *[x[:, :, 100:] for x in new], at=100)
+    want, got = pkg.cache8_read(near, n), pkg.cache8_read(cache, n)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))

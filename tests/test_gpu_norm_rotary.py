@@ -1,0 +1,320 @@
+"""GPU: norms of queries and keys with their rotary positions, forward and backward, against the definition in 64 bits."""
+import itertools
+import math
+
+import pytest
+import torch
+
+import paper_2602_12271_amd as pkg
+from decoding import angles, norm_backward, norm_forward, pair_size, weight_rows
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+# dim, split, tokens as (f, h, w) or n, heads, kv_heads, batch
+SHAPES = {
+    "chunk": (128, None, (3, 5, 7), 12, 12, 1),
+    "one-token": (128, (16, 24, 24), 1, 32, 8, 1),
+    "dim-64": (64, None, (2, 3, 5), 5, 1, 3),
+    "dim-72": (72, (18, 9, 9), 33, 3, 3, 2),
+    "dim-80": (80, (10, 10, 20), 33, 4, 2, 2),
+    "partial": (128, (8, 8, 8), (1, 6, 6), 4, 2, 1),
+    "one-axis": (96, (0, 0, 48), 70, 2, 1, 1),
+    "odd-pairs": (30, (3, 5, 6), 41, 3, 1, 2),
+    "odd-dim": (31, (4, 4, 4), 41, 3, 1, 1),
+    "dim-2": (2, (0, 1, 0), 300, 1, 1, 1),
+    "dim-1-of-3": (3, (1, 0, 0), 5, 2, 2, 1),
+    "dim-255": (255, (40, 44, 43), 9, 2, 1, 1),
+    "dim-256": (256, (40, 44, 44), 19, 2, 2, 1),
+    "dim-250": (250, (41, 42, 42), 19, 2, 2, 1),
+    "many-heads": (64, None, 3, 200, 40, 1),
+    "long": (64, None, 1000, 2, 1, 1),
+}
+TYPES = {"bf16": (BF16, BF16), "f32": (F32, F32), "f32-bf16": (F32, BF16), "bf16-f32": (BF16, F32)}
+EPS = 1e-6
+
+
+def half_step(t):
+    return torch.finfo(t).eps / 2
+
+
+def make(shape, types, weight, seed=3, gradient=False):
+    dim, split, tokens, heads, kv_heads, batch = shape
+    tin, tout = types
+    gen = torch.Generator().manual_seed(seed)
+    n = tokens if isinstance(tokens, int) else math.prod(tokens)
+    split = split or pkg.binding.rotary_pairs_split(dim)
+    sides = []
+    for h in (heads, kv_heads):
+        x = torch.randn(batch, h, n, dim, generator=gen).to(tin)
+        g = torch.randn(batch, h, n, dim, generator=gen).to(tout)
+        w = {"none": None, "f32": (dim,), "bf16": (dim,), "each": (h, dim), "each-bf16": (h, dim)}[weight]
+        if w is not None:
+            w = (1 + 0.3 * torch.randn(w, generator=gen)).to(BF16 if "bf16" in weight else F32)
+        sides.append((x, g, w))
+    if isinstance(tokens, int):
+        where = torch.randint(-50, 1 << 20, (batch, 3, n), generator=gen).to(torch.int32)
+        at, args = (where, where), dict(q_positions=where.cuda(), k_positions=where.cuda())
+    else:
+        f, h, w = tokens
+        grid = [torch.cartesian_prod(o + torch.arange(f), torch.arange(h), torch.arange(w)).reshape(-1, 3).t() for o in (18, 4)]
+        at, args = grid, dict(f_q=f, h=h, w=w, q_frame_offset=18, kv_frame_offset=4)
+    return sides, at, split, args
+
+
+def cuda(x):
+    return None if x is None else x.cuda()
+
+
+def forward_bound(x, w, want_n, split, layout, tout):
+    """An entry is off by half a step of the result's type, and by 32-bit arithmetic: the mean of d squares (d + 2 roundings
+    of a sum of positive numbers, halved by the root), the root, three products (16 in all), the turn (two products and an
+    addition: 4, cos and sin 2 ulp each: 4, angle 1e-7) of the pair's magnitudes."""
+    d = x.shape[-1]
+    size = pair_size(want_n, split, layout)
+    rel = (d / 2 + 1 + 16 + 8) * 2.0 ** -24 + 1e-7
+    return (half_step(tout) * (1 + rel) + rel) * size + 1e-30
+
+
+@pytest.mark.parametrize("layout,ladder", itertools.product(("adjacent", "halves"), ("axis", "shared")))
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward(shape, types, layout, ladder):
+    weight = {"adjacent": {"axis": "f32", "shared": "each"}, "halves": {"axis": "bf16", "shared": "none"}}[layout][ladder]
+    sides, at, split, args = make(SHAPES[shape], TYPES[types], weight)
+    tout = TYPES[types][1]
+    (q, _, qw), (k, _, kw) = sides
+    got = pkg.norm_rotary_fwd(q.cuda(), k.cuda(), cuda(qw), cuda(kw), eps=EPS, theta=1e4, split=split, layout=layout, ladder=ladder,
+                              dtype=tout, **args)
+    torch.cuda.synchronize()
+    for (x, _, w), y, positions in zip(sides, got, at):
+        assert y.dtype == tout and y.shape == x.shape
+        want = norm_forward(x, w, EPS, angles(positions, split, 1e4, ladder), split, layout)
+        n = x.double() * (x.double().square().mean(-1, keepdim=True) + EPS).rsqrt() * weight_rows(w, x.shape[1], x.shape[-1])
+        off = (y.cpu().double() - want).abs() / forward_bound(x, w, n, split, layout, tout)
+        assert off.max() <= 1, f"{off.max():.2f} of the bound"
+
+
+@pytest.mark.parametrize("layout,ladder", itertools.product(("adjacent", "halves"), ("axis", "shared")))
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_backward(shape, types, layout, ladder):
+    """dx = r (a - n mean(a n)), a = g w: with e the relative error of 32-bit factors, (d/2 + 1 + 16 + 8) 2^-24 + 1e-7 as in the
+    forward pass of g, n and r, an entry is off by 3 e of each of its two terms (with magnitudes of pairs in the place of g),
+    and the mean by (d + 4) 2^-24 of the sum of its magnitudes more.  dw: a sum of M products of a g and an n, 2 e each and
+    M 2^-24 of the sum of magnitudes."""
+    weight = {"adjacent": {"axis": "each", "shared": "f32"}, "halves": {"axis": "none", "shared": "each-bf16"}}[layout][ladder]
+    sides, at, split, args = make(SHAPES[shape], TYPES[types], weight, seed=4)
+    tin = TYPES[types][0]
+    (q, dq, qw), (k, dk, kw) = sides
+    got = pkg.norm_rotary_bwd(q.cuda(), k.cuda(), cuda(qw), cuda(kw), dq.cuda(), dk.cuda(), eps=EPS, theta=1e4, split=split,
+                              layout=layout, ladder=ladder, **args)
+    torch.cuda.synchronize()
+    for i, ((x, g, w), positions) in enumerate(zip(sides, at)):
+        d = x.shape[-1]
+        angle = angles(positions, split, 1e4, ladder)
+        dx, dw = norm_backward(x, w, EPS, angle, split, layout, g)
+        assert got[i].dtype == tin and got[i].shape == x.shape
+        e = (d / 2 + 1 + 16 + 8) * 2.0 ** -24 + 1e-7
+        r = (x.double().square().mean(-1, keepdim=True) + EPS).rsqrt()
+        n, size = (x.double() * r).abs(), pair_size(g.double(), split, layout)
+        a = size * weight_rows(w, x.shape[1], d).abs()
+        tol = r * (3 * e * (a + n * (a * n).mean(-1, keepdim=True)) + (d + 4) * 2.0 ** -24 * n * (a * n).mean(-1, keepdim=True))
+        tol = tol + half_step(tin) * (dx.abs() + tol) + 1e-30
+        off = (got[i].cpu().double() - dx).abs() / tol
+        assert off.max() <= 1, f"{off.max():.2f} of the bound"
+        if w is None:
+            assert got[2 + i] is None
+            continue
+        y = got[2 + i].cpu()
+        assert y.dtype == F32 and y.shape == w.shape
+        axes = (0, 2) if w.dim() == 2 else (0, 1, 2)
+        rows = x.numel() // d // (x.shape[1] if w.dim() == 2 else 1)
+        off = (y.double() - dw).abs() / ((2 * e + rows * 2.0 ** -24) * (size * n).sum(axes) + 1e-30)
+        assert off.max() <= 1, f"weights: {off.max():.2f} of the bound"
+
+
+@pytest.mark.parametrize("shape", ["chunk", "dim-72", "odd-dim"])
+@pytest.mark.parametrize("weight", ["f32", "each"])
+def test_gradient_against_differences(shape, weight):
+    """sum(dy y) of the forward kernel along a direction, central differences of width 2 h in the norm's input and in the
+    weights.  The definition in 64 bits has the same quotient; the kernel's is off from it by what its results are off,
+    over h.  And that quotient is the gradients' product with the direction, up to h^2: both parts are small against it."""
+    sides, at, split, args = make(SHAPES[shape], (F32, F32), weight, seed=5)
+    (q, dq, qw), _ = sides
+    angle, h = angles(at[0], split, 1e4, "axis"), 2.0 ** -7
+    args = {n: v for n, v in args.items() if not n.startswith("k")}
+    vq, vw = [(v / v.square().mean().sqrt()).float() for v in norm_backward(q, qw, EPS, angle, split, "adjacent", dq)]   # (steep)
+    grads = pkg.norm_rotary_bwd(q.cuda(), None, qw.cuda(), None, dq.cuda(), eps=EPS, split=split, **args)
+    along = (grads[0].cpu().double() * vq).sum() + (grads[2].cpu().double() * vw).sum()
+    quotient = exact = noise = 0.0
+    for sign in (1, -1):
+        x, w = q + sign * h * vq, qw + sign * h * vw
+        y = pkg.norm_rotary_fwd(x.cuda(), None, w.cuda(), eps=EPS, split=split, **args).cpu().double()
+        want = norm_forward(x, w, EPS, angle, split, "adjacent")
+        n = x.double() * (x.double().square().mean(-1, keepdim=True) + EPS).rsqrt() * weight_rows(w, x.shape[1], x.shape[-1])
+        noise += (forward_bound(x, w, n, split, "adjacent", F32) * dq.abs()).sum()
+        quotient += sign * (dq.double() * y).sum() / (2 * h)
+        exact += sign * (dq.double() * want).sum() / (2 * h)
+    noise = noise / (2 * h)
+    assert abs(quotient - exact) <= noise
+    # the third derivative of a norm along a direction of unit entries: at most 15 of |dy| |w| / rms^3 an entry
+    bend = h * h / 6 * 15 * (dq.abs() * weight_rows(qw, q.shape[1], q.shape[-1]).abs()).sum() * 8
+    assert abs(exact - along) <= bend + noise
+    assert abs(along) > 4 * (abs(exact - along) + noise), "the direction says nothing"
+
+
+STRIDED = {"tokens-outside": (0, 2, 1, 3), "batch-inside": (2, 0, 1, 3)}
+
+
+@pytest.mark.parametrize("order", STRIDED)
+@pytest.mark.parametrize("pad", [0, 8, 1])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_strides(order, pad, dtype):
+    """Other orders, rows with gaps that hold NaN and stay as they are, rows that 16 bytes do not divide."""
+    sides, at, split, args = make((64, (12, 10, 10), 37, 6, 2, 2), (dtype, dtype), "f32", seed=7)
+    perm = STRIDED[order]
+
+    def spread(x, fill):
+        y = torch.full([x.shape[p] for p in perm[:3]] + [x.shape[3] + pad], fill, dtype=x.dtype, device="cuda")
+        view = y[..., :x.shape[3]].permute(*[perm.index(i) for i in range(4)])
+        view.copy_(x)
+        return view, y
+    (q, dq, qw), (k, dk, kw) = sides
+    want = pkg.norm_rotary_fwd(q.cuda(), k.cuda(), qw.cuda(), kw.cuda(), split=split, **args)
+    back = pkg.norm_rotary_bwd(q.cuda(), k.cuda(), qw.cuda(), kw.cuda(), dq.cuda(), dk.cuda(), split=split, **args)
+    sq, sk, sdq, sdk = (spread(x, math.nan)[0] for x in (q, k, dq, dk))
+    (oq, mq), (ok, mk) = (spread(torch.zeros_like(x), 7.0) for x in (q, k))
+    pkg.norm_rotary_fwd(sq, sk, qw.cuda(), kw.cuda(), split=split, out=oq, k_out=ok, **args)
+    torch.cuda.synchronize()
+    step = half_step(dtype)
+    # (a sum over a row's lanes goes by how wide the accesses are.  Each of the two is within the forward bound of the exact
+    # result, whose magnitude is that of the PAIR: y0 = n0 cos - n1 sin may cancel, the errors of n0 and n1 do not)
+    for x, y, memory, (given, _, w) in ((want[0], oq, mq, sides[0]), (want[1], ok, mk, sides[1])):
+        n = given.double() * (given.double().square().mean(-1, keepdim=True) + EPS).rsqrt() * weight_rows(w, given.shape[1], 64)
+        assert bool(((x - y).abs().double().cpu() <= 2 * forward_bound(given, w, n, split, "adjacent", dtype)).all())
+        assert pad == 0 or (memory[..., 64:] == 7.0).all()
+    got = pkg.norm_rotary_bwd(sq, sk, qw.cuda(), kw.cuda(), sdq, sdk, split=split, out=oq, k_out=ok, **args)
+    torch.cuda.synchronize()
+    for x, y in zip(back, got):
+        assert float((x - y).double().norm() / x.double().norm()) <= 2 * (step + 200 * 2.0 ** -24)
+    assert pad == 0 or ((mq[..., 64:] == 7.0).all() and (mk[..., 64:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_in_place_into_a_cache_and_zero_rows(dtype):
+    sides, at, split, args = make((128, None, (2, 3, 5), 4, 2, 1), (dtype, dtype), "bf16", seed=8)
+    (q, dq, qw), (k, dk, kw) = sides
+    q, k = q.cuda(), k.cuda()
+    q[:, 1, 3] = 0
+    want = pkg.norm_rotary_fwd(q, k, qw.cuda(), kw.cuda(), **args)
+    cache = torch.full((1, 2, 90, 128), 5.0, dtype=dtype, device="cuda")
+    place, x = cache[:, :, 30:60], q.clone()
+    pkg.norm_rotary_fwd(x, k, qw.cuda(), kw.cuda(), out=x, k_out=place, **args)
+    torch.cuda.synchronize()
+    assert torch.equal(x, want[0]) and torch.equal(place, want[1])
+    assert (cache[:, :, :30] == 5).all() and (cache[:, :, 60:] == 5).all()
+    assert (want[0][:, 1, 3] == 0).all()
+    # a row of zeros: n = 0, dx = a / sqrt(eps)
+    dx = pkg.norm_rotary_bwd(q, None, None, None, dq.cuda(), eps=2.0 ** -20, f_q=2, h=3, w=5)[0]
+    back = pkg.rotary_bwd(dq.cuda().float(), f_q=2, h=3, w=5)
+    torch.cuda.synchronize()
+    size = back[:, 1, 3].abs().max()
+    assert (dx[:, 1, 3].float() - 1024 * back[:, 1, 3]).abs().max() <= 1024 * size * (half_step(dtype) + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("weight", ["none", "f32", "each"])
+def test_one_tensor_and_two(weight):
+    """One tensor a call, or both: the same bits; and the same in a second call."""
+    sides, at, split, args = make((128, None, (3, 7, 9), 8, 2, 2), (BF16, BF16), weight, seed=9)
+    (q, dq, qw), (k, dk, kw) = [[cuda(t) for t in s] for s in sides]
+    both = pkg.norm_rotary_fwd(q, k, qw, kw, **args)
+    only = {n: v for n, v in args.items() if n != "kv_frame_offset"}
+    one = pkg.norm_rotary_fwd(q, None, qw, **only)
+    grads = [pkg.norm_rotary_bwd(q, k, qw, kw, dq, dk, **args) for _ in range(2)]
+    alone = pkg.norm_rotary_bwd(q, None, qw, None, dq, **only)
+    torch.cuda.synchronize()
+    assert torch.equal(both[0], one) and torch.equal(grads[0][0], alone[0]) and alone[1] is None and alone[3] is None
+    for x, y in zip(*grads):
+        assert x is None and y is None or torch.equal(x, y)
+
+
+@pytest.mark.parametrize("heads,tokens,batch", [(3, 5000, 1), (1200, 3, 2), (1, 1, 1), (2, 70, 40)])
+@pytest.mark.parametrize("each", [False, True])
+def test_many_rows_of_ones(heads, tokens, batch, each):
+    """Rows of ones, no turn: n = 1 up to eps, so that the weights' gradients count rows; a row lost or met twice shows."""
+    x = torch.ones(batch, heads, tokens, 64, device="cuda", dtype=BF16)
+    w = torch.ones((heads, 64) if each else (64,), device="cuda")
+    where = torch.zeros(3, tokens, dtype=torch.int32, device="cuda")
+    dw = pkg.norm_rotary_bwd(x, None, w, None, x, eps=1e-30, q_positions=where)[2]
+    torch.cuda.synchronize()
+    rows = batch * tokens * (1 if each else heads)
+    assert (dw - rows).abs().max() <= rows * 2.0 ** -18       # (of the 2^-20 that the root and the products leave of 1)
+
+
+def test_streams_and_scratch():
+    sides, at, split, args = make((128, None, (3, 11, 13), 8, 4, 1), (BF16, BF16), "f32", seed=10)
+    (q, dq, qw), (k, dk, kw) = [[cuda(t) for t in s] for s in sides]
+    want = (*pkg.norm_rotary_fwd(q, k, qw, kw, **args), *pkg.norm_rotary_bwd(q, k, qw, kw, dq, dk, **args))
+    torch.cuda.synchronize()
+    poisoned = torch.full((1 << 21,), 255, dtype=torch.uint8, device="cuda")
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        got = []
+        for s in streams:
+            got.append((*pkg.norm_rotary_fwd(q, k, qw, kw, stream=s.cuda_stream, **args),
+                        *pkg.norm_rotary_bwd(q, k, qw, kw, dq, dk, stream=s.cuda_stream, **args)))
+        torch.cuda.synchronize()
+        got.append((*want[:2], *pkg.norm_rotary_bwd(q, k, qw, kw, dq, dk, workspace=poisoned, **args)))
+        torch.cuda.synchronize()
+        for g in got:
+            assert all(torch.equal(x, y) for x, y in zip(g, want))
+
+
+def test_captured():
+    """Forward and backward in a captured graph: every replay as the eager calls, on the inputs it finds."""
+    shape = (128, None, (2, 9, 11), 6, 2, 1)
+    sides, at, split, args = make(shape, (BF16, BF16), "f32", seed=11)
+    state = [[cuda(t) for t in s] for s in sides]
+
+    def step(sides):
+        (q, dq, qw), (k, dk, kw) = sides
+        return (*pkg.norm_rotary_fwd(q, k, qw, kw, **args), *pkg.norm_rotary_bwd(q, k, qw, kw, dq, dk, **args))
+    step(state)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(state)
+    for replay in range(4):
+        fresh = [[cuda(t) for t in s] for s in make(shape, (BF16, BF16), "f32", seed=20 + replay)[0]]
+        for s, f in zip(state, fresh):
+            for x, y in zip(s, f):
+                x.copy_(y)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(fresh)
+        torch.cuda.synchronize()
+        for n, (x, y) in enumerate(zip(out, want)):
+            assert torch.equal(x, y), f"replay {replay}, output {n}"
+
+
+def test_far_addresses():
+    """Rows 2^24 elements apart: tensors that reach past 2^31 elements."""
+    far, n = 1 << 24, 70
+    sides, at, split, args = make((64, None, (1, 7, 10), 3, 3, 2), (BF16, BF16), "f32", seed=12)
+    (q, dq, qw), (k, dk, kw) = [[cuda(t) for t in s] for s in sides]
+    want = (*pkg.norm_rotary_fwd(q, k, qw, kw, **args), *pkg.norm_rotary_bwd(q, k, qw, kw, dq, dk, **args))
+    memory = torch.empty(2 * n * far, dtype=BF16, device="cuda")
+    assert memory.numel() > 1 << 31
+    slots = [memory.as_strided((2, 3, n, 64), (n * far, 64, far, 1), i * (far // 8)) for i in range(6)]
+    for x, y in zip(slots, (q, k, dq, dk)):
+        x.copy_(y)
+    fq, fk, fdq, fdk = slots[:4]
+    both = pkg.norm_rotary_fwd(fq, fk, qw, kw, out=slots[4], k_out=slots[5], **args)
+    torch.cuda.synchronize()
+    assert torch.equal(both[0], want[0]) and torch.equal(both[1], want[1])
+    got = pkg.norm_rotary_bwd(fq, fk, qw, kw, fdq, fdk, out=slots[4], k_out=slots[5], **args)
+    torch.cuda.synchronize()
+    for x, y in zip(got, want[2:]):
+        assert torch.equal(x, y)
