@@ -1316,11 +1316,12 @@ mrt_status mrt_cache8_read(const mrt_cache8* c, const mrt_cache8_rows* r, void* 
   return cache8_run(c, r, K, V, true, hip_stream);
 }
 
-// p with the strides of the cache's codes for those of K and V
+// p with the strides of the cache's codes for those of K and V (a token by itself has whatever stride)
 static mrt_problem cache8_problem(const mrt_problem* p, const mrt_cache8* c) {
   mrt_problem q = *p;
   q.k = c->k;
   q.v = c->v;
+  if (c->capacity == 1) q.k.token = q.v.token = c->head_dim;
   return q;
 }
 
@@ -1339,7 +1340,13 @@ mrt_status dense_attn_cache8_check(const mrt_problem* p, const mrt_cache8* c, in
     return MRT_ERR_UNSUPPORTED;
   }
   if (c->batch != p->batch || c->head_dim != p->head_dim) { set_error("the cache has another batch or head_dim"); return MRT_ERR_SHAPE; }
-  if ((long long)p->f_kv * p->h * p->w > c->capacity) { set_error("more keys than the cache holds"); return MRT_ERR_SHAPE; }
+  const long long nkv = (long long)p->f_kv * p->h * p->w;
+  if (nkv > c->capacity) { set_error("more keys than the cache holds"); return MRT_ERR_SHAPE; }
+  // (the kernels reach up to 64 tokens beyond the last one, where bounds of 32 bits turn loads into zeros)
+  if ((nkv + 64) * (q.k.token > q.v.token ? q.k.token : q.v.token) > 0xffffffffll) {
+    set_error("(tokens + 64) x token stride of a cache must stay below 2^32 bytes");
+    return MRT_ERR_UNSUPPORTED;
+  }
   return MRT_OK;
 }
 
