@@ -36,7 +36,7 @@ struct NormTensor {
 };
 struct NormArgs {
   NormTensor t[2];
-  double turns[kMostPairs];
+  double quarters[kMostPairs];  // quarter turns of a pair, per position; negative for the inverse
   int end0, end1, pairs;
   int items, turned, d;
   int lanes;                    // of a row
@@ -44,20 +44,54 @@ struct NormArgs {
   float eps, inv_d;
 };
 
-__device__ inline float group_sum(float x, int lanes) {
-  if (lanes > 1) x += dpp_mov<0xB1>(x);
-  if (lanes > 2) x += dpp_mov<0x4E>(x);
-  if (lanes > 4) x += dpp_mov<0x141>(x);
-  if (lanes > 8) x += dpp_mov<0x140>(x);
-  if (lanes > 16) x += __shfl_xor(x, 16);
-  if (lanes > 32) x += __shfl_xor(x, 32);
-  return x;
+// Cosine and sine of an angle in quarter turns: the nearest quarter is taken off in 64 bits, which leaves half a quarter at
+// most for the Taylor series (the first terms left out are 2e-9 and 2e-9), and exchanges or negates them.  (Against
+// sincospif, which has to take any argument, gradients of 12 heads of 4680 tokens with a weight for every head 32.0 -> 30.9 us.)
+__device__ inline void cos_sin(double quarters, float& cs, float& sn) {
+  const double whole = rint(quarters);
+  const float x = (float)(quarters - whole), y = x * x;
+  const int q = (int)whole;
+  const float s = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.604411848e-04f, -4.681754135e-03f), 7.969262625e-02f), -6.459640975e-01f), 1.570796327e+00f);
+  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -2.520204237e-05f, 9.192602748e-04f), -2.086348076e-02f), 2.536695079e-01f), -1.233700550e+00f), 1.0f);
+  const float a = q & 1 ? c : s, b = q & 1 ? s : c;
+  sn = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, a) ^ ((unsigned)(q & 2) << 30));
+  cs = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, b) ^ ((unsigned)((q + 1) & 2) << 30));
 }
 
-// V, HALVES: elements of an access, as in k_rotary.  ITEMS: of a lane.
-template <typename TX, typename TY, int V, bool HALVES, int ITEMS, bool BWD>
+// The sums of the rows of a batch over their groups of lanes.
+template <int N>
+__device__ inline void group_sums(float (&x)[N], int lanes) {
+  auto each = [&](auto step) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] += step(x[k]);
+  };
+  if (lanes > 1) each([](float y) { return dpp_mov<0xB1>(y); });
+  if (lanes > 2) each([](float y) { return dpp_mov<0x4E>(y); });
+  if (lanes > 4) each([](float y) { return dpp_mov<0x141>(y); });
+  if (lanes > 8) each([](float y) { return dpp_mov<0x140>(y); });
+  if (lanes > 16) each([](float y) { return __shfl_xor(y, 16); });
+  if (lanes > 32) each([](float y) { return __shfl_xor(y, 32); });
+}
+
+// The accesses of an item, and its numbers: apart, so that all loads of a batch are under way before the first is waited for.
+template <typename T, int V, bool HALVES>
+struct Raw {
+  typename Run<T, V>::type v[HALVES ? 2 : 1];
+  __device__ inline void load(const T* at, int f0, int f1) {
+    v[0] = *(const typename Run<T, V>::type*)(at + f0);
+    if constexpr (HALVES) v[1] = *(const typename Run<T, V>::type*)(at + f1);
+  }
+  __device__ inline float operator[](int e) const {
+    if constexpr (V == 1) return (float)v[e];
+    else return (float)v[e / V][e % V];
+  }
+};
+
+// V, HALVES: elements of an access, as in k_rotary.  ITEMS: of a lane.  AHEAD: heads of a batch, of which one is loaded while
+// another is formed (forward two: three and four measured up to 5 % behind; backward two, or one where a lane has one head).
+template <typename TX, typename TY, int V, bool HALVES, int ITEMS, bool BWD, int AHEAD>
 __global__ __launch_bounds__(kThreadsNorm) void k_norm_rotary(const NormArgs a) {
-  constexpr int NP = HALVES ? V : V / 2, N = HALVES ? 2 * V : V, AHEAD = BWD ? 2 : 4;
+  constexpr int NP = HALVES ? V : V / 2, N = HALVES ? 2 * V : V;
   typedef typename std::conditional<BWD, TX, TY>::type TO;
   const bool second = (int)blockIdx.x >= a.split_block;
   const NormTensor& t = a.t[second];
@@ -71,16 +105,16 @@ __global__ __launch_bounds__(kThreadsNorm) void k_norm_rotary(const NormArgs a) 
   int f0[ITEMS], f1[ITEMS];
   float w[ITEMS][N], dw[ITEMS][N];
   auto weights = [&](int h) {
+    if (!t.weight) return;
+    const long long row = h * t.weight_head;
+    auto read = [&](auto* at) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
+      for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        w[i][e] = 1.f;
-        if (t.weight && there[i] && (e < V || turns[i])) {
-          const long long at = h * t.weight_head + (e < V ? f0[i] + e : f1[i] + e - V);
-          w[i][e] = t.weight_f32 ? ((const float*)t.weight)[at] : (float)((const __bf16*)t.weight)[at];
-        }
-      }
+        for (int e = 0; e < N; ++e) w[i][e] = (float)at[row + (e < V ? f0[i] + e : f1[i] + e - V)];
+    };
+    if (t.weight_f32) read((const float*)t.weight);
+    else read((const __bf16*)t.weight);
   };
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
@@ -88,13 +122,42 @@ __global__ __launch_bounds__(kThreadsNorm) void k_norm_rotary(const NormArgs a) 
     there[i] = item < a.items;
     turns[i] = item < a.turned;
     f0[i] = !turns[i] ? 2 * a.pairs + V * (item - a.turned) : next ? 2 * item : V * item;
-    f1[i] = next ? f0[i] + 1 : f0[i] + a.pairs;
+    f1[i] = !turns[i] ? f0[i] : next ? f0[i] + 1 : f0[i] + a.pairs;
+    if (!there[i]) f0[i] = f1[i] = 0;                // (loads are not conditional, what they bring there is dropped)
 #pragma unroll
-    for (int e = 0; e < N; ++e) dw[i][e] = 0.f;
+    for (int e = 0; e < N; ++e) { w[i][e] = 1.f; dw[i][e] = 0.f; }
   }
-  if (t.weight_head == 0) weights(0);
+  const bool whole = a.items == a.lanes * ITEMS && a.turned == a.items;
+  // (what does not depend on rows is loaded behind the first row, not before it)
+  double quarters[ITEMS][NP];
+  bool begun = false;
   for (long long row_l = (long long)block * rows_a_block + local; row_l < t.rows; row_l += (long long)t.blocks * rows_a_block) {
     const int row = (int)row_l, b = row / t.tokens, token = row - b * t.tokens;
+    const TX* x = (const TX*)t.x + b * t.xs.batch + token * t.xs.token;
+    const TY* dy = (const TY*)t.dy + b * t.dys.batch + token * t.dys.token;
+    TO* out = (TO*)t.out + b * t.os.batch + token * t.os.token;
+    Raw<TX, V, HALVES> rx[AHEAD][ITEMS];
+    Raw<TY, V, HALVES> ry[BWD ? AHEAD : 1][ITEMS];
+    auto fetch = [&](int h) {
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int hk = h + k < h1 ? h + k : h;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          rx[k][i].load(x + hk * t.xs.head, f0[i], f1[i]);
+          if constexpr (BWD) ry[k][i].load(dy + hk * t.dys.head, f0[i], f1[i]);
+        }
+      }
+    };
+    fetch(h0);
+    if (!begun) {
+      if (t.weight_head == 0) weights(0);
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+        for (int e = 0; e < NP; ++e) quarters[i][e] = turns[i] ? a.quarters[(HALVES ? V * (lane + i * a.lanes) : f0[i] / 2) + e] : 0.0;
+      begun = true;
+    }
     int pos[3];
     if (t.positions) {
       const int* at = t.positions + b * t.pos_batch + token;
@@ -112,32 +175,9 @@ __global__ __launch_bounds__(kThreadsNorm) void k_norm_rotary(const NormArgs a) 
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
       for (int e = 0; e < NP; ++e) {
-        cs[i][e] = 1.f;
-        sn[i][e] = 0.f;
-        if (turns[i]) {
-          const int p = (HALVES ? V * (lane + i * a.lanes) : f0[i] / 2) + e, at = p < a.end0 ? pos[0] : p < a.end1 ? pos[1] : pos[2];
-          const double turn = at * a.turns[p];
-          sincospif(2.0f * (float)(turn - rint(turn)), &sn[i][e], &cs[i][e]);
-        }
+        const int p = (HALVES ? V * (lane + i * a.lanes) : f0[i] / 2) + e, at = p < a.end0 ? pos[0] : p < a.end1 ? pos[1] : pos[2];
+        cos_sin(at * quarters[i][e], cs[i][e], sn[i][e]);          // (copied features: 0 turns)
       }
-    const TX* x = (const TX*)t.x + b * t.xs.batch + token * t.xs.token;
-    const TY* dy = (const TY*)t.dy + b * t.dys.batch + token * t.dys.token;
-    TO* out = (TO*)t.out + b * t.os.batch + token * t.os.token;
-    auto load = [&](auto* at, int i, float (&v)[N]) {
-      float u[V];
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = 0.f;
-      if (!there[i]) return;
-      load_run(at + f0[i], u);
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = u[e];
-      if constexpr (HALVES)
-        if (turns[i]) {
-          load_run(at + f1[i], u);
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[V + e] = u[e];
-        }
-    };
     auto store = [&](TO* at, int i, const float (&v)[N]) {
       if (!there[i]) return;
       float u[V];
@@ -161,53 +201,75 @@ __global__ __launch_bounds__(kThreadsNorm) void k_norm_rotary(const NormArgs a) 
       }
     };
     for (int h = h0; h < h1; h += AHEAD) {
-      float v[AHEAD][ITEMS][N], g[BWD ? AHEAD : 1][ITEMS][N];
+      // the next batch is under way while this one is formed
+      Raw<TX, V, HALVES> was[AHEAD][ITEMS];
+      Raw<TY, V, HALVES> gave[BWD ? AHEAD : 1][ITEMS];
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const int hk = h + k < h1 ? h + k : h;
+      for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-          load(x + hk * t.xs.head, i, v[k][i]);
-          if constexpr (BWD) load(dy + hk * t.dys.head, i, g[k][i]);
+          was[k][i] = rx[k][i];
+          if constexpr (BWD) gave[k][i] = ry[k][i];
         }
-      }
+      if (h + AHEAD < h1) fetch(h + AHEAD);
+      auto number = [&](const auto& raw, int i, int e) { return whole || (e < V ? there[i] : turns[i]) ? raw[e] : 0.f; };
+      float r[AHEAD];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
-        if (h + k >= h1) break;
-        if (t.weight_head != 0) weights(h + k);
-        float sum = 0.f;
+        r[k] = 0.f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-          for (int e = 0; e < N; ++e) sum = fmaf(v[k][i][e], v[k][i][e], sum);
-        const float r = rsqrtf(fmaf(group_sum(sum, a.lanes), a.inv_d, a.eps));
-        if constexpr (!BWD) {
+          for (int e = 0; e < N; ++e) r[k] = fmaf(number(was[k][i], i, e), number(was[k][i], i, e), r[k]);
+      }
+      group_sums(r, a.lanes);
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) r[k] = rsqrtf(fmaf(r[k], a.inv_d, a.eps));
+      if constexpr (!BWD) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          if (h + k >= h1) break;
+          if (t.weight_head != 0) weights(h + k);
 #pragma unroll
           for (int i = 0; i < ITEMS; ++i) {
+            float v[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[k][i][e] *= r * w[i][e];
-            turn(i, v[k][i]);
-            store(out + (h + k) * t.os.head, i, v[k][i]);
+            for (int e = 0; e < N; ++e) v[e] = number(was[k][i], i, e) * (r[k] * w[i][e]);
+            turn(i, v);
+            store(out + (h + k) * t.os.head, i, v);
           }
-        } else {
-          float along = 0.f;
+        }
+      } else {
+        float g[AHEAD][ITEMS][N], along[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          along[k] = 0.f;
+          if (t.weight_head != 0) weights(h + k < h1 ? h + k : h);
 #pragma unroll
           for (int i = 0; i < ITEMS; ++i) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[k][i][e] = number(gave[k][i], i, e);
             turn(i, g[k][i]);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-              v[k][i][e] *= r;
-              dw[i][e] = fmaf(g[k][i][e], v[k][i][e], dw[i][e]);
+              const float n = number(was[k][i], i, e) * r[k];
+              if (k == 0 || h + k < h1) dw[i][e] = fmaf(g[k][i][e], n, dw[i][e]);
               g[k][i][e] *= w[i][e];
-              along = fmaf(g[k][i][e], v[k][i][e], along);
+              along[k] = fmaf(g[k][i][e], n, along[k]);
             }
           }
-          along = group_sum(along, a.lanes) * a.inv_d;
+        }
+        group_sums(along, a.lanes);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          if (h + k >= h1) break;
+          const float by = along[k] * a.inv_d;
 #pragma unroll
           for (int i = 0; i < ITEMS; ++i) {
+            float v[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[k][i][e] = r * fmaf(-along, v[k][i][e], g[k][i][e]);
-            store(out + (h + k) * t.os.head, i, v[k][i]);
+            for (int e = 0; e < N; ++e) v[e] = r[k] * fmaf(-by, number(was[k][i], i, e) * r[k], g[k][i][e]);
+            store(out + (h + k) * t.os.head, i, v);
           }
         }
       }
@@ -269,7 +331,9 @@ int run_length(const mrt_rotary& r, const mrt_norm_tensor& x, const void* X, con
   const size_t xb = t.x_dtype == MRT_F32 ? 4 : 2, yb = t.y_dtype == MRT_F32 ? 4 : 2;
   const struct { const void* at; const mrt_strides* st; size_t size; } all[3] = {
       {X, &t.x, xb}, {backward ? dY : out, &t.y, yb}, {out, backward ? &x.dx : &t.y, backward ? xb : yb}};
-  for (int v = 8; v > 1; v /= 2) {
+  // (8 elements of both halves, or 8 of 32 bits on both sides, hold more registers than their wider accesses gain: 12 heads of
+  // 4680 tokens in halves forward 16.0 -> 13.4 us, backward 37.0 -> 23.6; 9 frames of 1560 in fp32 73 -> 68.)
+  for (int v = r.layout == MRT_ROTARY_HALVES || (xb == 4 && yb == 4) ? 4 : 8; v > 1; v /= 2) {
     bool ok = r.head_dim % v == 0 && (r.layout == MRT_ROTARY_ADJACENT ? 2 * pairs : pairs) % v == 0;
     for (const auto& k : all) {
       const size_t bytes = std::min<size_t>(v * k.size, 16);
@@ -281,26 +345,31 @@ int run_length(const mrt_rotary& r, const mrt_norm_tensor& x, const void* X, con
   return 1;
 }
 
-template <typename TX, typename TY, bool BWD>
+template <typename TX, typename TY, bool BWD, int AHEAD>
 void run_form(const NormArgs& a, int v, bool halves, dim3 grid, size_t lds, hipStream_t s) {
-  if (v == 1) k_norm_rotary<TX, TY, 1, true, 4, BWD><<<grid, kThreadsNorm, lds, s>>>(a);
+  if (v == 1) k_norm_rotary<TX, TY, 1, true, 4, BWD, AHEAD><<<grid, kThreadsNorm, lds, s>>>(a);
   else if (halves) {
-    if (v == 8) k_norm_rotary<TX, TY, 8, true, 1, BWD><<<grid, kThreadsNorm, lds, s>>>(a);
-    else if (v == 4) k_norm_rotary<TX, TY, 4, true, 1, BWD><<<grid, kThreadsNorm, lds, s>>>(a);
-    else k_norm_rotary<TX, TY, 2, true, 2, BWD><<<grid, kThreadsNorm, lds, s>>>(a);
+    if (v == 4) k_norm_rotary<TX, TY, 4, true, 1, BWD, AHEAD><<<grid, kThreadsNorm, lds, s>>>(a);
+    else k_norm_rotary<TX, TY, 2, true, 2, BWD, AHEAD><<<grid, kThreadsNorm, lds, s>>>(a);
   } else {
-    if (v == 8) k_norm_rotary<TX, TY, 8, false, 1, BWD><<<grid, kThreadsNorm, lds, s>>>(a);
-    else if (v == 4) k_norm_rotary<TX, TY, 4, false, 1, BWD><<<grid, kThreadsNorm, lds, s>>>(a);
-    else k_norm_rotary<TX, TY, 2, false, 2, BWD><<<grid, kThreadsNorm, lds, s>>>(a);
+    if constexpr (sizeof(TX) + sizeof(TY) < 8)
+      if (v == 8) return (void)(k_norm_rotary<TX, TY, 8, false, 1, BWD, AHEAD><<<grid, kThreadsNorm, lds, s>>>(a));
+    if (v == 4) k_norm_rotary<TX, TY, 4, false, 1, BWD, AHEAD><<<grid, kThreadsNorm, lds, s>>>(a);
+    else k_norm_rotary<TX, TY, 2, false, 2, BWD, AHEAD><<<grid, kThreadsNorm, lds, s>>>(a);
   }
 }
 template <typename TX, typename TY>
 void run_types(const NormArgs& a, int v, bool halves, bool backward, dim3 grid, size_t lds, hipStream_t s) {
-  if (backward) run_form<TX, TY, true>(a, v, halves, grid, lds, s);
-  else run_form<TX, TY, false>(a, v, halves, grid, 0, s);
+  if (!backward) run_form<TX, TY, false, 2>(a, v, halves, grid, 0, s);
+  else if (a.heads_a_thread > 1) run_form<TX, TY, true, 2>(a, v, halves, grid, lds, s);
+  else run_form<TX, TY, true, 1>(a, v, halves, grid, lds, s);
 }
 
-constexpr long long kEnoughThreads = 1 << 16;
+// Heads a lane turns with one set of angles, weights and, backward, sums: as many as leave enough threads to keep the
+// memory busy (us for Q and K, bf16, 12 heads of 128, with 2^16, 2^17 and 2^18 threads: forward 4680 tokens 14.1, 12.7, 13.7, a
+// weight for every head 16.3, 13.3, 14.3, 16 heads of 80, 3000 tokens, 12.6, 10.4, 10.4; backward 4680 tokens 22.6, 23.8, 26.5,
+// 1560 tokens 13.4, 13.7, 16.2).
+constexpr long long kEnoughForward = 1 << 17, kEnoughBackward = 1 << 16;
 
 }  // namespace
 
@@ -315,7 +384,8 @@ hipError_t launch_norm_rotary(const mrt_rotary& r, float eps, const mrt_norm_ten
   a.d = r.head_dim;
   a.eps = eps;
   a.inv_d = 1.0f / r.head_dim;
-  rotary_turns(r, backward, a.turns);
+  rotary_turns(r, backward, a.quarters);
+  for (int p = 0; p < a.pairs; ++p) a.quarters[p] *= 4;
   NormJoin join;
   join.d = r.head_dim;
   int most_joined = 0;
@@ -341,9 +411,12 @@ hipError_t launch_norm_rotary(const mrt_rotary& r, float eps, const mrt_norm_ten
       each = each || (backward && t.dweight && t.weight_head);
     }
     a.heads_a_thread = each ? 1 : 16;
-    while (a.heads_a_thread > 1 && threads / a.heads_a_thread < kEnoughThreads) a.heads_a_thread /= 2;
+    while (a.heads_a_thread > 1 && threads / a.heads_a_thread < (backward ? kEnoughBackward : kEnoughForward)) a.heads_a_thread /= 2;
     if (!each)
       while ((most_heads + a.heads_a_thread - 1) / a.heads_a_thread > (backward ? kMostNormParts : 65535)) a.heads_a_thread *= 2;
+    // (runs of one length)
+    const int runs_a_row = (most_heads + a.heads_a_thread - 1) / a.heads_a_thread;
+    a.heads_a_thread = (most_heads + runs_a_row - 1) / runs_a_row;
     int blocks[2] = {0, 0};
     for (int i = 0; i < count; ++i) {
       const int k = first + i;
