@@ -1353,7 +1353,8 @@ mrt_status dense_attn_cache8_check(const mrt_problem* p, const mrt_cache8* c, in
 size_t dense_attn_fwd_cache8_workspace_bytes(const mrt_problem* p, const mrt_cache8* c, int causal_chunk) {
   if (dense_attn_cache8_check(p, c, causal_chunk) != MRT_OK) return 0;
   const mrt_problem q = cache8_problem(p, c);
-  return dense_cache8_workspace_bytes(dense_params(&q, causal_chunk), p->batch * p->heads, p->heads / c->heads);
+  return dense_cache8_workspace_bytes(dense_params(&q, causal_chunk), p->batch * p->heads, p->heads / c->heads,
+                                       c->format == MRT_CACHE_E4M3);
 }
 
 mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, float* lse, const mrt_problem* p, const int* kv_len,
@@ -1379,6 +1380,7 @@ mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, fl
     cache.ke_batch = c->k_scale_batch; cache.ke_head = c->k_scale_head;
     cache.ve_batch = c->v_scale_batch; cache.ve_head = c->v_scale_head;
     cache.shift = shift;
+    cache.rounds = DenseRounds{0, 0, 0};
     return launch_dense_cache8(kp, BH, workspace, workspace_bytes, cache, s);
   };
   const hipError_t e = timed_launch(s, MRT_KERNEL_DENSE, [&] {

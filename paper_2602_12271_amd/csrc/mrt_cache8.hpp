@@ -61,6 +61,6 @@ hipError_t launch_cache8_read(const Cache8Call& c, bool e4m3, mrt_dtype dtype, h
 // The attention over a cache (mrt_dense_cache8.hip).
 template <bool E4M3>
 hipError_t launch_dense_cache8(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseCache8<E4M3>& cache, hipStream_t s);
-size_t dense_cache8_workspace_bytes(const KParams& kp, int nbh, int group);
+size_t dense_cache8_workspace_bytes(const KParams& kp, int nbh, int group, bool e4m3);
 
 }  // namespace mrt

@@ -155,8 +155,27 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
     tile = nx - 1 - (int)round;
     run = (int)(blockIdx.x - round * parts.runs);
   }
-  const int q0 = tile * WGQ;
-  const int bh = PART ? run / parts.n : run, part = PART ? run - bh * parts.n : 0;
+  int q0 = tile * WGQ;
+  int bh = PART ? run / parts.n : run, part = PART ? run - bh * parts.n : 0;
+  // CODES: of a call whose last round is shared (DenseRounds) the tile, counted from that round's first, or -1
+  [[maybe_unused]] int rest = -1;
+  [[maybe_unused]] bool own_rows = false;
+  if constexpr (PART && CODES)
+    if (save.rounds.rest > 0) {
+      const DenseRounds& r = save.rounds;
+      auto spread = [](int at, int n) { return (at & 7) * (n >> 3) + ((at & 7) < (n & 7) ? (at & 7) : (n & 7)) + (at >> 3); };
+      int unit = blockIdx.x;
+      if (unit < r.whole) unit = spread(unit, r.whole);
+      else {
+        const int x = spread(unit - r.whole, r.rest * parts.n);
+        rest = x / parts.n;
+        part = x - rest * parts.n;
+        unit = r.whole + rest;
+      }
+      own_rows = rest < 0;
+      bh = unit / nx;
+      q0 = (unit - bh * nx) * WGQ;
+    }
   const int b = bh / p.H, hd = bh - b * p.H;
   int kvh = hd;
   const int qw0 = q0 + 16 * QT * wq;                      // this wave's first query
@@ -164,11 +183,13 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
     kvh = hd / save.group;
     if (save.kv_len) p.Nkv = __builtin_amdgcn_readfirstlane(min(max(save.kv_len[b], 0), p.Nkv));
     if (p.Nkv == 0) {                                     // an empty sequence
-      const long long row0 = PART ? ((long long)part * parts.heads + bh) * p.Nq : 0;
+      long long row0 = PART ? ((long long)part * parts.heads + bh) * p.Nq : 0;
+      if constexpr (PART && CODES)
+        if (rest >= 0) row0 = ((long long)part * save.rounds.rest + rest) * WGQ - q0;
       for (int i = tid; i < WGQ * D; i += kDenseThreads) {
         const int q = q0 + i / D, f = i % D;
         if (q >= p.Nq) break;
-        if constexpr (PART) {
+        if (PART && !own_rows) {
           parts.o[(row0 + q) * D + f] = 0.f;
           if (f == 0) parts.ml[row0 + q] = make_float2(kNoKey, 0.f);
         } else {
@@ -198,7 +219,9 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
   const int mid = WK == 1 ? visible(q0 + WGQ / 2 - 1 < p.Nq ? q0 + WGQ / 2 - 1 : p.Nq - 1) : nkeys;
   const int nmid = (mid + 63) >> 6, npairs = nmid + ((nkeys - mid + 63) >> 6);
   auto first_key = [&](int pr) { return pr < nmid ? 64 * pr : mid + 64 * (pr - nmid); };
-  const int p0 = PART ? part * npairs / parts.n : 0, p1 = PART ? (part + 1) * npairs / parts.n : npairs;   // this part's pairs
+  int p0 = PART ? part * npairs / parts.n : 0, p1 = PART ? (part + 1) * npairs / parts.n : npairs;   // this part's pairs
+  if constexpr (PART && CODES)
+    if (own_rows) p0 = 0, p1 = npairs;
   const KV* Kp = (const KV*)p.K + b * p.ks.batch + kvh * p.ks.head;
   const KV* Vp = (const KV*)p.V + b * p.vs.batch + kvh * p.vs.head;
   const unsigned kvoff = (unsigned)(tid / Tile::CPR) * krow + 8u * EB * (tid % Tile::CPR);
@@ -396,17 +419,22 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
       for (int vt = 0; vt < NVT; ++vt) o[q][vt] = o[q][vt] * f0 + xo[(q * (NVT + 1) + vt) * 64] * f1;
     }
   }
-  if constexpr (PART) {
-    const long long row0 = ((long long)part * parts.heads + bh) * p.Nq;
+  if (PART && !own_rows) {
+    long long row0 = ((long long)part * parts.heads + bh) * p.Nq;
+    if constexpr (PART && CODES)
+      if (rest >= 0) row0 = ((long long)part * save.rounds.rest + rest) * WGQ - q0;
+    // (hidden for the same reason as below: 12 heads of 4680 queries of 32760 keys in four parts 777 -> 575 us)
+    int col = c, row = g;
+    if constexpr (CODES && D == 64) asm volatile("" : "+v"(col), "+v"(row));
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
-      const int qi = qw0 + 16 * q + c;
+      const int qi = qw0 + 16 * q + col;
       const float lsum = xsum(lrun[q]);
       if (qi < p.Nq) {
-        float* row = parts.o + (row0 + qi) * D + 4 * g;
+        float* at = parts.o + (row0 + qi) * D + 4 * row;
 #pragma unroll
-        for (int vt = 0; vt < NVT; ++vt) *(f32x4*)(row + 16 * vt) = o[q][vt];
-        if (g == 0) parts.ml[row0 + qi] = make_float2(mref[q], lsum);
+        for (int vt = 0; vt < NVT; ++vt) *(f32x4*)(at + 16 * vt) = o[q][vt];
+        if (row == 0) parts.ml[row0 + qi] = make_float2(mref[q], lsum);
       }
     }
     return;
@@ -469,12 +497,24 @@ __global__ __launch_bounds__(256) void k_dense_merge(KParams p, DenseParts parts
   }
   const float inv = lsum > 0.f ? 1.0f / lsum : 0.f;
   const f32x4 x = o * inv;
-  const int bh = row / p.Nq, q = row - bh * p.Nq, b = bh / p.H, hd = bh - b * p.H;
+  int bh = row / p.Nq, q = row - bh * p.Nq;
+  if constexpr (dense_codes<Save>)
+    if (save.rounds.rest > 0) {      // rows of the last round's tiles
+      const DenseRounds& r = save.rounds;
+      const int nx = (p.Nq + r.queries - 1) / r.queries, at = row / r.queries, unit = r.whole + at;
+      bh = unit / nx;
+      q = (unit - bh * nx) * r.queries + row - at * r.queries;
+      if (q >= p.Nq) return;
+    }
+  const int b = bh / p.H, hd = bh - b * p.H;
   typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
   *(bf16x4*)((u16*)p.O + b * p.os.batch + hd * p.os.head + (long long)q * p.os.token + f) =
       bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-  if constexpr (!std::is_same<Save, NoSave>::value)
+  if constexpr (dense_codes<Save>) {
+    if (f == 0) save.lse[(long long)bh * p.Nq + q] = natural_lse(m, lsum);
+  } else if constexpr (!std::is_same<Save, NoSave>::value) {
     if (f == 0) save.lse[row] = natural_lse(m, lsum);
+  }
 }
 
 template <int D, int QT, int WK, bool PART, typename Save>

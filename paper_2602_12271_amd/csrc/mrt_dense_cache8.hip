@@ -12,11 +12,14 @@
 #include "mrt_dense_bf16.hpp"
 
 #include <algorithm>
+#include <cmath>
 
 namespace mrt {
 
 namespace {
 
+constexpr int kMostFewParts = 128;
+constexpr size_t kMostRoundsBytes = (size_t)192 << 20;
 constexpr int kFewWaves = 4, kFewThreads = 64 * kFewWaves, kFewKeys = 32;
 
 // 32 keys and values of a wave, as they come from memory
@@ -28,9 +31,10 @@ struct FewTile {
   unsigned char ke[2], ve[2];
 };
 
+// part_tiles: tiles of 32 keys of a part.  A sequence has as many parts as its own length takes.
 template <int D, bool E4M3, int RT, bool PART>
 __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KParams p, DenseParts parts, DenseCache8<E4M3> cache,
-                                                                             int row_tiles) {
+                                                                             int row_tiles, int part_tiles) {
   constexpr int KP = D / 64, NK = D / 32, NV = D / 16, LD = D + 4;
   extern __shared__ __attribute__((aligned(16))) float few_lds[];      // [wave][row][LD], then [wave][row] references, sums
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
@@ -46,7 +50,8 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
   if (cache.kv_len) p.Nkv = __builtin_amdgcn_readfirstlane(min(max(cache.kv_len[b], 0), p.Nkv));
   const int nkeys = p.Nkv > 0 ? dense_visible(p, p.Nq - 1) : 0, nfree = dense_visible(p, 0);
   const int tiles = (nkeys + kFewKeys - 1) / kFewKeys;
-  const int t0 = PART ? (int)((long long)part * tiles / parts.n) : 0, t1 = PART ? (int)((long long)(part + 1) * tiles / parts.n) : tiles;
+  const int t0 = PART ? part * part_tiles : 0, t1 = PART ? min(t0 + part_tiles, tiles) : tiles;
+  if (PART && t0 >= tiles) return;                      // (k_cache8_join knows)
 
   // row r of the tile: query r % Nq of head r / Nq of those that share the keys
   int limit[RT];
@@ -61,31 +66,44 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
   }
 
   const unsigned krow = (unsigned)p.ks.token, vrow = (unsigned)p.vs.token, last = (unsigned)(nkeys - 1);
-  const auto kr = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)p.K + b * p.ks.batch + kvh * p.ks.head), 0, last * krow + D, 0x00020000);
-  const auto vr = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)p.V + b * p.vs.batch + kvh * p.vs.head), 0, last * vrow + D, 0x00020000);
-  const int exps = (int)(last >> cache.shift) + 1;
-  const auto ker = __builtin_amdgcn_make_buffer_rsrc((void*)(cache.k_exp + b * cache.ke_batch + kvh * cache.ke_head), 0, exps, 0x00020000);
-  const auto ver = __builtin_amdgcn_make_buffer_rsrc((void*)(cache.v_exp + b * cache.ve_batch + kvh * cache.ve_head), 0, exps, 0x00020000);
-  auto fetch = [&](FewTile<D>& x, int t) {              // (zeros beyond the last key)
-    const unsigned key = (unsigned)t * kFewKeys;
+  const char* Kp = (const char*)p.K + b * p.ks.batch + kvh * p.ks.head;
+  const char* Vp = (const char*)p.V + b * p.vs.batch + kvh * p.vs.head;
+  const unsigned char* ke = cache.k_exp + b * cache.ke_batch + kvh * cache.ke_head;
+  const unsigned char* ve = cache.v_exp + b * cache.ve_batch + kvh * cache.ve_head;
+  // a lane's places in a tile; a tile's resource begins at its first key, so that they stay (zeros beyond the last key)
+  unsigned koff[2][KP], voff[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      x.ke[h] = __builtin_amdgcn_raw_buffer_load_b8(ker, (key + 16 * h + c) >> cache.shift, 0, 0);
-      x.ve[h] = __builtin_amdgcn_raw_buffer_load_b8(ver, (key + 16 * h + 4 * g) >> cache.shift, 0, 0);
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int j = 0; j < KP; ++j) koff[h][j] = (16 * h + c) * krow + 16 * (g + 4 * j);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) voff[e] = (16 * (e / 4) + 4 * g + e % 4) * vrow + D / 16 * c;
+  auto fetch = [&](FewTile<D>& x, int t) {
+    const unsigned key = (unsigned)t * kFewKeys;
+    // (what is the same in all lanes has to be known as such, or every load becomes a loop over the resources of the lanes)
+    auto from = [&](const char* base, unsigned row) {
+      return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (unsigned)__builtin_amdgcn_readfirstlane(key * row)), 0,
+                                               __builtin_amdgcn_readfirstlane((last - key) * row + D), 0x00020000);
+    };
+    const auto kr = from(Kp, krow), vr = from(Vp, vrow);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                       // (a block has 16 tokens at least)
+      const unsigned block = __builtin_amdgcn_readfirstlane(min(key + 16 * h, last) >> cache.shift);
+      x.ke[h] = ke[block];
+      x.ve[h] = ve[block];
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int j = 0; j < KP; ++j) x.k[h][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, (key + 16 * h + c) * krow + 16 * (g + 4 * j), 0, 0);
+      for (int j = 0; j < KP; ++j) x.k[h][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff[h][j], 0, 0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const unsigned off = (key + 16 * (e / 4) + 4 * g + e % 4) * vrow + D / 16 * c;
       if constexpr (D == 128) {
-        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(vr, off, 0, 0);
+        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(vr, voff[e], 0, 0);
         x.v[e][0] = w[0];
         x.v[e][1] = w[1];
       } else {
-        x.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(vr, off, 0, 0);
+        x.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(vr, voff[e], 0, 0);
       }
     }
   };
@@ -104,7 +122,7 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
     f32x4 s[RT][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float scale = cache8_scale(x.ke[h]);
+      const float scale = cache8_scale(__builtin_amdgcn_readfirstlane(x.ke[h]));
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
         const u32x4 w = x.k[h][k / 2];
@@ -112,6 +130,7 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
 #pragma unroll
         for (int i = 0; i < RT; ++i) s[i][h] = mfma(key, qv[i][k], k ? s[i][h] : f32x4{0.f, 0.f, 0.f, 0.f});
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     bf16x8 pb[RT];
     const int key = t * kFewKeys;
@@ -146,8 +165,9 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
         }
       pb[i] = pack8(s[i][0], s[i][1]);
     }
+    __builtin_amdgcn_sched_barrier(0);
     // values: pairs of features of a key, then pairs of keys of a feature
-    const float vs[2] = {cache8_scale(x.ve[0]), cache8_scale(x.ve[1])};
+    const float vs[2] = {cache8_scale(__builtin_amdgcn_readfirstlane(x.ve[0])), cache8_scale(__builtin_amdgcn_readfirstlane(x.ve[1]))};
 #pragma unroll
     for (int w = 0; w < D / 64; ++w) {
       unsigned pair[2][8];                              // features 4w, 4w + 1 and 4w + 2, 4w + 3 of each key
@@ -167,18 +187,21 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
 #pragma unroll
         for (int i = 0; i < RT; ++i) o[i][4 * w + f] = mfma(__builtin_bit_cast(bf16x8, a), pb[i], o[i][4 * w + f]);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  FewTile<D> x, y;
+  // two tiles by turns: one is loaded while the other is used (three or four, at the price of registers, measured no faster)
+  FewTile<D> x[2];
   int t = t0 + wave;
-  if (t < t1) fetch(x, t);
+  if (t < t1) fetch(x[0], t);
   for (; t < t1; t += 2 * kFewWaves) {
-    if (t + kFewWaves < t1) fetch(y, t + kFewWaves);
-    use(x, t);
-    if (t + kFewWaves >= t1) break;
-    if (t + 2 * kFewWaves < t1) fetch(x, t + 2 * kFewWaves);
-    use(y, t + kFewWaves);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = t + i * kFewWaves, next = at + kFewWaves;
+      if (next < t1) fetch(x[1 - i], next);
+      if (at < t1) use(x[i], at);
+    }
   }
 
   // the waves' sums, against the largest reference
@@ -228,20 +251,88 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
   }
 }
 
+// O from the parts of few rows: a workgroup a row, whose threads take four features of every eighth (or sixteenth) part, all
+// of them under way at once.
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256) void k_cache8_join(KParams p, DenseParts parts, DenseCache8<E4M3> cache, int part_tiles) {
+  constexpr int TPR = D / 4, RUNS = 256 / TPR, MOST = kMostFewParts / RUNS;
+  __shared__ __attribute__((aligned(16))) float sums[RUNS][D + 4];
+  __shared__ float2 mls[RUNS];
+  const int row = blockIdx.x, bh = row / p.Nq, q = row - bh * p.Nq, b = bh / p.H, hd = bh - b * p.H;
+  if (cache.kv_len) p.Nkv = min(max(cache.kv_len[b], 0), p.Nkv);
+  const int nkeys = p.Nkv > 0 ? dense_visible(p, p.Nq - 1) : 0;
+  const int n = ((nkeys + kFewKeys - 1) / kFewKeys + part_tiles - 1) / part_tiles;
+  const int run = threadIdx.x / TPR, f = 4 * (threadIdx.x % TPR);
+  const size_t rows = (size_t)parts.heads * p.Nq;
+  float2 ml[MOST];
+  f32x4 po[MOST];
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) {
+    const int part = run + RUNS * i;
+    ml[i] = make_float2(kNoKey, 0.f);
+    po[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (part < n) {
+      ml[i] = parts.ml[part * rows + row];
+      po[i] = *(const f32x4*)(parts.o + (part * rows + row) * D + f);
+    }
+  }
+  float m = kNoKey, sum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) m = fmaxf(m, ml[i].x);
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) {
+    const float w = exp2_fast(ml[i].x - m);
+    sum += ml[i].y * w;
+    o = o + po[i] * w;
+  }
+  *(f32x4*)&sums[run][f] = o;
+  if (f == 0) mls[run] = make_float2(m, sum);
+  __syncthreads();
+  if (threadIdx.x >= TPR) return;
+  m = kNoKey;
+  sum = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i) m = fmaxf(m, mls[i].x);
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i) {
+    const float w = exp2_fast(mls[i].x - m);
+    sum += mls[i].y * w;
+    o = o + *(const f32x4*)&sums[i][f] * w;
+  }
+  const f32x4 x = o * (sum > 0.f ? 1.0f / sum : 0.f);
+  typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+  *(bf16x4*)((u16*)p.O + b * p.os.batch + hd * p.os.head + (long long)q * p.os.token + f) =
+      bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+  if (f == 0) cache.lse[row] = natural_lse(m, sum);
+}
+
 struct FewShape {
   int rt, row_tiles, parts;      // tiles of 16 rows of a workgroup, workgroups for all rows, for all keys; rt = 0: not this kernel
+  int part_tiles;
 };
 
-constexpr int kFewQueries = 16;
 FewShape few_shape(const KParams& kp, int nbh, int group, bool may_split) {
-  FewShape f = {0, 1, 1};
-  if (kp.Nq > kFewQueries) return f;
+  FewShape f = {0, 1, 1, 0};
+  if (kp.Nq > 32) return f;
   const int rows = group * kp.Nq;
   f.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   f.row_tiles = (rows + 16 * f.rt - 1) / (16 * f.rt);
-  const long long wgs = (long long)nbh / group * f.row_tiles, tiles = (dense_visible(kp, kp.Nq - 1) + kFewKeys - 1) / kFewKeys;
-  const long long want = (4ll * compute_units() / (f.rt == 4 ? 2 : 1) + wgs - 1) / wgs;
-  f.parts = may_split ? (int)std::max(1ll, std::min({want, tiles / 8, 64ll})) : 1;
+  const long long wgs = (long long)nbh / group * f.row_tiles;
+  // The kernel of many rows takes 64 queries of a head at a time, whose keys it has in LDS once (us, that one | this one: 12
+  // heads over 4680 keys, 12 queries 17.5 | 12.9, 32 18.1 | 16.5, 48 19.0 | 18.8; 32 sharing 8 over 8192 keys 28.4 | 19.1, 29.8 | 25.8, 30.9 |
+  // 30.4; over 2048 keys, batch of 8, where tiles fill the chip without sharing keys, 36.8 | 25.5, 24 queries 36.7 | 38.7, 32 38.1 | 43.8).
+  if (kp.Nq > 16 && wgs > 64) return {0, 1, 1, 0};
+  const long long tiles = (dense_visible(kp, kp.Nq - 1) + kFewKeys - 1) / kFewKeys;
+  // As many workgroups as the chip holds at once (two a compute unit, one of 64 rows), each with a tile for every wave.  us by the
+  // number of parts: 32 heads sharing 8 over 32760 keys, batch of 4 (lengths 8190 .. 32760), 8 47.8, 16 46.0, 24 48.2, 32 47.5, 64
+  // 50.3; 12 heads 10 34.6, 20 25.5, 42 25.2, 64 26.6; 8 key heads, 4096 keys, 8 10.3, 16 9.2, 32 8.3, 64 9.5; one of 32760 keys 32
+  // 13.5, 64 11.1, 96 10.3; 32 heads of 2048 keys, batch of 64, 1 199, 2 210, 8 226; 300 keys 1 6.3, 2 8.2, 6 7.2.
+  const long long want = 2ll * compute_units() / (f.rt == 4 ? 2 : 1) / wgs;
+  const long long n = may_split && tiles > 12 ? std::max(1ll, std::min({want, tiles / kFewWaves, (long long)kMostFewParts})) : 1;
+  f.part_tiles = (int)((tiles + n - 1) / n);
+  f.parts = (int)((tiles + f.part_tiles - 1) / f.part_tiles);
   return f;
 }
 
@@ -251,11 +342,8 @@ hipError_t run_few(const KParams& kp, int nbh, const FewShape& f, const DensePar
   const auto kernel = f.parts > 1 ? k_cache8_few<D, E4M3, RT, true> : k_cache8_few<D, E4M3, RT, false>;
   const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
-  kernel<<<nbh / cache.group * f.row_tiles * f.parts, kFewThreads, lds, s>>>(kp, parts, cache, f.row_tiles);
-  if (f.parts > 1) {
-    const int rows = nbh * kp.Nq, rpw = 256 / (D / 4);
-    k_dense_merge<D><<<(rows + rpw - 1) / rpw, 256, 0, s>>>(kp, parts, rows, cache);
-  }
+  kernel<<<nbh / cache.group * f.row_tiles * f.parts, kFewThreads, lds, s>>>(kp, parts, cache, f.row_tiles, f.part_tiles);
+  if (f.parts > 1) k_cache8_join<D><<<nbh * kp.Nq, 256, 0, s>>>(kp, parts, cache, f.part_tiles);
   return hipGetLastError();
 }
 template <int D, bool E4M3>
@@ -265,26 +353,113 @@ hipError_t run_few_d(const KParams& kp, int nbh, const FewShape& f, const DenseP
   return run_few<D, E4M3, 4>(kp, nbh, f, parts, cache, s);
 }
 
+// The shape of a call of many rows that all see the same keys: queries of a workgroup, and workgroups that share the keys of
+// every tile of queries, or of those of the last round only (DenseRounds), where tiles beside full rounds would leave a part of
+// the chip idle.  A model of microseconds: rounds of as many workgroups as the chip holds (128 features: one a compute unit; 64:
+// two, with a lower cost where there is one), each of its steps of 64 keys and a beginning and an end; the launch that joins
+// parts, and their bytes, written and read.  Fitted to 40 shapes of 1 to 40 heads and 576 to 32760 keys, each timed with up to 35
+// ways; us | model: 12 heads of 1560 queries of 32760 keys, 256 queries shared by three 330 | 321, one by one 831 | 879; 16 heads of
+// 4680 of 14040, 256 whole rounds and 48 tiles shared by five 494 | 491, by four 505 | 507, all shared by three 568, one by one
+// 755 | 766.  (Two workgroups of unequal length for every tile of one incomplete round, so that units without a tile take the shorter
+// ones by turns, measured 894 us where one by one takes 856: 228 tiles of 512 steps.)
+struct RoundsShape {
+  DenseRounds r;         // rest = 0: no tiles of their own kind
+  int parts;             // 0: no call of this kind
+  size_t bytes;
+};
+RoundsShape rounds_shape(const KParams& kp, int nbh, bool e4m3, size_t most_bytes) {
+  RoundsShape best = {{0, 0, 0}, 0, 0};
+  if (dense_visible(kp, 0) != dense_visible(kp, kp.Nq - 1)) return best;
+  const bool wide = kp.d == 128;
+  const long long steps = (dense_visible(kp, 0) + 63) / 64, slots = compute_units() * (wide ? 1ll : 2ll);
+  double least = 0;
+  for (int i = 0, queries = 64; queries <= (wide ? 256 : 128); queries *= 2, ++i) {
+    static const double full_step[2][2][3] = {{{0.90, 1.14, 1.69}, {1.13, 1.43, 1.92}}, {{0.66, 1.17}, {0.99, 1.38}}};
+    static const double lone_step[2][2] = {{0.54, 0.78}, {0.62, 0.92}};
+    const long long units = (long long)((kp.Nq + queries - 1) / queries) * nbh;
+    if (units > 0xffffff) continue;
+    auto time = [&](long long wgs, long long n, bool split) {       // `wgs` workgroups of n steps
+      const long long whole = wgs / slots, rest = wgs % slots;
+      const double full = full_step[!wide][!e4m3][i] * (wide || split || queries == 64 ? 1.0 : 1.06), lone = wide ? full : lone_step[!e4m3][i];
+      const double edge = wide ? 9.0 : 3.0;             // (two beside each other hide each other's)
+      return whole * (n * full + edge) + (rest ? n * (2 * rest > slots ? full : lone) + edge : 0.0);
+    };
+    auto look = [&](long long rest, int parts) {        // the tiles that `parts` workgroups share, of `units`
+      const size_t bytes = parts > 1 ? dense_parts_bytes(rest == units ? kp.Nq * nbh : (int)rest * queries, parts, kp.d) : 0;
+      if (bytes > most_bytes || bytes > kMostRoundsBytes) return;
+      double us = time(units - rest, steps, parts > 1) + time(rest * parts, (steps + parts - 1) / parts, parts > 1);
+      if (parts > 1) us = 1.03 * (us + (wide ? 5.5 : 4.0) + 2 * bytes / 5.0e6);       // (it has to promise something)
+      if (least > 0 && us >= least) return;
+      least = us;
+      best = {{(int)(units - rest), (int)rest, queries}, parts, bytes};
+    };
+    look(units, 1);
+    for (int parts = 2; parts <= 32 && 4 * parts <= steps && units * parts <= 6 * slots; ++parts) look(units, parts);
+    if (const long long rest = units % slots; rest > 0 && rest < units)
+      for (int parts = 2; parts <= kMostFewParts && 4 * parts <= steps && rest * parts <= slots; ++parts) look(rest, parts);
+  }
+  if (best.r.whole == 0) best.r.rest = 0;               // all tiles alike: the launches of every dense call
+  return best;
+}
+
+template <int D, bool E4M3, int QT, int WK>
+hipError_t run_rounds(const KParams& kp, int nbh, const RoundsShape& shape, const DenseParts& parts, DenseCache8<E4M3> cache, hipStream_t s) {
+  const auto kernel = k_bf16_dense<D, QT, WK, true, DenseCache8<E4M3>>;
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kDenseLds<D>);
+  if (e != hipSuccess) return e;
+  cache.rounds = shape.r;
+  kernel<<<shape.r.whole + shape.r.rest * shape.parts, kDenseThreads, kDenseLds<D>, s>>>(kp, parts, cache);
+  const int rows = shape.r.rest * shape.r.queries, rpw = 256 / (D / 4);
+  k_dense_merge<D><<<(rows + rpw - 1) / rpw, 256, 0, s>>>(kp, parts, rows, cache);
+  return hipGetLastError();
+}
+template <bool E4M3>
+hipError_t run_rounds(const KParams& kp, int nbh, const RoundsShape& shape, const DenseParts& parts, const DenseCache8<E4M3>& cache, hipStream_t s) {
+  if (kp.d == 64)
+    return shape.r.queries == 64 ? run_rounds<64, E4M3, 1, 2>(kp, nbh, shape, parts, cache, s) : run_rounds<64, E4M3, 2, 2>(kp, nbh, shape, parts, cache, s);
+  if (shape.r.queries == 64) return run_rounds<128, E4M3, 1, 2>(kp, nbh, shape, parts, cache, s);
+  return shape.r.queries == 128 ? run_rounds<128, E4M3, 2, 2>(kp, nbh, shape, parts, cache, s) : run_rounds<128, E4M3, 2, 1>(kp, nbh, shape, parts, cache, s);
+}
+
+// What a call with `bytes` of scratch does.
+struct Cache8Shape {
+  FewShape few;
+  RoundsShape rounds;    // rest = 0: the dense shape's
+  DenseShape dense;
+  size_t bytes;          // of parts
+};
+Cache8Shape cache8_shape(const KParams& kp, int nbh, int group, bool e4m3, size_t bytes) {
+  Cache8Shape c;
+  c.few = few_shape(kp, nbh, group, bytes > 0);
+  c.rounds = {{0, 0, 0}, 0, 0};
+  c.dense = {0, 1};
+  c.bytes = 0;
+  if (c.few.rt) {
+    c.bytes = c.few.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, c.few.parts, kp.d) : 0;
+    return c.bytes > bytes ? cache8_shape(kp, nbh, group, e4m3, 0) : c;
+  }
+  c.rounds = rounds_shape(kp, nbh, e4m3, bytes);
+  c.dense = c.rounds.parts ? DenseShape{c.rounds.r.queries, c.rounds.parts} : dense_call_shape(kp, nbh, bytes, true);
+  c.bytes = c.rounds.r.rest ? c.rounds.bytes : c.dense.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, c.dense.parts, kp.d) : 0;
+  return c;
+}
+
 }  // namespace
 
-size_t dense_cache8_workspace_bytes(const KParams& kp, int nbh, int group) {
-  const FewShape f = few_shape(kp, nbh, group, true);
-  if (f.rt == 0) return bf16_dense_workspace_bytes(kp, nbh, true);
-  return f.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, f.parts, kp.d) : 0;
+size_t dense_cache8_workspace_bytes(const KParams& kp, int nbh, int group, bool e4m3) {
+  return cache8_shape(kp, nbh, group, e4m3, ~(size_t)0).bytes;
 }
 
 template <bool E4M3>
 hipError_t launch_dense_cache8(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseCache8<E4M3>& cache, hipStream_t s) {
-  const size_t bytes = workspace ? workspace_bytes : 0;
-  FewShape f = few_shape(kp, nbh, cache.group, bytes > 0);
-  if (f.parts > 1 && bytes < dense_parts_bytes(kp.Nq * nbh, f.parts, kp.d)) f = few_shape(kp, nbh, cache.group, false);
-  const DenseShape shape = f.rt ? DenseShape{0, f.parts} : dense_call_shape(kp, nbh, bytes, true);
-  const size_t rows = (size_t)kp.Nq * nbh * shape.parts;
+  const Cache8Shape c = cache8_shape(kp, nbh, cache.group, E4M3, workspace ? workspace_bytes : 0);
+  const int n = c.few.rt ? c.few.parts : c.dense.parts;
+  const size_t rows = (c.rounds.r.rest ? (size_t)c.rounds.r.rest * c.rounds.r.queries : (size_t)kp.Nq * nbh) * n;
   const bool even = dense_visible(kp, 0) == dense_visible(kp, kp.Nq - 1);
-  const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), shape.parts, (unsigned)nbh,
-                            even ? 0u : (unsigned)nbh * shape.parts};
-  if (f.rt) return kp.d == 128 ? run_few_d<128>(kp, nbh, f, parts, cache, s) : run_few_d<64>(kp, nbh, f, parts, cache, s);
-  return run_dense_shape(kp, nbh, shape, parts, cache, s);
+  const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), n, (unsigned)nbh, even ? 0u : (unsigned)nbh * n};
+  if (c.few.rt) return kp.d == 128 ? run_few_d<128>(kp, nbh, c.few, parts, cache, s) : run_few_d<64>(kp, nbh, c.few, parts, cache, s);
+  if (c.rounds.r.rest) return run_rounds(kp, nbh, c.rounds, parts, cache, s);
+  return run_dense_shape(kp, nbh, c.dense, parts, cache, s);
 }
 template hipError_t launch_dense_cache8<true>(const KParams&, int, void*, size_t, const DenseCache8<true>&, hipStream_t);
 template hipError_t launch_dense_cache8<false>(const KParams&, int, void*, size_t, const DenseCache8<false>&, hipStream_t);

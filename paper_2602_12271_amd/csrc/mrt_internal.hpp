@@ -127,11 +127,17 @@ struct DenseSave {
   int group;            // heads that share one head of K and V
 };
 struct NoSave {};
+// A call of many rows over a cache whose tiles of queries do not fill the chip's last round: `whole` tiles have a workgroup
+// each, the keys of the `rest` behind them are shared by the call's number of parts.
+struct DenseRounds {
+  int whole, rest, queries;
+};
 // A forward call over a cache of 8 bits: keys and values are codes (KParams: strides in bytes), e4m3 or whole numbers.
 template <bool E4M3> struct DenseCache8 : DenseSave {
   const unsigned char *k_exp, *v_exp;             // exponents + 127 of the blocks of a (batch, key head)
   long long ke_batch, ke_head, ve_batch, ve_head; // their strides
   int shift;                                      // log2 of the tokens of a block
+  DenseRounds rounds;                             // rest = 0: not such a call
 };
 
 struct Plan {

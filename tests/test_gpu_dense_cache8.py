@@ -151,9 +151,53 @@ def test_hidden_nan_of_other_rows():
     assert got["O"][:, :, 640:].isnan().all() and torch.equal(got["O"][:, :, :512], want["O"][:, :, :512])
 
 
+ROUNDS = {
+    # tiles of queries beside the chip's 256 units: a few behind full rounds, which share their keys between many; most of a
+    # round, whose second parts the units without a tile take; lengths of their own, an empty one among them
+    "few-behind": Step(1, 1, 47, 69, heads=20),
+    "few-behind-d64": Step(1, 1, 47, 69, heads=21, dim=64),
+    "most-of-a-round": Step(1, 120, 10, 25, heads=234, kv_heads=2),
+    "most-of-a-round-d64": Step(1, 120, 10, 25, heads=234, kv_heads=2, dim=64),
+    "odd-tiles-padded": Step(1, 1, 41, 77, heads=10, batch=2, kv_len=(3000, 1033)),
+    "padded-empty": Step(1, 1, 47, 69, heads=5, kv_heads=1, batch=4, kv_len=(3243, 0, 100, 1)),
+    "padded-empty-d64": Step(1, 1, 47, 69, heads=5, kv_heads=1, dim=64, batch=4, kv_len=(3243, 0, 100, 1)),
+    "masked-alike": Step(3, 6, 22, 49, heads=20, chunk=3, offset=3),
+}
+
+
+@pytest.mark.parametrize("name", ROUNDS)
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+def test_last_round(name, format):
+    """Calls whose last round of workgroups is shared: the same as without scratch, up to roundings, everywhere."""
+    c = ROUNDS[name]
+    q, cache, k, v, do, kv_len = cached(c, seed=13, format=format)
+    got = attend(c, q, cache, kv_len)
+    again = attend(c, q, cache, kv_len)
+    alone = attend(c, q, cache, kv_len, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    ref, cost = reference(c, q, k, v, do)
+    print(f"  {name}: {check(c, got, ref, cost)}", flush=True)
+    check(c, alone, ref, cost)
+    for n in got:
+        assert torch.equal(got[n], again[n])
+
+
+def test_some_calls_share_their_last_round():
+    """Scratch of the rows of the tiles behind full rounds, not of all rows."""
+    for name in ("few-behind", "few-behind-d64", "masked-alike"):
+        c = ROUNDS[name]
+        q, cache, *_ = cached(c, seed=13)
+        args = {n: x for n, x in c.args.items() if n != "compute"}
+        need = pkg.dense_attn_fwd_cache8_workspace_bytes(q, cache, **args)
+        row = (c.dim + 2) * 4
+        print(f"  {name}: {need / row:.0f} rows of parts", flush=True)
+        assert need > 0 and need % (c.heads * c.nq * row) != 0 and need % (64 * row) == 0, name
+
+
 def test_same_bits_as_over_bf16_keys():
-    """Calls of many rows are those of the training step over the cache's values."""
-    for c in (Step(3, 9, 10, 11, heads=2, chunk=3, offset=6), Step(1, 4, 30, 52, heads=12), Step(700, 700, heads=4, kv_heads=2, chunk=1)):
+    """Calls under a mask that parts the queries are those of the training step over the cache's values."""
+    for c in (Step(6, 6, 9, 13, heads=4, kv_heads=1, chunk=2), Step(700, 700, heads=4, kv_heads=2, chunk=1),
+              Step(700, 700, heads=4, kv_heads=2, chunk=1, dim=64)):
         for format in ("e4m3", "int8"):
             q, cache, k, v, *_ = cached(c, seed=6, format=format)
             got = attend(c, q, cache)
