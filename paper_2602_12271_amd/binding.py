@@ -759,8 +759,10 @@ def _norm_weight(weight, x, name):
 
 def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder, positions):
     """x, y, dx: the norm's input, its result (or the gradient of that) and the gradient of x, of one or two tensors."""
-    key = (tuple([_layout_of(t) for t in (*x, *y, *dx, *weights, *positions)]), len(x), f_q, f_kv, h, w, q_frame_offset,
-           kv_frame_offset, theta, None if split is None else tuple(split), layout, ladder)
+    key = [f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, None if split is None else tuple(split), layout, ladder, len(x)]
+    for t in (*x, *y, *dx, *weights, *positions):
+        key += (None,) if t is None else (t.shape, t.stride(), t.dtype)
+    key = tuple(key)
     found = _norm_problems.get(key)
     if found is not None:
         return found
@@ -859,7 +861,7 @@ def norm_rotary_bwd(Q, K, q_weight, k_weight, dQ, dK=None, *, eps=1e-6, f_q=None
         weights, positions = (q_weight, k_weight), (q_positions, k_positions)
         r, tensors, pointers = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
                                              layout, ladder, positions)
-        dw = [None if u is None else torch.empty(u.shape, dtype=torch.float32, device=Q.device) for u in weights]
+        dw = [None if u is None else Q.new_empty(u.shape, dtype=torch.float32) for u in weights]
         tensors = _norm_tensors(tensors, weights, positions, dw)
         nbytes = lib.mrt_norm_rotary_bwd_workspace_bytes(ctypes.byref(r), tensors, len(x))
         scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if workspace is None and nbytes else workspace
@@ -925,19 +927,42 @@ def _cache8_of(c):
     return found
 
 
+# descriptions of recent rows without addresses, by their values, like _problems
+_rows: dict = {}
+
+
 def _cache8_rows(cache, K, V, at, lengths):
+    number = type(at) is int
+    key = (cache.K.shape, K.shape, K.stride(), K.dtype, V.shape, V.stride(), V.dtype, number or (at.dtype, at.shape, at.stride()),
+           lengths is None or (lengths.dtype, lengths.shape, lengths.stride()))
+    found = _rows.get(key)
+    if found is None:
+        import torch
+        B, H, _, d = cache.K.shape
+        _require(K.dim() == 4 and K.shape == V.shape and K.shape[:2] == (B, H) and K.shape[3] == d and K.dtype == V.dtype,
+                 f"K and V are [{B}, {H}, tokens, {d}] of one type")
+        _require(K.stride(3) == 1 and V.stride(3) == 1, "head_dim must be contiguous")
+        for name, x in (("at", None if number else at), ("lengths", lengths)):
+            _require(x is None or (x.dtype == torch.int32 and x.shape == (B,) and x.is_contiguous()),
+                     f"{name}: int32 [{B}], contiguous" + (", or a number" if name == "at" else ""))
+        found = MrtCache8Rows(K.shape[2], 0, None, None, MrtStrides(*K.stride()[:3]), MrtStrides(*V.stride()[:3]), _dtype_of(K, "K"))
+        if len(_rows) >= _MAX_PROBLEMS:
+            _rows.clear()
+        _rows[key] = found
+    found = MrtCache8Rows.from_buffer_copy(found)
+    if number:
+        found.at = at
+    else:
+        found.at_each = at.data_ptr()
+    if lengths is not None:
+        found.tokens_each = lengths.data_ptr()
+    return found
+
+
+def _require_places(at, lengths=None):
     import torch
-    B, H, _, d = cache.K.shape
-    _require(K.dim() == 4 and K.shape == V.shape and K.shape[:2] == (B, H) and K.shape[3] == d and K.dtype == V.dtype,
-             f"K and V are [{B}, {H}, tokens, {d}] of one type")
-    _require(K.stride(3) == 1 and V.stride(3) == 1, "head_dim must be contiguous")
-    each = []
-    for name, x in (("at", None if type(at) is int else at), ("lengths", lengths)):
-        _require(x is None or (isinstance(x, torch.Tensor) and x.dtype == torch.int32 and x.shape == (B,) and x.is_contiguous()),
-                 f"{name}: int32 [{B}], contiguous" + (", or a number" if name == "at" else ""))
-        each.append(None if x is None else x.data_ptr())
-    return MrtCache8Rows(K.shape[2], at if type(at) is int else 0, *each, MrtStrides(*K.stride()[:3]), MrtStrides(*V.stride()[:3]),
-                         _dtype_of(K, "K"))
+    _require(type(at) is int or isinstance(at, torch.Tensor), "at: a number, or int32 [batch] on the device")
+    _require(lengths is None or isinstance(lengths, torch.Tensor), "lengths: int32 [batch] on the device")
 
 
 def cache8_write(cache, K, V, *, at=0, lengths=None, stream=None):
@@ -946,6 +971,7 @@ def cache8_write(cache, K, V, *, at=0, lengths=None, stream=None):
     sequence that are there.  Rows before `at` keep their values; what was behind the new ones in their last block is no longer
     part of the cache.  The rounding is in the header's comment."""
     lib = load_library()
+    _require_places(at, lengths)
     _same_device(K, V, cache.K, cache.V, cache.K_scale, cache.V_scale, None if type(at) is int else at, lengths)
 
     def call(s):
@@ -963,12 +989,13 @@ def cache8_read(cache, tokens, *, at=0, dtype=None, out=None, v_out=None, stream
     import torch
     for y in (out, v_out):
         _require(y is None or dtype is None or y.dtype == dtype, "dtype is not that of the given output")
+    _require_places(at)
     _same_device(cache.K, cache.V, cache.K_scale, cache.V_scale, None if type(at) is int else at, out, v_out)
 
     def call(s):
         B, H, _, d = cache.K.shape
         given = dtype if dtype is not None else out.dtype if out is not None else v_out.dtype if v_out is not None else torch.bfloat16
-        K, V = [torch.empty(B, H, tokens, d, dtype=given, device=cache.K.device) if y is None else y for y in (out, v_out)]
+        K, V = [cache.K.new_empty((B, H, tokens, d), dtype=given) if y is None else y for y in (out, v_out)]
         _require(K.shape[2] == tokens, f"the output has {K.shape[2]} tokens, not {tokens}")
         c, rows = _cache8_of(cache), _cache8_rows(cache, K, V, at, None)
         st = lib.mrt_cache8_read(ctypes.byref(c), ctypes.byref(rows), K.data_ptr(), V.data_ptr(), s)
@@ -1028,14 +1055,14 @@ def dense_attn_fwd_cache8(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_
         O = torch.empty_like(Q) if out is None else out
         c = _cache8_of(cache)
         prob, nbytes = _cache8_problem(Q, O, cache, c, f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)
-        stats = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if lse is None else lse
+        stats = Q.new_empty(Q.shape[:3], dtype=torch.float32) if lse is None else lse
         _require_lse(stats, Q)
         _require(kv_len is None or (kv_len.dtype == torch.int32 and kv_len.shape == Q.shape[:1] and kv_len.is_contiguous()),
                  f"kv_len: int32 [{Q.shape[0]}], contiguous")
         scratch = workspace
         if scratch is None and nbytes and not torch.cuda.is_current_stream_capturing():
             try:
-                scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
+                scratch = Q.new_empty(nbytes, dtype=torch.uint8)
             except torch.cuda.OutOfMemoryError:       # a call that fits without its scratch still runs
                 pass
         ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())

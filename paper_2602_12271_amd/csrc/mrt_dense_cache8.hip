@@ -340,8 +340,10 @@ template <int D, bool E4M3, int RT>
 hipError_t run_few(const KParams& kp, int nbh, const FewShape& f, const DenseParts& parts, const DenseCache8<E4M3>& cache, hipStream_t s) {
   constexpr int lds = kFewWaves * 16 * RT * (D + 4 + 2) * (int)sizeof(float);
   const auto kernel = f.parts > 1 ? k_cache8_few<D, E4M3, RT, true> : k_cache8_few<D, E4M3, RT, false>;
-  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return e;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
   kernel<<<nbh / cache.group * f.row_tiles * f.parts, kFewThreads, lds, s>>>(kp, parts, cache, f.row_tiles, f.part_tiles);
   if (f.parts > 1) k_cache8_join<D><<<nbh * kp.Nq, 256, 0, s>>>(kp, parts, cache, f.part_tiles);
   return hipGetLastError();

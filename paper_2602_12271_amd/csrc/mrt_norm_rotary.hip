@@ -384,8 +384,18 @@ hipError_t launch_norm_rotary(const mrt_rotary& r, float eps, const mrt_norm_ten
   a.d = r.head_dim;
   a.eps = eps;
   a.inv_d = 1.0f / r.head_dim;
-  rotary_turns(r, backward, a.quarters);
-  for (int p = 0; p < a.pairs; ++p) a.quarters[p] *= 4;
+  // powers of the ladder's ratio in 64 significant bits, as rotary_turns has them, with one pow for a ladder that is shared
+  const long double quarter = (backward ? -2.0L : 2.0L) / 3.14159265358979323846264338327950288L;
+  long double at = quarter, ratio = 1;
+  for (int axis = 0, p = 0; axis < 3; ++axis) {
+    const bool shared = r.ladder == MRT_ROTARY_SHARED;
+    if (p == 0 || !shared) {
+      if (r.pairs[axis] == 0) continue;
+      at = quarter;
+      ratio = powl((long double)r.theta, -1.0L / (shared ? a.pairs : r.pairs[axis]));
+    }
+    for (int i = 0; i < r.pairs[axis]; ++i, at *= ratio) a.quarters[p++] = (double)at;
+  }
   NormJoin join;
   join.d = r.head_dim;
   int most_joined = 0;

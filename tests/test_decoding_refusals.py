@@ -290,8 +290,11 @@ def test_cache_binding_refusals():
                 dict(K=k.half(), V=k.half())):
         args = dict(K=k, V=k, at=0, lengths=None)
         args.update(bad)
-        with pytest.raises(pkg.MrtError):
-            B._cache8_rows(c, **args)
+        for _ in range(2):       # (refused again where a description is kept)
+            with pytest.raises(pkg.MrtError):
+                B._require_places(args["at"], args["lengths"])
+                B._cache8_rows(c, **args)
+            B._cache8_rows(c, k, k, 0, None)
     for bad in (dict(format="e5m2"), dict(block=48)):
         with pytest.raises(pkg.MrtError):
             pkg.cache8(1, 1, 8, 32, device="cpu", **bad)
