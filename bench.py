@@ -318,6 +318,70 @@ def bench_dense_step(args, wl, pkg, syn, torch, np, host, dev):
     }))
 
 
+def bench_cache_step(args, wl, pkg, torch, dev):
+    """A layer's decoding step against a cache of 8 bits, on the workload's tokens: norms and rotary positions of the
+    queries and of the newest rows of keys, these and their values into the cache, dense attention over it."""
+    Q, K, V = dev
+    n, first = wl.n_q, wl.n_kv - wl.n_q
+    cache = pkg.cache8(wl.batch, wl.heads, wl.n_kv, wl.head_dim, format=args.cache_format)
+    pkg.cache8_write(cache, K, V)
+    kn, vn = K[:, :, first:], V[:, :, first:]
+    gen = torch.Generator().manual_seed(7)
+    qw, kw = [(1 + 0.2 * torch.randn(wl.head_dim, generator=gen)).to(Q.device) for _ in range(2)]
+    grid = dict(f_q=wl.f_q, f_kv=wl.f_q, h=wl.h, w=wl.w, q_frame_offset=wl.q_frame_offset, kv_frame_offset=wl.q_frame_offset)
+    mask = dict(f_q=wl.f_q, f_kv=wl.f_kv, h=wl.h, w=wl.w, q_frame_offset=wl.q_frame_offset, causal_chunk=wl.causal_chunk, scale=wl.scale)
+
+    def step():
+        q, k = pkg.norm_rotary_fwd(Q, kn, qw, kw, **grid)
+        pkg.cache8_write(cache, k, vn, at=first)
+        return q, k, pkg.dense_attn_fwd_cache8(q, cache, **mask)
+
+    steps, warmup = min(args.steps, 50), min(args.warmup, 5)
+    for _ in range(warmup):
+        step()
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(steps):
+        q, k, (O, lse) = step()
+    torch.cuda.synchronize()
+    ms = (time.perf_counter() - t0) * 1e3 / steps
+    parts = {}
+    for name, fn in (("norm_rotary_fwd", lambda: pkg.norm_rotary_fwd(Q, kn, qw, kw, **grid)),
+                     ("cache8_write", lambda: pkg.cache8_write(cache, k, vn, at=first)),
+                     ("dense_attn_fwd_cache8", lambda: pkg.dense_attn_fwd_cache8(q, cache, **mask)),
+                     ("cache8_read", lambda: pkg.cache8_read(cache, wl.n_kv))):
+        fn()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(steps):
+            fn()
+        torch.cuda.synchronize()
+        parts[name + "_ms"] = (time.perf_counter() - t0) * 1e3 / steps
+    parity = None
+    if not args.no_cpu_baseline:
+        # head 0 in 64 bits from the cache's values, as many rows as take a few seconds
+        rows = min(n, 512)
+        a, (b, v) = q[0, 0, :rows].double().cpu(), (x[0, 0].double().cpu() for x in pkg.cache8_read(cache, wl.n_kv))
+        z = wl.scale * a @ b.t()
+        if wl.causal_chunk:
+            hw = wl.h * wl.w
+            chunk = lambda n, first: (first + torch.arange(n) // hw) // wl.causal_chunk       # noqa: E731
+            z.masked_fill_(chunk(wl.n_kv, 0)[None] > chunk(rows, wl.q_frame_offset)[:, None], -math.inf)
+        want = torch.softmax(z, -1) @ v
+        parity = float((O[0, 0, :rows].double().cpu() - want).norm() / want.norm())
+    flops = dense_flops(wl)
+    ach = flops / (ms / 1e3) / 1e12
+    print(json.dumps({
+        "metric": "cache8_decoding_step_ms", "value": ms, "unit": "ms/step", "n_gpus": 1, "steps": steps, "warmup": warmup,
+        "ms_per_step": ms, "higher_is_better": False, "scaling": "weak", "vs_baseline": None, "dtype": wl.dtype, "data": "synthetic",
+        "config": {"workload": f"{wl.name} decoding step: {wl.heads} heads x d{wl.head_dim}, N_q={n}, N_kv={wl.n_kv}, cache {args.cache_format}",
+                   **parts},
+        "roofline": {"bound": "mfma", "achieved": ach, "peak": 2500.0, "unit": "TFLOP/s", "frac": ach / 2500.0,
+                     "algorithmic_gflop": flops / 1e9, "note": "the two products of the attention over the time of the whole step"},
+        "parity_max_rel_err_head0": parity,
+    }))
+
+
 def measure_forward(wl, env, steps, warmup, *, head_groups=0, settle_s=0.0, with_dense=True, with_oracle=True,
                     oracle_budget_s=0.0, calibration_copy_mb=0, copy_gbs=None):
     """One workload through monarch_attn_fwd: whole-call time (default launch configuration),
@@ -526,9 +590,11 @@ def main():
     ap.add_argument("--also", default=None,
                     help="comma-separated workloads measured after the headline one and reported under "
                          "other_workloads (default: C2,C3,C4 when the headline is C1; 'none' for none)")
-    ap.add_argument("--op", default="fwd", choices=["fwd", "bwd", "dense-step"],
+    ap.add_argument("--op", default="fwd", choices=["fwd", "bwd", "dense-step", "cache-step"],
                     help="fwd: the forward operator (the headline metric); bwd: the backward pass; dense-step: rotary "
-                         "positions and the dense attention's forward and backward pass")
+                         "positions and the dense attention's forward and backward pass; cache-step: norms with rotary "
+                         "positions, the newest rows into a cache of 8 bits and dense attention over it")
+    ap.add_argument("--cache-format", default="e4m3", choices=["e4m3", "int8"], help="of --op cache-step")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-dense", action="store_true")
     ap.add_argument("--head-groups", type=int, default=0,
@@ -565,6 +631,10 @@ def main():
         Q, K, V = (torch.from_numpy(x).to(dev).to(tdt) for x in (Qh, Kh, Vh))
         if args.op == "dense-step":
             return bench_dense_step(args, wl, pkg, syn, torch, np, (Qh, Kh, Vh), (Q, K, V))
+        if args.op == "cache-step":
+            if wl.dtype != "bf16":
+                ap.error("--op cache-step takes a bf16 workload")
+            return bench_cache_step(args, wl, pkg, torch, (Q, K, V))
         prob = binding._torch_problem(Q, K, V, torch.empty_like(Q), wl.f_q, wl.f_kv, wl.h, wl.w,
                                       wl.q_frame_offset, wl.scale, pkg.MRT_COMPUTE_DEFAULT, wl.assign, wl.tile_h)
         stream = torch.cuda.current_stream(dev).cuda_stream

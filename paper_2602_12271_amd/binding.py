@@ -757,6 +757,11 @@ def _norm_weight(weight, x, name):
     return weight, _dtype_of(weight, name + "'s weight"), weight.stride(0) if weight.dim() == 2 and x.shape[1] > 1 else 0
 
 
+def _own_rows(weight):
+    """A weight of every head with a row of its own (expanded ones have one place for all, where their gradients have not)."""
+    return weight.contiguous() if weight is not None and weight.dim() == 2 and 0 <= weight.stride(0) < weight.shape[1] else weight
+
+
 def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder, positions):
     """x, y, dx: the norm's input, its result (or the gradient of that) and the gradient of x, of one or two tensors."""
     key = [f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, None if split is None else tuple(split), layout, ladder, len(x)]
@@ -825,7 +830,7 @@ def norm_rotary_fwd(Q, K=None, q_weight=None, k_weight=None, *, eps=1e-6, f_q=No
         if K is not None:
             x.append(K)
             y.append(torch.empty_like(K, dtype=dtype) if k_out is None else k_out)
-        weights, positions = (q_weight, k_weight), (q_positions, k_positions)
+        weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
         r, tensors, pointers = _norm_problem(x, y, (), weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
                                              layout, ladder, positions)
         tensors = _norm_tensors(tensors, weights, positions)
@@ -858,7 +863,7 @@ def norm_rotary_bwd(Q, K, q_weight, k_weight, dQ, dK=None, *, eps=1e-6, f_q=None
             x.append(K)
             g.append(dK)
             dx.append(torch.empty_like(K) if k_out is None else k_out)
-        weights, positions = (q_weight, k_weight), (q_positions, k_positions)
+        weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
         r, tensors, pointers = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
                                              layout, ladder, positions)
         dw = [None if u is None else Q.new_empty(u.shape, dtype=torch.float32) for u in weights]
@@ -961,7 +966,7 @@ def _cache8_rows(cache, K, V, at, lengths):
 
 def _require_places(at, lengths=None):
     import torch
-    _require(type(at) is int or isinstance(at, torch.Tensor), "at: a number, or int32 [batch] on the device")
+    _require(isinstance(at, torch.Tensor) or (type(at) is int and 0 <= at <= 1 << 24), "at: a number (0 .. 2^24), or int32 [batch] on the device")
     _require(lengths is None or isinstance(lengths, torch.Tensor), "lengths: int32 [batch] on the device")
 
 

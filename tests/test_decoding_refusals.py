@@ -285,7 +285,7 @@ def test_cache_binding_refusals():
                 c._replace(V=torch.zeros(2, 3, 40, 32, dtype=torch.int8)), c._replace(K=c.K.transpose(2, 3), V=c.V.transpose(2, 3))):
         with pytest.raises(pkg.MrtError):
             B._cache8_of(bad)
-    for bad in (dict(K=k[:, :2]), dict(V=k.bfloat16()), dict(K=k[..., :16], V=k[..., :16]), dict(at=torch.zeros(2)), dict(at=1.0),
+    for bad in (dict(K=k[:, :2]), dict(V=k.bfloat16()), dict(K=k[..., :16], V=k[..., :16]), dict(at=torch.zeros(2)), dict(at=1.0), dict(at=-1), dict(at=1 << 32), dict(at=None),
                 dict(at=torch.zeros(3, dtype=torch.int32)), dict(lengths=torch.zeros(2, dtype=torch.int64)), dict(lengths=5),
                 dict(K=k.half(), V=k.half())):
         args = dict(K=k, V=k, at=0, lengths=None)

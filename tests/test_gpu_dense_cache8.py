@@ -43,6 +43,8 @@ CASES = {
     "few-16-d64": Step(16, 640, heads=2, dim=64),
     "few-16-shared": Step(16, 1300, heads=16, kv_heads=2),
     "few-17": Step(17, 400, heads=3),
+    "few-24-many": Step(24, 300, heads=140, kv_heads=70),
+    "few-20-all-share-one": Step(20, 900, heads=40, kv_heads=1),
     "few-33-shared-d64": Step(33, 500, heads=8, kv_heads=4, dim=64),
     "few-causal": Step(5, 205, heads=4, kv_heads=2, chunk=1, offset=200),
     "few-causal-from-0": Step(9, 9, heads=4, kv_heads=2, chunk=1),

@@ -318,3 +318,20 @@ def test_far_addresses():
     torch.cuda.synchronize()
     for x, y in zip(got, want[2:]):
         assert torch.equal(x, y)
+
+
+def test_expanded_weights():
+    """A row of weights expanded over the heads is a weight of every head: gradients have a row each."""
+    sides, at, split, args = make((64, None, (2, 3, 5), 6, 3, 2), (BF16, BF16), "f32", seed=13)
+    (q, dq, qw), (k, dk, kw) = [[cuda(t) for t in s] for s in sides]
+    wide = [w[None].expand(h, 64) for w, h in ((qw, 6), (kw, 3))]
+    want = pkg.norm_rotary_bwd(q, k, *[w.contiguous() for w in wide], dq, dk, **args)
+    got = pkg.norm_rotary_bwd(q, k, *wide, dq, dk, **args)
+    shared = pkg.norm_rotary_bwd(q, k, qw, kw, dq, dk, **args)
+    both = [pkg.norm_rotary_fwd(q, k, *w, **args) for w in (wide, (qw, kw))]
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    assert all(torch.equal(x, y) for x, y in zip(*both))
+    for x, y in zip(got[2:], shared[2:]):
+        assert x.shape == (6 if x is got[2] else 3, 64) and (x.sum(0) - y).abs().max() <= 1e-4 * (1 + y.abs().max())
