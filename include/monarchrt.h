@@ -393,7 +393,8 @@ mrt_status mrt_norm_rotary_bwd(const mrt_rotary* r, double eps, const mrt_norm_t
  *   p->k and p->v not looked at.  kv_len: device memory, int [batch], or NULL, as mrt_dense_train.kv_len; masks, shared key heads,
  *   lse, rows that see no key, and infinities (NaN codes) as there.  Values meet the matrix unit unrounded; probabilities are rounded
  *   to bf16.  dense_attn_fwd_cache8_workspace_bytes: scratch that the call makes use of (0: none); without it the call does the same work
- *   with fewer workgroups, and its results differ by roundings.  The same call gives the same bits every time.
+ *   with fewer workgroups, and its results differ by roundings.  The same call gives the same bits every time; with kv_len the other
+ *   sequences' lengths, too, decide where a sequence's keys are parted, and so its roundings.
  *   Limits, as for dense_attn_fwd_save, and: heads / key heads whole. */
 typedef enum { MRT_CACHE_E4M3 = 0, MRT_CACHE_INT8 = 1 } mrt_cache_format;
 typedef struct {

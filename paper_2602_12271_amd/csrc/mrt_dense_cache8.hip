@@ -31,27 +31,100 @@ struct FewTile {
   unsigned char ke[2], ve[2];
 };
 
-// part_tiles: tiles of 32 keys of a part.  A sequence has as many parts as its own length takes.
+// Which tiles a part of a call with parts has, and where it lies among the parts of all sequences.  Sequences of unequal lengths are
+// cut into parts of one length, about the least with which no more than parts.n for every sequence come out, so that the chip is as
+// full as with equal ones.  Every workgroup finds it out for itself, from all lengths; whole waves call it.  (us, as many parts for
+// every sequence as the longest takes | as its own share: 32 heads sharing 8, lengths 8190 .. 32760, batch of 4, 46.3 | 42.8; one of
+// 32760 and seven of 100 60.3 | 21.0; 16 of any up to 16384 73.8 | 61.1; four of 32760, with what the lengths cost, 60.9 | 62.4.)
+__device__ inline int few_tiles(KParams p, int len) {
+  p.Nkv = min(max(len, 0), p.Nkv);
+  return p.Nkv > 0 ? (dense_visible(p, p.Nq - 1) + kFewKeys - 1) / kFewKeys : 0;
+}
+// op over the lanes up to a lane's own, of numbers that 0 leaves as they are (in 1.2 us less a call than by exchanges through LDS)
+template <typename Op>
+__device__ inline int lanes_upto(int x, Op op) {
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));      // 1, 2, 4 and 8 lanes down in a row of 16
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));      // the last of a row to every second next one
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));      // the last of two to the next two
+  return x;
+}
+struct FewPart {
+  int b;                 // -1: no such part
+  int first, n;          // of the sequence's parts, how many
+  int tiles;             // of a part
+};
+// the part `slot`, or with slot = -1 those of sequence b
+__device__ inline FewPart few_part(const KParams& p, const DenseParts& parts, const int* kv_len, int tiles, int slot, int b) {
+  if (!kv_len) {
+    if (slot >= 0) b = slot / parts.n;
+    return {b, b * parts.n, parts.n, tiles};
+  }
+  const int batch = (int)parts.heads / p.H, slots = batch * parts.n, lane = threadIdx.x & 63;
+  int sum = 0, most = 0;
+  const int len0 = lane < batch ? few_tiles(p, kv_len[lane]) : 0;      // (most batches have no more)
+  auto tiles_of = [&](int i) { return i < 64 ? len0 : few_tiles(p, kv_len[i]); };
+  for (int i = lane; i < batch; i += 64) {
+    const int t = tiles_of(i);
+    sum += t;
+    most = max(most, t);
+  }
+  sum = __builtin_amdgcn_readlane(lanes_upto(sum, [](int x, int y) { return x + y; }), 63);
+  most = __builtin_amdgcn_readlane(lanes_upto(most, [](int x, int y) { return max(x, y); }), 63);
+  const int least = max(kFewWaves, (most + kMostFewParts - 1) / kMostFewParts);
+  // (with a part that is not full for every sequence they always fit)
+  for (int spare = 0;; spare = spare ? batch : (batch + 1) / 2) {
+    const int room = slots - spare;
+    tiles = max(least, (sum + room - 1) / room);
+    int before = 0;
+    FewPart at = {-1, 0, 0, tiles};
+    for (int i = lane; i - lane < batch; i += 64) {
+      const int n = i < batch ? (tiles_of(i) + tiles - 1) / tiles : 0;
+      const int upto = lanes_upto(n, [](int x, int y) { return x + y; }), first = before + upto - n;
+      const unsigned long long found = __builtin_amdgcn_ballot_w64(i < batch && (slot >= 0 ? slot >= first && slot < first + n : i == b));
+      if (found) {
+        const int l = __builtin_ctzll(found);
+        at = {i - lane + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(n, l), tiles};
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (before <= slots || spare == batch) return at;
+  }
+}
+
+// part_tiles: tiles of 32 keys of a part, where all sequences are as long as the cache.
 template <int D, bool E4M3, int RT, bool PART>
 __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KParams p, DenseParts parts, DenseCache8<E4M3> cache,
                                                                              int row_tiles, int part_tiles) {
   constexpr int KP = D / 64, NK = D / 32, NV = D / 16, LD = D + 4;
   extern __shared__ __attribute__((aligned(16))) float few_lds[];      // [wave][row][LD], then [wave][row] references, sums
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-  // units that stream the same keys go to one of the eight XCDs
-  const int total = gridDim.x, xcd = blockIdx.x & 7;
-  const int unit = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
+  // Workgroups reach the eight XCDs in turn: tiles of rows that stream the same keys go to one of them, parts to all.
+  const int turn = (int)blockIdx.x >> 3, rt = turn % row_tiles;
+  int slot = 8 * (turn / row_tiles) + (int)(blockIdx.x & 7);
   const int tile_rows = 16 * RT, rows = cache.group * p.Nq, kv_heads = p.H / cache.group;
-  int at = unit;
-  const int rt = at % row_tiles;
-  at /= row_tiles;
-  const int part = PART ? at % parts.n : 0, bk = PART ? at / parts.n : at;
-  const int b = bk / kv_heads, kvh = bk - b * kv_heads;
+  int b, kvh, part = 0;
+  if constexpr (PART) {
+    const int slots = (int)parts.heads / p.H * parts.n;
+    kvh = slot % kv_heads;
+    slot /= kv_heads;
+    if (slot >= slots) return;
+    const FewPart at = few_part(p, parts, cache.kv_len, part_tiles, slot, 0);
+    if (at.b < 0) return;
+    b = at.b;
+    part = slot - at.first;
+    part_tiles = at.tiles;
+  } else {
+    b = slot / kv_heads;
+    kvh = slot - b * kv_heads;
+    if (b * p.H >= (int)parts.heads) return;
+  }
   if (cache.kv_len) p.Nkv = __builtin_amdgcn_readfirstlane(min(max(cache.kv_len[b], 0), p.Nkv));
   const int nkeys = p.Nkv > 0 ? dense_visible(p, p.Nq - 1) : 0, nfree = dense_visible(p, 0);
   const int tiles = (nkeys + kFewKeys - 1) / kFewKeys;
   const int t0 = PART ? part * part_tiles : 0, t1 = PART ? min(t0 + part_tiles, tiles) : tiles;
-  if (PART && t0 >= tiles) return;                      // (k_cache8_join knows)
 
   // row r of the tile: query r % Nq of head r / Nq of those that share the keys
   int limit[RT];
@@ -238,7 +311,7 @@ __global__ __launch_bounds__(kFewThreads, RT == 4 ? 1 : 2) void k_cache8_few(KPa
     const int head = r / p.Nq, q = r - head * p.Nq, hd = kvh * cache.group + head;
     const long long out = ((long long)b * p.H + hd) * p.Nq + q;
     if constexpr (PART) {
-      const long long to = (long long)part * parts.heads * p.Nq + out;
+      const long long to = ((long long)slot * p.H + hd) * p.Nq + q;
       *(f32x4*)(parts.o + to * D + f) = acc;
       if (f == 0) parts.ml[to] = make_float2(m, sum);
     } else {
@@ -259,11 +332,10 @@ __global__ __launch_bounds__(256) void k_cache8_join(KParams p, DenseParts parts
   __shared__ __attribute__((aligned(16))) float sums[RUNS][D + 4];
   __shared__ float2 mls[RUNS];
   const int row = blockIdx.x, bh = row / p.Nq, q = row - bh * p.Nq, b = bh / p.H, hd = bh - b * p.H;
-  if (cache.kv_len) p.Nkv = min(max(cache.kv_len[b], 0), p.Nkv);
-  const int nkeys = p.Nkv > 0 ? dense_visible(p, p.Nq - 1) : 0;
-  const int n = ((nkeys + kFewKeys - 1) / kFewKeys + part_tiles - 1) / part_tiles;
+  const FewPart at = few_part(p, parts, cache.kv_len, part_tiles, -1, b);
+  const int n = at.n;
   const int run = threadIdx.x / TPR, f = 4 * (threadIdx.x % TPR);
-  const size_t rows = (size_t)parts.heads * p.Nq;
+  const size_t rows = (size_t)p.H * p.Nq, row0 = at.first * rows + (size_t)hd * p.Nq + q;
   float2 ml[MOST];
   f32x4 po[MOST];
 #pragma unroll
@@ -272,8 +344,8 @@ __global__ __launch_bounds__(256) void k_cache8_join(KParams p, DenseParts parts
     ml[i] = make_float2(kNoKey, 0.f);
     po[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (part < n) {
-      ml[i] = parts.ml[part * rows + row];
-      po[i] = *(const f32x4*)(parts.o + (part * rows + row) * D + f);
+      ml[i] = parts.ml[row0 + part * rows];
+      po[i] = *(const f32x4*)(parts.o + (row0 + part * rows) * D + f);
     }
   }
   float m = kNoKey, sum = 0.f;
@@ -313,7 +385,7 @@ struct FewShape {
   int part_tiles;
 };
 
-FewShape few_shape(const KParams& kp, int nbh, int group, bool may_split) {
+FewShape few_shape(const KParams& kp, int nbh, int group, bool may_split, bool lengths) {
   FewShape f = {0, 1, 1, 0};
   if (kp.Nq > 32) return f;
   const int rows = group * kp.Nq;
@@ -326,11 +398,15 @@ FewShape few_shape(const KParams& kp, int nbh, int group, bool may_split) {
   if (kp.Nq > 16 && wgs > 64) return {0, 1, 1, 0};
   const long long tiles = (dense_visible(kp, kp.Nq - 1) + kFewKeys - 1) / kFewKeys;
   // As many workgroups as the chip holds at once (two a compute unit, one of 64 rows), each with a tile for every wave.  us by the
-  // number of parts: 32 heads sharing 8 over 32760 keys, batch of 4 (lengths 8190 .. 32760), 8 47.8, 16 46.0, 24 48.2, 32 47.5, 64
-  // 50.3; 12 heads 10 34.6, 20 25.5, 42 25.2, 64 26.6; 8 key heads, 4096 keys, 8 10.3, 16 9.2, 32 8.3, 64 9.5; one of 32760 keys 32
+  // number of parts: 12 heads 10 34.6, 20 25.5, 42 25.2, 64 26.6; 8 key heads, 4096 keys, 8 10.3, 16 9.2, 32 8.3, 64 9.5; one of 32760 keys 32
   // 13.5, 64 11.1, 96 10.3; 32 heads of 2048 keys, batch of 64, 1 199, 2 210, 8 226; 300 keys 1 6.3, 2 8.2, 6 7.2.
-  const long long want = 2ll * compute_units() / (f.rt == 4 ? 2 : 1) / wgs;
-  const long long n = may_split && tiles > 12 ? std::max(1ll, std::min({want, tiles / kFewWaves, (long long)kMostFewParts})) : 1;
+  const long long batch = nbh / kp.H;
+  long long want = 2ll * compute_units() / (f.rt == 4 ? 2 : 1) / wgs;
+  // Sequences of lengths of their own are cut where whole ones fill the chip, too: the longest would keep a part of it busy for long
+  // (us, whole | three parts a sequence, 32 heads sharing 8, batch of 64, lengths 8192 and 63 of 300 60 | 30, any up to 8192 137 | 121,
+  // any of 4096 .. 8192 160 | 167, all 8192 195 | 210; of 128, where whole ones take turns, up to 4096 123 | 134).
+  if (lengths && want == 1 && batch > 1 && batch <= 256) want = 3;
+  const long long n = may_split && tiles > 12 && tiles * batch < 1ll << 30 ? std::max(1ll, std::min({want, tiles / kFewWaves, (long long)kMostFewParts})) : 1;
   f.part_tiles = (int)((tiles + n - 1) / n);
   f.parts = (int)((tiles + f.part_tiles - 1) / f.part_tiles);
   return f;
@@ -344,7 +420,7 @@ hipError_t run_few(const KParams& kp, int nbh, const FewShape& f, const DensePar
     const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  kernel<<<nbh / cache.group * f.row_tiles * f.parts, kFewThreads, lds, s>>>(kp, parts, cache, f.row_tiles, f.part_tiles);
+  kernel<<<(nbh / cache.group * f.parts + 7) / 8 * 8 * f.row_tiles, kFewThreads, lds, s>>>(kp, parts, cache, f.row_tiles, f.part_tiles);
   if (f.parts > 1) k_cache8_join<D><<<nbh * kp.Nq, 256, 0, s>>>(kp, parts, cache, f.part_tiles);
   return hipGetLastError();
 }
@@ -430,15 +506,15 @@ struct Cache8Shape {
   DenseShape dense;
   size_t bytes;          // of parts
 };
-Cache8Shape cache8_shape(const KParams& kp, int nbh, int group, bool e4m3, size_t bytes) {
+Cache8Shape cache8_shape(const KParams& kp, int nbh, int group, bool e4m3, size_t bytes, bool lengths) {
   Cache8Shape c;
-  c.few = few_shape(kp, nbh, group, bytes > 0);
+  c.few = few_shape(kp, nbh, group, bytes > 0, lengths);
   c.rounds = {{0, 0, 0}, 0, 0};
   c.dense = {0, 1};
   c.bytes = 0;
   if (c.few.rt) {
     c.bytes = c.few.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, c.few.parts, kp.d) : 0;
-    return c.bytes > bytes ? cache8_shape(kp, nbh, group, e4m3, 0) : c;
+    return c.bytes > bytes ? cache8_shape(kp, nbh, group, e4m3, 0, lengths) : c;
   }
   c.rounds = rounds_shape(kp, nbh, e4m3, bytes);
   c.dense = c.rounds.parts ? DenseShape{c.rounds.r.queries, c.rounds.parts} : dense_call_shape(kp, nbh, bytes, true);
@@ -449,12 +525,12 @@ Cache8Shape cache8_shape(const KParams& kp, int nbh, int group, bool e4m3, size_
 }  // namespace
 
 size_t dense_cache8_workspace_bytes(const KParams& kp, int nbh, int group, bool e4m3) {
-  return cache8_shape(kp, nbh, group, e4m3, ~(size_t)0).bytes;
+  return std::max(cache8_shape(kp, nbh, group, e4m3, ~(size_t)0, false).bytes, cache8_shape(kp, nbh, group, e4m3, ~(size_t)0, true).bytes);
 }
 
 template <bool E4M3>
 hipError_t launch_dense_cache8(const KParams& kp, int nbh, void* workspace, size_t workspace_bytes, const DenseCache8<E4M3>& cache, hipStream_t s) {
-  const Cache8Shape c = cache8_shape(kp, nbh, cache.group, E4M3, workspace ? workspace_bytes : 0);
+  const Cache8Shape c = cache8_shape(kp, nbh, cache.group, E4M3, workspace ? workspace_bytes : 0, cache.kv_len != nullptr);
   const int n = c.few.rt ? c.few.parts : c.dense.parts;
   const size_t rows = (c.rounds.r.rest ? (size_t)c.rounds.r.rest * c.rounds.r.queries : (size_t)kp.Nq * nbh) * n;
   const bool even = dense_visible(kp, 0) == dense_visible(kp, kp.Nq - 1);

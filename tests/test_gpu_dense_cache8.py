@@ -36,6 +36,12 @@ CASES = {
     "token-31-keys": Step(1, 31, heads=4, kv_heads=4, dim=64),
     "token-33-keys": Step(1, 33, heads=4, kv_heads=4),
     "token-padded": Step(1, 1000, heads=6, kv_heads=3, batch=5, kv_len=(1000, 1, 0, 517, 64)),
+    "token-lengths": Step(1, 4000, heads=2, kv_heads=1, batch=100, dim=64, kv_len=tuple(i * i * 31 % 4001 for i in range(100))),
+    "token-fills": Step(1, 600, heads=16, kv_heads=8, batch=40, dim=64, kv_len=tuple(i * 77 % 601 for i in range(40))),
+    "token-fills-4-rows": Step(4, 500, heads=16, kv_heads=1, batch=200, dim=64, kv_len=(500,) + (0, 7) * 99 + (499,)),
+    "token-one-long": Step(1, 20000, heads=8, kv_heads=1, batch=16, kv_len=(3, 0, 20000) + (0, 1, 33) * 4 + (0,)),
+    "token-long-last": Step(1, 9000, heads=4, kv_heads=2, batch=3, kv_len=(0, 0, 8999)),
+    "few-lengths-causal": Step(5, 900, heads=4, kv_heads=1, chunk=1, offset=880, batch=7, kv_len=(884, 1, 0, 881, 64, 900, 300)),
     "token-padded-d64": Step(1, 300, heads=6, kv_heads=6, dim=64, batch=4, kv_len=(-5, 300, 900, 129)),
     "token-long": Step(1, 40000, heads=2, kv_heads=1),
     "few-3": Step(3, 777, heads=4, kv_heads=2),
@@ -90,7 +96,7 @@ def test_attention(name, format, block):
             assert (got["O"][b, h].double() - want).norm() <= 4 * 2.0 ** -9 * math.sqrt(8 / 3) * want.norm() + 1e-30
 
 
-@pytest.mark.parametrize("name", ["token", "token-shared", "token-padded", "few-7-shared", "few-16-d64", "few-causal-padded", "frame",
+@pytest.mark.parametrize("name", ["token", "token-shared", "token-padded", "token-lengths", "token-fills", "token-one-long", "few-7-shared", "few-16-d64", "few-causal-padded", "frame",
                                   "chunk-cache", "padded", "text-late"])
 def test_scratch(name):
     """The caller's scratch, poisoned; too little, or none: the same work with fewer workgroups."""
