@@ -274,3 +274,21 @@ def test_far_addresses():
     want, got = pkg.cache8_read(near, n), pkg.cache8_read(cache, n)
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+def test_long_run(format):
+    """More rows than workgroups take in one round."""
+    n, block = 150001, 32
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    cache = pkg.cache8(1, 1, n, 128, format=format, block=block)
+    new = [torch.randn(1, 1, n, 128, generator=gen, device="cuda").bfloat16() for _ in range(2)]
+    pkg.cache8_write(cache, *new)
+    got = pkg.cache8_read(cache, n)
+    for codes, powers, x, values in ((cache.K, cache.K_scale, new[0], got[0]), (cache.V, cache.V_scale, new[1], got[1])):
+        # (from the bits: torch.ldexp of a tensor of exponents goes through pow, which is off by 2^-53 of 2^-4 on the device)
+        scale = (powers.int() << 23).view(torch.float32).double().repeat_interleave(block, 2)[:, :, :n, None]
+        assert torch.equal(values.double(), codes.double() * scale)
+        # half a step of the code: 2^-4 of the value, or half the smallest step of the scale; half the scale
+        bound = (x.double().abs() * 2.0 ** -4).clamp(min=2.0 ** -10 * scale) if format == "e4m3" else 0.5 * scale
+        assert ((values.double() - x.double()).abs() <= bound).all()
