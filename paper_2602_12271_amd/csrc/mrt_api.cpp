@@ -1381,6 +1381,7 @@ mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, fl
     cache.ve_batch = c->v_scale_batch; cache.ve_head = c->v_scale_head;
     cache.shift = shift;
     cache.rounds = DenseRounds{0, 0, 0};
+    cache.by_length = 0;
     return launch_dense_cache8(kp, BH, workspace, workspace_bytes, cache, s);
   };
   const hipError_t e = timed_launch(s, MRT_KERNEL_DENSE, [&] {

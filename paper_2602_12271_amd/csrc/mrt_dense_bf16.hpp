@@ -179,6 +179,27 @@ __global__ __launch_bounds__(kDenseThreads, D == 64 ? 4 : 2) void k_bf16_dense(K
       bh = unit / nx;
       q0 = (unit - bh * nx) * WGQ;
     }
+  // CODES, sequences of lengths of their own: the longest one's tiles go first, or they are the last to end, and every sequence's go to
+  // all XCDs, each a run of them, or some have the longest one alone (us, as they come | so: 12 heads, 4680 queries of 14040, 9360,
+  // 4680 and 0 keys 1485 | 766, of 14040 and 7000 739 | 567, of two times 32760 1698 | 1706; parted, 8 heads, 780 queries of 9360
+  // and 300 84.7 | 82.0)
+  if constexpr (CODES)
+    if (save.by_length > 0) {
+      const int units = nx * p.H * (PART ? parts.n : 1), rank = blockIdx.x / units, at = blockIdx.x - rank * units;
+      const int len = lane < save.by_length ? min(max(save.kv_len[lane], 0), p.Nkv) : -1;
+      int before = 0;
+      for (int i = 0; i < save.by_length; ++i) {
+        const int other = __builtin_amdgcn_readlane(len, i);
+        before += other > len || (other == len && i < lane);
+      }
+      const int seq = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < save.by_length && before == rank));
+      const int unit = (at & 7) * (units >> 3) + ((at & 7) < (units & 7) ? (at & 7) : (units & 7)) + (at >> 3);
+      run = unit / nx;
+      q0 = (unit - run * nx) * WGQ;
+      const int head = PART ? run / parts.n : run;
+      if constexpr (PART) part = run - head * parts.n;
+      bh = seq * p.H + head;
+    }
   const int b = bh / p.H, hd = bh - b * p.H;
   int kvh = hd;
   const int qw0 = q0 + 16 * QT * wq;                      // this wave's first query

@@ -537,7 +537,10 @@ hipError_t launch_dense_cache8(const KParams& kp, int nbh, void* workspace, size
   const DenseParts parts = {(float*)workspace, (float2*)((float*)workspace + rows * kp.d), n, (unsigned)nbh, even ? 0u : (unsigned)nbh * n};
   if (c.few.rt) return kp.d == 128 ? run_few_d<128>(kp, nbh, c.few, parts, cache, s) : run_few_d<64>(kp, nbh, c.few, parts, cache, s);
   if (c.rounds.r.rest) return run_rounds(kp, nbh, c.rounds, parts, cache, s);
-  return run_dense_shape(kp, nbh, c.dense, parts, cache, s);
+  DenseCache8<E4M3> ordered = cache;
+  const int batch = nbh / kp.H;
+  if (cache.kv_len && batch > 1 && batch <= 64 && even) ordered.by_length = batch;
+  return run_dense_shape(kp, nbh, c.dense, parts, ordered, s);
 }
 template hipError_t launch_dense_cache8<true>(const KParams&, int, void*, size_t, const DenseCache8<true>&, hipStream_t);
 template hipError_t launch_dense_cache8<false>(const KParams&, int, void*, size_t, const DenseCache8<false>&, hipStream_t);

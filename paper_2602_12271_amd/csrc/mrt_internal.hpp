@@ -138,6 +138,7 @@ template <bool E4M3> struct DenseCache8 : DenseSave {
   long long ke_batch, ke_head, ve_batch, ve_head; // their strides
   int shift;                                      // log2 of the tokens of a block
   DenseRounds rounds;                             // rest = 0: not such a call
+  int by_length;                                  // sequences in the order of their lengths: how many there are (else 0)
 };
 
 struct Plan {

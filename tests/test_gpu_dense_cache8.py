@@ -67,6 +67,10 @@ CASES = {
     "text-late": Step(150, 900, heads=2, chunk=1, offset=740),
     "padded": Step(300, 300, batch=3, heads=2, kv_len=(300, 33, 0)),
     "padded-d64": Step(90, 450, batch=4, heads=4, kv_heads=2, dim=64, kv_len=(450, 449, 64, 1)),
+    "padded-by-length": Step(700, 700, heads=12, kv_heads=4, batch=5, kv_len=(699, 64, 0, 700, 700)),
+    "padded-by-length-d64": Step(2, 2, 17, 23, heads=10, batch=6, dim=64, kv_len=(1, 0, 782, 500, 781, 65)),
+    "padded-64": Step(40, 200, heads=2, batch=64, kv_len=tuple(i * 37 % 201 for i in range(64))),
+    "padded-65": Step(40, 200, heads=2, batch=65, kv_len=tuple(i * 37 % 201 for i in range(65))),
     "padded-causal": Step(200, 200, batch=2, heads=1, chunk=1, kv_len=(190, 30)),
     "many-heads": Step(260, 520, heads=48, kv_heads=6, batch=2),
     "tokens-outside": Step(70, 140, heads=4, layout="bnhd"),
@@ -97,7 +101,7 @@ def test_attention(name, format, block):
 
 
 @pytest.mark.parametrize("name", ["token", "token-shared", "token-padded", "token-lengths", "token-fills", "token-one-long", "few-7-shared", "few-16-d64", "few-causal-padded", "frame",
-                                  "chunk-cache", "padded", "text-late"])
+                                  "chunk-cache", "padded", "padded-by-length", "padded-by-length-d64", "padded-64", "text-late"])
 def test_scratch(name):
     """The caller's scratch, poisoned; too little, or none: the same work with fewer workgroups."""
     c = CASES[name]
