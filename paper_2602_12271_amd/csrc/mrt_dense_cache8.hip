@@ -440,12 +440,16 @@ hipError_t run_few_d(const KParams& kp, int nbh, const FewShape& f, const DenseP
 // 4680 of 14040, 256 whole rounds and 48 tiles shared by five 494 | 491, by four 505 | 507, all shared by three 568, one by one
 // 755 | 766.  (Two workgroups of unequal length for every tile of one incomplete round, so that units without a tile take the shorter
 // ones by turns, measured 894 us where one by one takes 856: 228 tiles of 512 steps.)
+// Where sequences have lengths of their own the host does not know them: 128 features, a third of what equal ones would take and two
+// thirds of what is left if half the work is missing and the rest in pieces of the longest one (us, as equal ones | so: 12 heads of
+// 1560 queries, batch of 4, keys 32760, 20000, 9000, 3000 904 | 640 .. 680, all 32760 1276 | 1337; 8 heads of 780 queries of 9360 and 300
+// keys 82 | 72; 4 heads of 576 of 4680, 100, 1000, 200 50 | 45.  64 features gained nothing).
 struct RoundsShape {
   DenseRounds r;         // rest = 0: no tiles of their own kind
   int parts;             // 0: no call of this kind
   size_t bytes;
 };
-RoundsShape rounds_shape(const KParams& kp, int nbh, bool e4m3, size_t most_bytes) {
+RoundsShape rounds_shape(const KParams& kp, int nbh, bool e4m3, size_t most_bytes, bool lengths) {
   RoundsShape best = {{0, 0, 0}, 0, 0};
   if (dense_visible(kp, 0) != dense_visible(kp, kp.Nq - 1)) return best;
   const bool wide = kp.d == 128;
@@ -466,6 +470,10 @@ RoundsShape rounds_shape(const KParams& kp, int nbh, bool e4m3, size_t most_byte
       const size_t bytes = parts > 1 ? dense_parts_bytes(rest == units ? kp.Nq * nbh : (int)rest * queries, parts, kp.d) : 0;
       if (bytes > most_bytes || bytes > kMostRoundsBytes) return;
       double us = time(units - rest, steps, parts > 1) + time(rest * parts, (steps + parts - 1) / parts, parts > 1);
+      if (lengths && wide && rest == units) {
+        const double piece = time(1, (steps + parts - 1) / parts, parts > 1);
+        us = (us + 2 * std::max(piece, 0.5 * piece * units * parts / slots)) / 3;
+      }
       if (parts > 1) us = 1.03 * (us + (wide ? 5.5 : 4.0) + 2 * bytes / 5.0e6);       // (it has to promise something)
       if (least > 0 && us >= least) return;
       least = us;
@@ -516,7 +524,7 @@ Cache8Shape cache8_shape(const KParams& kp, int nbh, int group, bool e4m3, size_
     c.bytes = c.few.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, c.few.parts, kp.d) : 0;
     return c.bytes > bytes ? cache8_shape(kp, nbh, group, e4m3, 0, lengths) : c;
   }
-  c.rounds = rounds_shape(kp, nbh, e4m3, bytes);
+  c.rounds = rounds_shape(kp, nbh, e4m3, bytes, lengths && nbh > kp.H && nbh / kp.H <= 64);
   c.dense = c.rounds.parts ? DenseShape{c.rounds.r.queries, c.rounds.parts} : dense_call_shape(kp, nbh, bytes, true);
   c.bytes = c.rounds.r.rest ? c.rounds.bytes : c.dense.parts > 1 ? dense_parts_bytes(kp.Nq * nbh, c.dense.parts, kp.d) : 0;
   return c;

@@ -69,6 +69,7 @@ CASES = {
     "padded-d64": Step(90, 450, batch=4, heads=4, kv_heads=2, dim=64, kv_len=(450, 449, 64, 1)),
     "padded-by-length": Step(700, 700, heads=12, kv_heads=4, batch=5, kv_len=(699, 64, 0, 700, 700)),
     "padded-by-length-d64": Step(2, 2, 17, 23, heads=10, batch=6, dim=64, kv_len=(1, 0, 782, 500, 781, 65)),
+    "padded-shared": Step(390, 1500, heads=4, kv_heads=2, batch=4, kv_len=(1500, 40, 0, 700)),
     "padded-64": Step(40, 200, heads=2, batch=64, kv_len=tuple(i * 37 % 201 for i in range(64))),
     "padded-65": Step(40, 200, heads=2, batch=65, kv_len=tuple(i * 37 % 201 for i in range(65))),
     "padded-causal": Step(200, 200, batch=2, heads=1, chunk=1, kv_len=(190, 30)),
