@@ -5,7 +5,7 @@
 // magnitude, and stores codes.  The scale is the smallest power of two that brings that magnitude to the largest code, found
 // from its bits; codes are the nearest, ties to even, of a product with a power of two, which is exact.  Both calls move
 // every byte once and are bound by memory: 12 heads of 4680 tokens, e4m3, written in 11.7 us (28.8 MB read, 14.4 written) and read
-// in 9.9; 28080 of them in whole numbers read in 53 (258 MB, 4.9 TB/s).
+// in 9.9; 32760 of them in whole numbers read in 52 (101 MB read, 201 written).
 #include "mrt_cache8.hpp"
 
 #include <algorithm>
@@ -19,7 +19,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int kThreadsCache = 256, kItem = 16;       // codes of an access
-// Workgroups along a head's rows: one access a thread up to long runs (28080 rows of 12 heads and their 4680 new ones, whole numbers,
+// Workgroups along a head's rows: one access a thread up to long runs (4680 rows of 12 heads written, 32760 read, whole numbers,
 // by the most: 4096 68 us, 512 74, 256 79, 64 85).
 constexpr unsigned kMostReadWgs = 4096;
 

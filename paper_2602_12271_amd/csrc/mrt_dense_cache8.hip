@@ -8,7 +8,8 @@
 // first product wants them, 16 contiguous features; of the values it loads D / 16 features of the 8 keys whose weights it
 // will hold (rows 4g .. 4g + 3 of the two tiles of 16, as the first product leaves them), so that no weight changes lanes, and
 // brings pairs of keys of one feature together in registers.  No LDS and no barrier until the four waves of a workgroup join
-// their sums at the end; `parts` workgroups share the keys, and a second launch joins theirs.
+// their sums at the end; `parts` workgroups share the keys, and a second launch joins theirs.  Memory bounds it: one token of 32
+// heads sharing 8, four sequences of 8190 .. 32760 keys, 168 MB, in 34.9 us and 4.1 for the join.
 #include "mrt_dense_bf16.hpp"
 
 #include <algorithm>

