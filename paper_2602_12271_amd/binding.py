@@ -762,11 +762,19 @@ def _own_rows(weight):
     return weight.contiguous() if weight is not None and weight.dim() == 2 and 0 <= weight.stride(0) < weight.shape[1] else weight
 
 
-def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder, positions):
-    """x, y, dx: the norm's input, its result (or the gradient of that) and the gradient of x, of one or two tensors."""
-    key = [f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, None if split is None else tuple(split), layout, ladder, len(x)]
-    for t in (*x, *y, *dx, *weights, *positions):
-        key += (None,) if t is None else (t.shape, t.stride(), t.dtype)
+def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split, layout, ladder, positions,
+                  given=None):
+    """x, y, dx: the norm's input, its result (or the gradient of that) and the gradient of x, of one or two tensors.  given: None,
+    or those of y and dx whose layout does not follow from x (the others come from empty_like), behind the type asked of that."""
+    if given is None:
+        given = (None, *y, *dx)
+    key = [f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, None if split is None else tuple(split), layout, ladder, len(x), len(dx),
+           given[0]]
+    for t in (*x, *weights, *positions, *given[1:]):
+        if t is None:
+            key.append(None)
+        else:
+            key += (t.shape, t.stride(), t.dtype)
     key = tuple(key)
     found = _norm_problems.get(key)
     if found is not None:
@@ -798,13 +806,14 @@ def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_o
 def _norm_tensors(tensors, weights, positions, dweights=()):
     """The description with the call's addresses (one that is shared is not written)."""
     tensors = type(tensors).from_buffer_copy(tensors)
-    for i, t in enumerate(tensors):
-        if weights[i] is not None:
-            t.weight = weights[i].data_ptr()
-        if positions[i] is not None:
-            t.t.positions = positions[i].data_ptr()
-        if dweights and dweights[i] is not None:
-            t.dweight = dweights[i].data_ptr()
+    for t, weight, position in zip(tensors, weights, positions):
+        if weight is not None:
+            t.weight = weight.data_ptr()
+        if position is not None:
+            t.t.positions = position.data_ptr()
+    for t, dweight in zip(tensors, dweights):
+        if dweight is not None:
+            t.dweight = dweight.data_ptr()
     return tensors
 
 
@@ -832,7 +841,7 @@ def norm_rotary_fwd(Q, K=None, q_weight=None, k_weight=None, *, eps=1e-6, f_q=No
             y.append(torch.empty_like(K, dtype=dtype) if k_out is None else k_out)
         weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
         r, tensors, pointers = _norm_problem(x, y, (), weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
-                                             layout, ladder, positions)
+                                             layout, ladder, positions, (dtype, out, k_out))
         tensors = _norm_tensors(tensors, weights, positions)
         st = lib.mrt_norm_rotary_fwd(ctypes.byref(r), eps, tensors, len(x), pointers(*[t.data_ptr() for t in x]),
                                      pointers(*[t.data_ptr() for t in y]), s)
@@ -865,7 +874,7 @@ def norm_rotary_bwd(Q, K, q_weight, k_weight, dQ, dK=None, *, eps=1e-6, f_q=None
             dx.append(torch.empty_like(K) if k_out is None else k_out)
         weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
         r, tensors, pointers = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
-                                             layout, ladder, positions)
+                                             layout, ladder, positions, (None, *g, out, k_out))
         dw = [None if u is None else Q.new_empty(u.shape, dtype=torch.float32) for u in weights]
         tensors = _norm_tensors(tensors, weights, positions, dw)
         nbytes = lib.mrt_norm_rotary_bwd_workspace_bytes(ctypes.byref(r), tensors, len(x))
@@ -936,10 +945,11 @@ def _cache8_of(c):
 _rows: dict = {}
 
 
-def _cache8_rows(cache, K, V, at, lengths):
+def _cache8_rows(cache, K, V, at, lengths, given=True):
+    """given: K and V may have any layout; else they are contiguous, of the cache's shape but for their number of rows."""
     number = type(at) is int
-    key = (cache.K.shape, K.shape, K.stride(), K.dtype, V.shape, V.stride(), V.dtype, number or (at.dtype, at.shape, at.stride()),
-           lengths is None or (lengths.dtype, lengths.shape, lengths.stride()))
+    key = (cache.K.shape, (K.shape, K.stride(), K.dtype, V.shape, V.stride(), V.dtype) if given else (K.shape[2], K.dtype),
+           number or (at.dtype, at.shape, at.stride()), lengths is None or (lengths.dtype, lengths.shape, lengths.stride()))
     found = _rows.get(key)
     if found is None:
         import torch
@@ -1000,9 +1010,10 @@ def cache8_read(cache, tokens, *, at=0, dtype=None, out=None, v_out=None, stream
     def call(s):
         B, H, _, d = cache.K.shape
         given = dtype if dtype is not None else out.dtype if out is not None else v_out.dtype if v_out is not None else torch.bfloat16
-        K, V = [cache.K.new_empty((B, H, tokens, d), dtype=given) if y is None else y for y in (out, v_out)]
+        K = torch.empty(B, H, tokens, d, dtype=given, device=cache.K.device) if out is None else out
+        V = v_out if v_out is not None else torch.empty_like(K) if out is None else cache.K.new_empty((B, H, tokens, d), dtype=given)
         _require(K.shape[2] == tokens, f"the output has {K.shape[2]} tokens, not {tokens}")
-        c, rows = _cache8_of(cache), _cache8_rows(cache, K, V, at, None)
+        c, rows = _cache8_of(cache), _cache8_rows(cache, K, V, at, None, out is not None or v_out is not None)
         st = lib.mrt_cache8_read(ctypes.byref(c), ctypes.byref(rows), K.data_ptr(), V.data_ptr(), s)
         if st != MRT_OK:
             _raise(lib, st)
