@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import NamedTuple, Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -164,17 +165,18 @@ def load_library() -> ctypes.CDLL:
     N = ctypes.POINTER(MrtNormTensor)
     cd = ctypes.c_double
     lib.mrt_norm_rotary_check.argtypes = [R, cd, N, ci, ci]
-    lib.mrt_norm_rotary_fwd.argtypes = [R, cd, N, ci, vp, vp, vp]
-    lib.mrt_norm_rotary_bwd.argtypes = [R, cd, N, ci, vp, vp, vp, vp, sz, vp]
-    lib.mrt_norm_rotary_bwd_workspace_bytes.argtypes = [R, N, ci]
+    # (descriptions with a call's addresses are bytes that a struct.Struct has packed: 0.4 us where fields one by one take 1)
+    lib.mrt_norm_rotary_fwd.argtypes = [R, cd, vp, ci, vp, vp, vp]
+    lib.mrt_norm_rotary_bwd.argtypes = [R, cd, vp, ci, vp, vp, vp, vp, sz, vp]
+    lib.mrt_norm_rotary_bwd_workspace_bytes.argtypes = [R, vp, ci]
     lib.mrt_norm_rotary_bwd_workspace_bytes.restype = sz
     C, W = ctypes.POINTER(MrtCache8), ctypes.POINTER(MrtCache8Rows)
     lib.mrt_cache8_check.argtypes = [C, W]
-    lib.mrt_cache8_write.argtypes = lib.mrt_cache8_read.argtypes = [C, W, vp, vp, vp]
+    lib.mrt_cache8_write.argtypes = lib.mrt_cache8_read.argtypes = [vp, vp, vp, vp, vp]
     lib.dense_attn_cache8_check.argtypes = [P, C, ci]
-    lib.dense_attn_fwd_cache8_workspace_bytes.argtypes = [P, C, ci]
+    lib.dense_attn_fwd_cache8_workspace_bytes.argtypes = [P, vp, ci]
     lib.dense_attn_fwd_cache8_workspace_bytes.restype = sz
-    lib.dense_attn_fwd_cache8.argtypes = [vp, C, vp, vp, P, vp, ci, vp, sz, vp]
+    lib.dense_attn_fwd_cache8.argtypes = [vp, vp, vp, vp, P, vp, ci, vp, sz, vp]
     for f in (lib.mrt_norm_rotary_check, lib.mrt_norm_rotary_fwd, lib.mrt_norm_rotary_bwd, lib.mrt_cache8_check,
               lib.mrt_cache8_write, lib.mrt_cache8_read, lib.dense_attn_cache8_check, lib.dense_attn_fwd_cache8):
         f.restype = ci
@@ -744,8 +746,26 @@ def rotary_bwd(dQ, dK=None, *, f_q=None, f_kv=None, h=None, w=None, q_frame_offs
 
 
 # ---- norms of queries and keys with their rotary positions ---------------------------------------
-# (description, tensors without addresses) of recent calls by their values, like _problems
+# (description, tensors without addresses, how to fill these in, arrays of addresses) of recent calls by their values, like _problems
 _norm_problems: dict = {}
+
+
+def _packing(template, offsets):
+    """(pack, pieces): pieces of the template's bytes with places for addresses between them; pack(*pieces) joins them."""
+    raw, form, pieces, last = bytes(template), "=", [], 0
+    for offset in offsets:
+        form += f"{offset - last}sQ"
+        pieces += (raw[last:offset], 0)
+        last = offset + 8
+    pieces.append(raw[last:])
+    return struct.Struct(f"{form}{len(raw) - last}s").pack, pieces
+
+
+def _packed(packing, addresses):
+    pack, pieces = packing
+    pieces = pieces.copy()                       # (what is shared is not written)
+    pieces[1::2] = addresses
+    return pack(*pieces)
 
 
 def _norm_weight(weight, x, name):
@@ -796,25 +816,25 @@ def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_o
                      f"{name}: the gradient has its shape and type, head_dim contiguous")
             strides = MrtStrides(*dx[i].stride()[:3])
         tensors.append(MrtNormTensor(t, None, dtype, apart, strides, None))
-    found = r, (MrtNormTensor * len(x))(*tensors), ctypes.c_void_p * len(x)
+    array = (MrtNormTensor * len(x))(*tensors)
+    offsets = [i * ctypes.sizeof(MrtNormTensor) + at for i in range(len(x)) for at in _NORM_ADDRESSES]
+    found = r, array, _packing(array, offsets), struct.Struct(f"{len(x)}Q").pack
     if len(_norm_problems) >= _MAX_PROBLEMS:
         _norm_problems.clear()
     _norm_problems[key] = found
     return found
 
 
-def _norm_tensors(tensors, weights, positions, dweights=()):
-    """The description with the call's addresses (one that is shared is not written)."""
-    tensors = type(tensors).from_buffer_copy(tensors)
-    for t, weight, position in zip(tensors, weights, positions):
-        if weight is not None:
-            t.weight = weight.data_ptr()
-        if position is not None:
-            t.t.positions = position.data_ptr()
-    for t, dweight in zip(tensors, dweights):
-        if dweight is not None:
-            t.dweight = dweight.data_ptr()
-    return tensors
+_NORM_ADDRESSES = (MrtNormTensor.t.offset + MrtRotaryTensor.positions.offset, MrtNormTensor.weight.offset, MrtNormTensor.dweight.offset)
+
+
+def _norm_tensors(packing, x, weights, positions, dweights=(None, None)):
+    """The description with the call's addresses."""
+    addresses = []
+    for _, weight, position, dweight in zip(x, weights, positions, dweights):
+        addresses += (0 if position is None else position.data_ptr(), 0 if weight is None else weight.data_ptr(),
+                      0 if dweight is None else dweight.data_ptr())
+    return _packed(packing, addresses)
 
 
 def norm_rotary_fwd(Q, K=None, q_weight=None, k_weight=None, *, eps=1e-6, f_q=None, f_kv=None, h=None, w=None, q_frame_offset=0,
@@ -840,9 +860,9 @@ def norm_rotary_fwd(Q, K=None, q_weight=None, k_weight=None, *, eps=1e-6, f_q=No
             x.append(K)
             y.append(torch.empty_like(K, dtype=dtype) if k_out is None else k_out)
         weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
-        r, tensors, pointers = _norm_problem(x, y, (), weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
+        r, _, packing, pointers = _norm_problem(x, y, (), weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
                                              layout, ladder, positions, (dtype, out, k_out))
-        tensors = _norm_tensors(tensors, weights, positions)
+        tensors = _norm_tensors(packing, x, weights, positions)
         st = lib.mrt_norm_rotary_fwd(ctypes.byref(r), eps, tensors, len(x), pointers(*[t.data_ptr() for t in x]),
                                      pointers(*[t.data_ptr() for t in y]), s)
         if st != MRT_OK:
@@ -873,10 +893,10 @@ def norm_rotary_bwd(Q, K, q_weight, k_weight, dQ, dK=None, *, eps=1e-6, f_q=None
             g.append(dK)
             dx.append(torch.empty_like(K) if k_out is None else k_out)
         weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
-        r, tensors, pointers = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
+        r, _, packing, pointers = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
                                              layout, ladder, positions, (None, *g, out, k_out))
         dw = [None if u is None else Q.new_empty(u.shape, dtype=torch.float32) for u in weights]
-        tensors = _norm_tensors(tensors, weights, positions, dw)
+        tensors = _norm_tensors(packing, x, weights, positions, dw)
         nbytes = lib.mrt_norm_rotary_bwd_workspace_bytes(ctypes.byref(r), tensors, len(x))
         scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if workspace is None and nbytes else workspace
         ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
@@ -914,7 +934,11 @@ def cache8(batch, heads, capacity, head_dim, *, format="e4m3", block=64, device=
 _caches: dict = {}
 
 
-def _cache8_of(c):
+_CACHE_ADDRESSES = tuple(getattr(MrtCache8, name).offset for name in ("k_codes", "v_codes", "k_scales", "v_scales"))
+
+
+def _cache8_bytes(c):
+    """The C description of a cache."""
     key = (c.K.shape, c.K.stride(), c.K.dtype, c.V.shape, c.V.stride(), c.V.dtype, _layout_of(c.K_scale), _layout_of(c.V_scale), c.block,
            type(c.block))
     found = _caches.get(key)
@@ -930,19 +954,23 @@ def _cache8_of(c):
             _require(x.dtype == torch.uint8 and x.shape == (B, H, blocks) and (blocks == 1 or x.stride(2) == 1),
                      f"scales of the cache are uint8 [{B}, {H}, {blocks}], blocks contiguous")
         _require(c.K.stride(3) == 1 and c.V.stride(3) == 1, "head_dim must be contiguous")
-        found = MrtCache8(B, H, d, n, c.block, 0 if c.K.dtype == torch.float8_e4m3fn else 1, MrtStrides(*c.K.stride()[:3]),
-                          MrtStrides(*c.V.stride()[:3]), *c.K_scale.stride()[:2], *c.V_scale.stride()[:2])
+        found = _packing(MrtCache8(B, H, d, n, c.block, 0 if c.K.dtype == torch.float8_e4m3fn else 1, MrtStrides(*c.K.stride()[:3]),
+                                   MrtStrides(*c.V.stride()[:3]), *c.K_scale.stride()[:2], *c.V_scale.stride()[:2]), _CACHE_ADDRESSES)
         if len(_caches) >= _MAX_PROBLEMS:
             _caches.clear()
         _caches[key] = found
-    found = MrtCache8.from_buffer_copy(found)
-    found.k_codes, found.v_codes = c.K.data_ptr(), c.V.data_ptr()
-    found.k_scales, found.v_scales = c.K_scale.data_ptr(), c.V_scale.data_ptr()
-    return found
+    return _packed(found, (c.K.data_ptr(), c.V.data_ptr(), c.K_scale.data_ptr(), c.V_scale.data_ptr()))
+
+
+def _cache8_of(c):
+    return MrtCache8.from_buffer_copy(_cache8_bytes(c))
 
 
 # descriptions of recent rows without addresses, by their values, like _problems
 _rows: dict = {}
+
+
+_ROWS = struct.Struct(f"={MrtCache8Rows.at.offset}siQQ{ctypes.sizeof(MrtCache8Rows) - MrtCache8Rows.k.offset}s").pack
 
 
 def _cache8_rows(cache, K, V, at, lengths, given=True):
@@ -960,18 +988,12 @@ def _cache8_rows(cache, K, V, at, lengths, given=True):
         for name, x in (("at", None if number else at), ("lengths", lengths)):
             _require(x is None or (x.dtype == torch.int32 and x.shape == (B,) and x.is_contiguous()),
                      f"{name}: int32 [{B}], contiguous" + (", or a number" if name == "at" else ""))
-        found = MrtCache8Rows(K.shape[2], 0, None, None, MrtStrides(*K.stride()[:3]), MrtStrides(*V.stride()[:3]), _dtype_of(K, "K"))
+        found = bytes(MrtCache8Rows(K.shape[2], 0, None, None, MrtStrides(*K.stride()[:3]), MrtStrides(*V.stride()[:3]), _dtype_of(K, "K")))
+        found = found[:MrtCache8Rows.at.offset], found[MrtCache8Rows.k.offset:]
         if len(_rows) >= _MAX_PROBLEMS:
             _rows.clear()
         _rows[key] = found
-    found = MrtCache8Rows.from_buffer_copy(found)
-    if number:
-        found.at = at
-    else:
-        found.at_each = at.data_ptr()
-    if lengths is not None:
-        found.tokens_each = lengths.data_ptr()
-    return found
+    return _ROWS(found[0], at if number else 0, 0 if number else at.data_ptr(), 0 if lengths is None else lengths.data_ptr(), found[1])
 
 
 def _require_places(at, lengths=None):
@@ -990,8 +1012,7 @@ def cache8_write(cache, K, V, *, at=0, lengths=None, stream=None):
     _same_device(K, V, cache.K, cache.V, cache.K_scale, cache.V_scale, None if type(at) is int else at, lengths)
 
     def call(s):
-        c, rows = _cache8_of(cache), _cache8_rows(cache, K, V, at, lengths)
-        st = lib.mrt_cache8_write(ctypes.byref(c), ctypes.byref(rows), K.data_ptr(), V.data_ptr(), s)
+        st = lib.mrt_cache8_write(_cache8_bytes(cache), _cache8_rows(cache, K, V, at, lengths), K.data_ptr(), V.data_ptr(), s)
         if st != MRT_OK:
             _raise(lib, st)
     _run_on(K, stream, call)
@@ -1013,8 +1034,8 @@ def cache8_read(cache, tokens, *, at=0, dtype=None, out=None, v_out=None, stream
         K = torch.empty(B, H, tokens, d, dtype=given, device=cache.K.device) if out is None else out
         V = v_out if v_out is not None else torch.empty_like(K) if out is None else cache.K.new_empty((B, H, tokens, d), dtype=given)
         _require(K.shape[2] == tokens, f"the output has {K.shape[2]} tokens, not {tokens}")
-        c, rows = _cache8_of(cache), _cache8_rows(cache, K, V, at, None, out is not None or v_out is not None)
-        st = lib.mrt_cache8_read(ctypes.byref(c), ctypes.byref(rows), K.data_ptr(), V.data_ptr(), s)
+        rows = _cache8_rows(cache, K, V, at, None, out is not None or v_out is not None)
+        st = lib.mrt_cache8_read(_cache8_bytes(cache), rows, K.data_ptr(), V.data_ptr(), s)
         if st != MRT_OK:
             _raise(lib, st)
         return K, V
@@ -1037,9 +1058,9 @@ def _cache8_problem(Q, O, cache, c, f_q, f_kv, h, w, causal_chunk, q_frame_offse
         prob = make_problem(batch=B, heads=H, head_dim=d, f_q=f_q, f_kv=f_kv, h=h, w=w, q_frame_offset=q_frame_offset,
                             dtype=_dtype_of(Q, "Q"), scale=scale, q_strides=Q.stride()[:3], o_strides=O.stride()[:3])
         lib = load_library()
-        nbytes = int(lib.dense_attn_fwd_cache8_workspace_bytes(ctypes.byref(prob), ctypes.byref(c), causal_chunk))
+        nbytes = int(lib.dense_attn_fwd_cache8_workspace_bytes(ctypes.byref(prob), c, causal_chunk))
         if nbytes == 0:
-            st = lib.dense_attn_cache8_check(ctypes.byref(prob), ctypes.byref(c), causal_chunk)
+            st = lib.dense_attn_cache8_check(ctypes.byref(prob), ctypes.byref(MrtCache8.from_buffer_copy(c)), causal_chunk)
             if st != MRT_OK:
                 _raise(lib, st)
         if len(_cache8_problems) >= _MAX_PROBLEMS:
@@ -1050,7 +1071,7 @@ def _cache8_problem(Q, O, cache, c, f_q, f_kv, h, w, causal_chunk, q_frame_offse
 
 def dense_attn_fwd_cache8_workspace_bytes(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0) -> int:
     """Scratch that dense_attn_fwd_cache8 makes use of with these arguments (0: none)."""
-    return _cache8_problem(Q, Q, cache, _cache8_of(cache), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)[1]
+    return _cache8_problem(Q, Q, cache, _cache8_bytes(cache), f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)[1]
 
 
 def dense_attn_fwd_cache8(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_offset=0, scale=1.0, kv_len=None, out=None,
@@ -1069,12 +1090,13 @@ def dense_attn_fwd_cache8(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_
 
     def call(s):
         O = torch.empty_like(Q) if out is None else out
-        c = _cache8_of(cache)
+        c = _cache8_bytes(cache)
         prob, nbytes = _cache8_problem(Q, O, cache, c, f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)
         stats = Q.new_empty(Q.shape[:3], dtype=torch.float32) if lse is None else lse
         _require_lse(stats, Q)
-        _require(kv_len is None or (kv_len.dtype == torch.int32 and kv_len.shape == Q.shape[:1] and kv_len.is_contiguous()),
-                 f"kv_len: int32 [{Q.shape[0]}], contiguous")
+        if kv_len is not None:
+            _require(kv_len.dtype == torch.int32 and kv_len.shape == Q.shape[:1] and kv_len.is_contiguous(),
+                     f"kv_len: int32 [{Q.shape[0]}], contiguous")
         scratch = workspace
         if scratch is None and nbytes and not torch.cuda.is_current_stream_capturing():
             try:
@@ -1082,7 +1104,7 @@ def dense_attn_fwd_cache8(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_
             except torch.cuda.OutOfMemoryError:       # a call that fits without its scratch still runs
                 pass
         ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
-        st = lib.dense_attn_fwd_cache8(Q.data_ptr(), ctypes.byref(c), O.data_ptr(), stats.data_ptr(), ctypes.byref(prob),
+        st = lib.dense_attn_fwd_cache8(Q.data_ptr(), c, O.data_ptr(), stats.data_ptr(), ctypes.byref(prob),
                                        None if kv_len is None else kv_len.data_ptr(), causal_chunk, ws, nbytes, s)
         if st != MRT_OK:
             _raise(lib, st)
