@@ -401,13 +401,15 @@ FewShape few_shape(const KParams& kp, int nbh, int group, bool may_split, bool l
   // As many workgroups as the chip holds at once (two a compute unit, one of 64 rows), each with a tile for every wave.  us by the
   // number of parts: 12 heads 10 34.6, 20 25.5, 42 25.2, 64 26.6; 8 key heads, 4096 keys, 8 10.3, 16 9.2, 32 8.3, 64 9.5; one of 32760 keys 32
   // 13.5, 64 11.1, 96 10.3; 32 heads of 2048 keys, batch of 64, 1 199, 2 210, 8 226; 300 keys 1 6.3, 2 8.2, 6 7.2.
+  // Few keys are not parted: the second launch costs 5 us of host time besides (us, parted | not: 8 heads sharing 2, batch of 2, 500 keys
+  // 7.6 | 7.3, 1000 7.6 | 10.0; 16 heads of 64 features 700 7.5 | 6.3, 1000 7.2 | 7.1, 1400 7.3 | 8.5).
   const long long batch = nbh / kp.H;
   long long want = 2ll * compute_units() / (f.rt == 4 ? 2 : 1) / wgs;
   // Sequences of lengths of their own are cut where whole ones fill the chip, too: the longest would keep a part of it busy for long
   // (us, whole | three parts a sequence, 32 heads sharing 8, batch of 64, lengths 8192 and 63 of 300 60 | 30, any up to 8192 137 | 121,
   // any of 4096 .. 8192 160 | 167, all 8192 195 | 210; of 128, where whole ones take turns, up to 4096 123 | 134).
   if (lengths && want == 1 && batch > 1 && batch <= 256) want = 3;
-  const long long n = may_split && tiles > 12 && tiles * batch < 1ll << 30 ? std::max(1ll, std::min({want, tiles / kFewWaves, (long long)kMostFewParts})) : 1;
+  const long long n = may_split && tiles > (kp.d == 64 ? 32 : 16) && tiles * batch < 1ll << 30 ? std::max(1ll, std::min({want, tiles / kFewWaves, (long long)kMostFewParts})) : 1;
   f.part_tiles = (int)((tiles + n - 1) / n);
   f.parts = (int)((tiles + f.part_tiles - 1) / f.part_tiles);
   return f;

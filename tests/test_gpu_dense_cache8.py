@@ -39,6 +39,8 @@ CASES = {
     "token-lengths": Step(1, 4000, heads=2, kv_heads=1, batch=100, dim=64, kv_len=tuple(i * i * 31 % 4001 for i in range(100))),
     "token-fills": Step(1, 600, heads=16, kv_heads=8, batch=40, dim=64, kv_len=tuple(i * 77 % 601 for i in range(40))),
     "token-fills-4-rows": Step(4, 500, heads=16, kv_heads=1, batch=200, dim=64, kv_len=(500,) + (0, 7) * 99 + (499,)),
+    "token-fills-parted": Step(1, 600, heads=16, kv_heads=8, batch=40, kv_len=tuple(i * 77 % 601 for i in range(40))),
+    "token-fills-4-rows-parted": Step(4, 1100, heads=16, kv_heads=1, batch=200, dim=64, kv_len=(1100,) + (0, 7) * 99 + (1099,)),
     "token-one-long": Step(1, 20000, heads=8, kv_heads=1, batch=16, kv_len=(3, 0, 20000) + (0, 1, 33) * 4 + (0,)),
     "token-long-last": Step(1, 9000, heads=4, kv_heads=2, batch=3, kv_len=(0, 0, 8999)),
     "few-lengths-causal": Step(5, 900, heads=4, kv_heads=1, chunk=1, offset=880, batch=7, kv_len=(884, 1, 0, 881, 64, 900, 300)),
@@ -101,7 +103,7 @@ def test_attention(name, format, block):
             assert (got["O"][b, h].double() - want).norm() <= 4 * 2.0 ** -9 * math.sqrt(8 / 3) * want.norm() + 1e-30
 
 
-@pytest.mark.parametrize("name", ["token", "token-shared", "token-padded", "token-lengths", "token-fills", "token-one-long", "few-7-shared", "few-16-d64", "few-causal-padded", "frame",
+@pytest.mark.parametrize("name", ["token", "token-shared", "token-padded", "token-lengths", "token-fills-parted", "token-one-long", "few-7-shared", "few-16-d64", "few-causal-padded", "frame",
                                   "chunk-cache", "padded", "padded-by-length", "padded-by-length-d64", "padded-64", "text-late"])
 def test_scratch(name):
     """The caller's scratch, poisoned; too little, or none: the same work with fewer workgroups."""
