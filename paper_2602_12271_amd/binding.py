@@ -939,27 +939,27 @@ _CACHE_ADDRESSES = tuple(getattr(MrtCache8, name).offset for name in ("k_codes",
 
 def _cache8_bytes(c):
     """The C description of a cache."""
-    key = (c.K.shape, c.K.stride(), c.K.dtype, c.V.shape, c.V.stride(), c.V.dtype, _layout_of(c.K_scale), _layout_of(c.V_scale), c.block,
-           type(c.block))
+    K, V, ks, vs, block = c.K, c.V, c.K_scale, c.V_scale, c.block
+    key = (K.shape, K.stride(), K.dtype, V.shape, V.stride(), V.dtype, ks.shape, ks.stride(), ks.dtype, vs.shape, vs.stride(), vs.dtype,
+           block, type(block))
     found = _caches.get(key)
     if found is None:
         import torch
-        _require(c.K.dim() == 4 and c.V.shape == c.K.shape and c.K.dtype == c.V.dtype and
-                 c.K.dtype in (torch.float8_e4m3fn, torch.int8),
+        _require(K.dim() == 4 and V.shape == K.shape and K.dtype == V.dtype and K.dtype in (torch.float8_e4m3fn, torch.int8),
                  "K and V of a cache are [batch, heads, capacity, head_dim], torch.float8_e4m3fn or torch.int8")
-        _require(type(c.block) is int and c.block in (16, 32, 64, 128), "block is 16, 32, 64 or 128")
-        B, H, n, d = c.K.shape
-        blocks = -(-n // c.block)
-        for x in (c.K_scale, c.V_scale):
+        _require(type(block) is int and block in (16, 32, 64, 128), "block is 16, 32, 64 or 128")
+        B, H, n, d = K.shape
+        blocks = -(-n // block)
+        for x in (ks, vs):
             _require(x.dtype == torch.uint8 and x.shape == (B, H, blocks) and (blocks == 1 or x.stride(2) == 1),
                      f"scales of the cache are uint8 [{B}, {H}, {blocks}], blocks contiguous")
-        _require(c.K.stride(3) == 1 and c.V.stride(3) == 1, "head_dim must be contiguous")
-        found = _packing(MrtCache8(B, H, d, n, c.block, 0 if c.K.dtype == torch.float8_e4m3fn else 1, MrtStrides(*c.K.stride()[:3]),
-                                   MrtStrides(*c.V.stride()[:3]), *c.K_scale.stride()[:2], *c.V_scale.stride()[:2]), _CACHE_ADDRESSES)
+        _require(K.stride(3) == 1 and V.stride(3) == 1, "head_dim must be contiguous")
+        found = _packing(MrtCache8(B, H, d, n, block, 0 if K.dtype == torch.float8_e4m3fn else 1, MrtStrides(*K.stride()[:3]),
+                                   MrtStrides(*V.stride()[:3]), *ks.stride()[:2], *vs.stride()[:2]), _CACHE_ADDRESSES)
         if len(_caches) >= _MAX_PROBLEMS:
             _caches.clear()
         _caches[key] = found
-    return _packed(found, (c.K.data_ptr(), c.V.data_ptr(), c.K_scale.data_ptr(), c.V_scale.data_ptr()))
+    return _packed(found, (K.data_ptr(), V.data_ptr(), ks.data_ptr(), vs.data_ptr()))
 
 
 def _cache8_of(c):
@@ -1092,8 +1092,12 @@ def dense_attn_fwd_cache8(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_
         O = torch.empty_like(Q) if out is None else out
         c = _cache8_bytes(cache)
         prob, nbytes = _cache8_problem(Q, O, cache, c, f_q, f_kv, h, w, causal_chunk, q_frame_offset, scale)
-        stats = Q.new_empty(Q.shape[:3], dtype=torch.float32) if lse is None else lse
-        _require_lse(stats, Q)
+        if lse is None:
+            B, H, nq, _ = Q.shape
+            stats = torch.empty(B, H, nq, dtype=torch.float32, device=Q.device)
+        else:
+            stats = lse
+            _require_lse(stats, Q)
         if kv_len is not None:
             _require(kv_len.dtype == torch.int32 and kv_len.shape == Q.shape[:1] and kv_len.is_contiguous(),
                      f"kv_len: int32 [{Q.shape[0]}], contiguous")
