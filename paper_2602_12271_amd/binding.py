@@ -746,7 +746,7 @@ def rotary_bwd(dQ, dK=None, *, f_q=None, f_kv=None, h=None, w=None, q_frame_offs
 
 
 # ---- norms of queries and keys with their rotary positions ---------------------------------------
-# (description, tensors without addresses, how to fill these in, arrays of addresses) of recent calls by their values, like _problems
+# (description, tensors without addresses, how to fill these in, arrays of addresses, backward scratch) of recent calls by their values, like _problems
 _norm_problems: dict = {}
 
 
@@ -818,7 +818,11 @@ def _norm_problem(x, y, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_o
         tensors.append(MrtNormTensor(t, None, dtype, apart, strides, None))
     array = (MrtNormTensor * len(x))(*tensors)
     offsets = [i * ctypes.sizeof(MrtNormTensor) + at for i in range(len(x)) for at in _NORM_ADDRESSES]
-    found = r, array, _packing(array, offsets), struct.Struct(f"{len(x)}Q").pack
+    packing, nbytes = _packing(array, offsets), 0
+    if dx:                                       # (scratch: of a call whose addresses are there)
+        there = _packed(packing, [256 if t is not None else 0 for i in range(len(x)) for t in (positions[i], weights[i], weights[i])])
+        nbytes = load_library().mrt_norm_rotary_bwd_workspace_bytes(ctypes.byref(r), there, len(x))
+    found = r, array, packing, struct.Struct(f"{len(x)}Q").pack, nbytes
     if len(_norm_problems) >= _MAX_PROBLEMS:
         _norm_problems.clear()
     _norm_problems[key] = found
@@ -860,7 +864,7 @@ def norm_rotary_fwd(Q, K=None, q_weight=None, k_weight=None, *, eps=1e-6, f_q=No
             x.append(K)
             y.append(torch.empty_like(K, dtype=dtype) if k_out is None else k_out)
         weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
-        r, _, packing, pointers = _norm_problem(x, y, (), weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
+        r, _, packing, pointers, _ = _norm_problem(x, y, (), weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
                                              layout, ladder, positions, (dtype, out, k_out))
         tensors = _norm_tensors(packing, x, weights, positions)
         st = lib.mrt_norm_rotary_fwd(ctypes.byref(r), eps, tensors, len(x), pointers(*[t.data_ptr() for t in x]),
@@ -893,11 +897,11 @@ def norm_rotary_bwd(Q, K, q_weight, k_weight, dQ, dK=None, *, eps=1e-6, f_q=None
             g.append(dK)
             dx.append(torch.empty_like(K) if k_out is None else k_out)
         weights, positions = (_own_rows(q_weight), _own_rows(k_weight)), (q_positions, k_positions)
-        r, _, packing, pointers = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
+        r, _, packing, pointers, nbytes = _norm_problem(x, g, dx, weights, f_q, f_kv, h, w, q_frame_offset, kv_frame_offset, theta, split,
                                              layout, ladder, positions, (None, *g, out, k_out))
-        dw = [None if u is None else Q.new_empty(u.shape, dtype=torch.float32) for u in weights]
+        # (contiguous: rows of weights are, and rows apart come out side by side)
+        dw = [None if u is None else torch.empty_like(u, dtype=torch.float32) for u in weights]
         tensors = _norm_tensors(packing, x, weights, positions, dw)
-        nbytes = lib.mrt_norm_rotary_bwd_workspace_bytes(ctypes.byref(r), tensors, len(x))
         scratch = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if workspace is None and nbytes else workspace
         ws, nbytes = (None, 0) if scratch is None else (scratch.data_ptr(), scratch.numel() * scratch.element_size())
         st = lib.mrt_norm_rotary_bwd(ctypes.byref(r), eps, tensors, len(x), pointers(*[t.data_ptr() for t in x]),
