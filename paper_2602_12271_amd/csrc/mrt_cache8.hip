@@ -116,6 +116,8 @@ __global__ __launch_bounds__(kThreadsCache) void k_cache8_write(const Cache8Call
   const T* rows = (const T*)side.rows + b * side.rs.batch + head * side.rs.head;
   const int per = c.d / kItem, items = runs ? per << c.shift : 0;
   const int old = runs && first < lo ? exps[block] : 0;
+  // An infinity does not take the scale of a block whose earlier rows are kept: under 2^119 they would be zeros.
+  const unsigned largest = first < lo ? kInf - 1 : kInf;
   Item<T> x[ITEMS];
   unsigned top = 0;
 #pragma unroll
@@ -135,7 +137,7 @@ __global__ __launch_bounds__(kThreadsCache) void k_cache8_write(const Cache8Call
 #pragma unroll
     for (int e = 0; e < kItem; ++e) {
       const unsigned m = x[i].bits(e) & 0x7fffffffu;
-      top = max(top, m > kInf ? 0u : m);
+      top = max(top, m > largest ? 0u : m);
     }
   }
 #pragma unroll
