@@ -434,8 +434,9 @@ void mrt_set_head_groups(int n);
 
 /* Per-kernel timing for benchmarks.  mrt_profile_enable(r) with r >= 1 (at most 64) makes the two
  * entry points above issue every kernel launch r times in a row between a pair of HIP events
- * recorded on the launch's stream; r = 0 switches this off.  Every kernel reads only buffers it
- * does not write, so the repeated launches leave the same result; r > 1 spreads the cost of the
+ * recorded on the launch's stream; r = 0 switches this off.  The repeated launches leave the same
+ * result; calls whose output is in the place of an input, where they would not, run once and are
+ * not recorded.  r > 1 spreads the cost of the
  * event pair and of the first dispatch over r launches.  This is the only mode in which the
  * library creates HIP objects, and while it is on head groups run one after the other.
  * mrt_profile_read waits for the recorded events, writes up to `capacity` (elapsed milliseconds

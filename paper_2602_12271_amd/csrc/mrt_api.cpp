@@ -260,8 +260,9 @@ static std::atomic<int> g_prof_on{0};   // 0 = off, r > 0 = each launch issued r
 static std::vector<ProfRecord> g_prof;
 static std::mutex g_prof_mu;
 
-// Runs `launch` once, or, while profiling, g_prof_on times between two events.  Every kernel of
-// this library reads only buffers it does not write, so a repeated launch leaves the same result.
+// Runs `launch` once, or, while profiling, g_prof_on times between two events.  A repeated launch leaves the same result: kernels
+// read only buffers they do not write, but for those of a call with its output in the place of an input (may_time is false then) and
+// the cache's writing kernel, which finds its own bytes and forms them again.
 template <class F>
 static hipError_t timed_launch(hipStream_t s, int kind, F launch, bool may_time = true) {
   const int reps = may_time ? g_prof_on.load(std::memory_order_relaxed) : 0;
@@ -436,7 +437,7 @@ mrt_status fwd_run(const void* Q, const void* K, const void* V, void* O, const m
     const size_t inter_per_launch = pl.slab_aL * per_head * G;
     want_groups = (inter_per_launch >= (size_t(128) << 20) && pl.T >= 2) ? 2 : 1;
   }
-  const bool may_time = !own_stream_only;
+  const bool may_time = !own_stream_only && O != Q;
   StreamPool* pool = (own_stream_only || g_prof_on.load() || want_groups <= 1) ? nullptr : get_pool();
   std::unique_lock<std::mutex> pool_lock;
   if (pool) pool_lock = std::unique_lock<std::mutex>(pool->in_use);
@@ -871,7 +872,7 @@ mrt_status dense_attn_fwd_ws(const void* Q, const void* K, const void* V, void* 
   hipError_t e = timed_launch((hipStream_t)hip_stream, MRT_KERNEL_DENSE, [&] {
     return f32 ? launch_f32_dense(kp, p->dtype, BH, (hipStream_t)hip_stream)
                : launch_bf16_dense(kp, BH, workspace, workspace_bytes, nullptr, (hipStream_t)hip_stream);
-  });
+  }, O != Q);
   if (e != hipSuccess) return hip_fail(e, "dense launch");
   return MRT_OK;
 }
@@ -1386,7 +1387,7 @@ mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, fl
   };
   const hipError_t e = timed_launch(s, MRT_KERNEL_DENSE, [&] {
     return c->format == MRT_CACHE_E4M3 ? run(DenseCache8<true>()) : run(DenseCache8<false>());
-  });
+  }, O != Q);
   if (e != hipSuccess) return hip_fail(e, "dense launch");
   return MRT_OK;
 }
