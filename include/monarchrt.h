@@ -396,6 +396,7 @@ mrt_status mrt_norm_rotary_bwd(const mrt_rotary* r, double eps, const mrt_norm_t
  *   to bf16.  dense_attn_fwd_cache8_workspace_bytes: scratch that the call makes use of (0: none); without it the call does the same work
  *   with fewer workgroups, and its results differ by roundings.  The same call gives the same bits every time; with kv_len the other
  *   sequences' lengths, too, decide where a sequence's keys are parted, and so its roundings.
+ *   O may be Q itself, with Q's strides, as for monarch_attn_fwd.
  *   Limits, as for dense_attn_fwd_save, and: heads / key heads whole. */
 typedef enum { MRT_CACHE_E4M3 = 0, MRT_CACHE_INT8 = 1 } mrt_cache_format;
 typedef struct {

@@ -1367,6 +1367,12 @@ mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, fl
   for (const void* x : {c->k_codes, c->v_codes, (void*)c->k_scales, (void*)c->v_scales})
     if (x == O || x == lse) { set_error("an output in the place of the cache"); return MRT_ERR_SHAPE; }
   if (O == lse || Q == lse) { set_error("lse in the place of Q or O"); return MRT_ERR_SHAPE; }
+  const bool in_place = O == Q;
+  if (in_place && (((long long)p->f_q * p->h * p->w > 1 && p->q.token != p->o.token) || (p->heads > 1 && p->q.head != p->o.head) ||
+                   (p->batch > 1 && p->q.batch != p->o.batch))) {
+    set_error("O in the place of Q needs Q's strides");
+    return MRT_ERR_SHAPE;
+  }
   if ((uintptr_t)workspace % 256) { set_error("workspace must be 256-byte aligned"); return MRT_ERR_WORKSPACE; }
   const mrt_problem q = cache8_problem(p, c);
   KParams kp = dense_params(&q, causal_chunk);
@@ -1387,7 +1393,7 @@ mrt_status dense_attn_fwd_cache8(const void* Q, const mrt_cache8* c, void* O, fl
   };
   const hipError_t e = timed_launch(s, MRT_KERNEL_DENSE, [&] {
     return c->format == MRT_CACHE_E4M3 ? run(DenseCache8<true>()) : run(DenseCache8<false>());
-  }, O != Q);
+  }, !in_place);
   if (e != hipSuccess) return hip_fail(e, "dense launch");
   return MRT_OK;
 }
