@@ -380,7 +380,8 @@ mrt_status mrt_norm_rotary_bwd(const mrt_rotary* r, double eps, const mrt_norm_t
  *   its largest finite magnitude, new rows and kept ones, to 448 (127) or below, within 2^-124 .. 2^119; codes are the nearest, ties
  *   to even.  So a value is off by at most 2^-4 of itself (e4m3; 2^-10 of the scale below 2^-6 of it), or by half the scale, which
  *   above 2^-124 is less than 1/127 of the block's largest magnitude (whole numbers).  Where the scale grows kept rows are rounded
- *   again: an e4m3 code only where it turns subnormal, a whole number by less than one unit of the final scale in all, however often.
+ *   again: an e4m3 code only where it turns subnormal, a whole number by less than one unit of the largest scale that the block has
+ *   had since they came, in all, however often.  Replacing the rows behind them by smaller ones does not undo that.
  *   Infinite and larger magnitudes become the largest code; NaN stays NaN in e4m3 and becomes 0 in whole numbers.  An infinity leaves
  *   the scale of a block that keeps rows to the finite magnitudes; a block that keeps none has the largest scale, 2^119, with it,
  *   under which numbers below 2^109 (2^118) become 0.

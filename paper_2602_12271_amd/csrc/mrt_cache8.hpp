@@ -3,7 +3,8 @@
 // A power of two, held as its exponent + 127: a code times its scale then is a bf16 number exactly (4 or 7 significant
 // bits), which the matrix unit takes as it is, and a scale that has to grow when rows are appended to a block rounds the
 // rows that are there by a whole number of halvings: not at all for e4m3 codes that stay normal, and by less than one new
-// step in all, however often, for whole numbers (each halving adds half a new step, and halves what was there before).
+// step in all, however often, for whole numbers (each halving adds half a new step, and halves what was there before).  A scale
+// that shrinks again, since the rows behind were replaced, gives nothing back of that.
 // Against the scale max / 127 it costs whole numbers up to one bit; e4m3 codes, whose precision is relative, nothing.
 #pragma once
 #include "mrt_internal.hpp"

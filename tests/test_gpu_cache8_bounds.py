@@ -51,3 +51,30 @@ def test_kernels(format):
         values = values.cpu()[0, 0]
         values = (values.flip(1) if flip else values).reshape(x.shape)
         check(x, values, 2.0 ** (scales.cpu()[0, 0, :, None].double() - 127), format)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("format", ["e4m3", "int8"])
+def test_rows_behind_are_replaced(format):
+    """A block's last rows written again and again, larger and smaller: the rows before them are off by what the largest scale costs."""
+    gen = torch.Generator().manual_seed(5)
+    block, n, first = 32, 8, 20
+    kept = torch.randn(1, 1, first, 64, generator=gen)
+    cache, host = pkg.cache8(1, 1, block, 64, format=format, block=block), HostCache(block, 64, block, format)
+    pkg.cache8_write(cache, kept.cuda(), kept.cuda())
+    host.write(kept[0, 0], 0)
+    largest = int(host.bytes[0])
+    for size in (1.0, 40.0, 3.0, 11.0, 0.01):
+        rows = size * torch.randn(1, 1, n, 64, generator=gen)
+        pkg.cache8_write(cache, rows.cuda(), rows.cuda(), at=first)
+        host.write(rows[0, 0], first)
+        largest = max(largest, int(host.bytes[0]))
+        values = pkg.cache8_read(cache, first, dtype=torch.float32)[0][0, 0].cpu().double()
+        assert torch.equal(values, host.values(torch.arange(first)))
+        off, unit = (values - kept[0, 0].double()).abs(), 2.0 ** (largest - 127)
+        # an e4m3 code: rounded once as a normal one, 2^-4 of it; where growing scales make it subnormal, by 2^-10 of each, 2^-9 of the
+        # largest in all; a whole number by half of each, one unit of the largest in all
+        assert (off <= (2.0 ** -4 * kept[0, 0].double().abs() + 2.0 ** -9 * unit if format == "e4m3" else unit)).all()
+    assert int(host.bytes[0]) < largest
+    if format == "int8":
+        assert off.max() > 2.0 ** (int(host.bytes[0]) - 127)          # more than one unit of the last scale
