@@ -1009,8 +1009,9 @@ def _require_places(at, lengths=None):
 def cache8_write(cache, K, V, *, at=0, lengths=None, stream=None):
     """Rows K and V, [batch, heads, tokens, head_dim], fp32 or bf16, into the cache, from token `at` on: a number, or int32
     [batch] on the device (rows outside the cache are then left out).  lengths (int32 [batch], on the device): rows of every
-    sequence that are there.  Rows before `at` keep their values; what was behind the new ones in their last block is no longer
-    part of the cache.  The rounding is in the header's comment."""
+    sequence that are there.  Rows before `at` keep their values.  A write ends its last block: what was behind the new rows in it
+    is lost, so rows inside a cache are replaced up to a multiple of the block (4680 tokens are not one), or with those that
+    follow up to there.  The rounding is in the header's comment."""
     lib = load_library()
     _require_places(at, lengths)
     _same_device(K, V, cache.K, cache.V, cache.K_scale, cache.V_scale, None if type(at) is int else at, lengths)
@@ -1082,7 +1083,7 @@ def dense_attn_fwd_cache8(Q, cache, *, f_q, f_kv, h, w, causal_chunk=0, q_frame_
                           lse=None, workspace=None, stream=None):
     """Dense attention of bf16 queries [batch, heads, tokens, head_dim] over the first f_kv h w tokens of a cache, whose heads
     divide those of Q: (O, lse), as dense_attn_fwd_save gives them.  kv_len (int32 [batch], on the device): tokens that each
-    sequence has.  The cache's values take part exactly; the probabilities are rounded to bf16.
+    sequence has.  out may be Q itself.  The cache's values take part exactly; the probabilities are rounded to bf16.
 
     Calls of few queries share their keys over several workgroups if they have scratch memory
     (dense_attn_fwd_cache8_workspace_bytes): `workspace`, or memory of torch's allocator.  Without `workspace` a call under a
